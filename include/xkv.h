@@ -271,6 +271,112 @@ XKV_API int xkv_dense_attend(xkv_group* grp, int layer_begin, int layer_end, con
                              float* lse, void* stream);
 
 /*
+ * Drafted tokens and bounded caches over an UNCOMPRESSED bf16 cache (the layout of xkv_dense_attend, or of the tail):
+ *   xkv_tree_attend     attention of a tree of drafted tokens (speculative decoding)
+ *   xkv_tree_commit     the accepted path becomes the next rows of the cache
+ *   xkv_cache_weigh     the attention weight that every row has drawn so far
+ *   xkv_evict_select    which rows stay: the recent ones, then those of the largest weight
+ *   xkv_evict_compact   the rows that stay close the holes
+ * K, V are bf16 [G][batch][H_kv][cap][d_h]; sequence b holds len[b] rows in every head of every layer, keys as the model stores
+ * them (rotated), so the order of rows carries no meaning; a row's age, where it matters, is its token position in
+ *   pos  int32 [G][batch][H_kv][cap], kept by the caller's calls of xkv_tree_commit and xkv_evict_compact.
+ * No handle and no allocation: a call gets the cache's sizes in a host struct and everything else as device pointers.  What is
+ * behind the last row of a sequence is neither read into a result nor written, whatever it holds.
+ * flags  one device word or NULL: bits XKV_FLAG_INDEX_RANGE (a length or row index was out of range: lengths are clamped, rows
+ *        skipped) and XKV_FLAG_TIMEOUT (a bounded wait ran out, outputs unspecified) are OR-ed in; the caller clears it.
+ * Limits: d_h 64 or 128, H_q a multiple of H_kv with H_q/H_kv <= 16, 1 <= cap <= XKV_CACHE_MAX_ROWS,
+ * G*batch*H_kv <= 65535, G*batch*H_kv*cap < 2^31 (else UNSUPPORTED).  Data pointers are 16-byte aligned, int32 and fp32 arrays 4-byte.
+ * Layers layer_begin <= l < layer_end are worked on; arrays span all G layers.  Calls may run at the same time as long as they
+ * share no output and no workspace.
+ * Errors of all of them: INVALID_ARG, UNSUPPORTED, ARCH, CUDA.
+ */
+#define XKV_CACHE_MAX_ROWS (1 << 22)
+typedef struct {
+  uint32_t struct_size; /* sizeof(xkv_cache_config) */
+  int32_t G, batch, H_kv, H_q, d_h;
+  int32_t cap;          /* rows that a head's part of the cache has room for */
+  float softmax_scale;  /* logit scale; 0 means 1/sqrt(d_h) */
+} xkv_cache_config;
+
+/*
+ * Attention of up to n_draft drafted tokens per sequence.  The first len[b] rows of sequence b are its committed tokens; the
+ * keys and values of its draft j are row len[b] + j.  Token i attends to every committed row and to the drafts j of its mask:
+ *   out_i = softmax(scale * q_i K^T) V over those rows,  lse_i = ln sum exp of the scaled logits.
+ * n_draft    1 <= n_draft <= min(XKV_TREE_MAX_DRAFT, cap).  One token without a tree is a decode step (n_draft = 1, mask NULL).
+ * q          bf16 [G][batch][n_draft][H_q][d_h], rotated.
+ * mask       uint32 [batch][n_draft][W], W = ceil(n_draft/32): bit j % 32 of word j / 32 of token i is set if it attends to draft j
+ *            (its own bit included).  NULL: a chain, token i attends to drafts 0 .. i.
+ * draft_len  int32 [batch] or NULL for n_draft in every sequence: drafts of the sequence.  out and lse of tokens at and behind
+ *            draft_len[b] are left as they were, mask bits of drafts behind it are ignored.
+ * len        int32 [batch] or NULL for cap - n_draft; len[b] + draft_len[b] <= cap (else len is clamped, flag raised).
+ * workspace  device scratch of xkv_tree_workspace_bytes(cfg, n_draft) bytes, 16-byte aligned, used during the call's kernels only:
+ *            calls that may overlap (two streams, two captured graphs that are replayed at once) need one each.
+ * out        bf16 [G][batch][n_draft][H_q][d_h];  lse  optional fp32 [G][batch][n_draft][H_q].
+ * A token that attends to nothing (len = 0 and an empty mask), or whose logits are all minus infinity, gets 0 and lse -inf.
+ * A row that a token does not attend to has no influence on it, also where its keys or values are not finite.
+ * Weights are rounded to bf16 for the product with the values; sums, maxima and the product's accumulation are fp32.
+ */
+#define XKV_TREE_MAX_DRAFT 256
+XKV_API int xkv_tree_workspace_bytes(const xkv_cache_config* cfg, int32_t n_draft, uint64_t* bytes);
+XKV_API int xkv_tree_attend(const xkv_cache_config* cfg, int layer_begin, int layer_end, const void* q, int32_t n_draft,
+                            const uint32_t* mask, const int32_t* draft_len, const void* K, const void* V, const int32_t* len,
+                            void* workspace, uint64_t workspace_bytes, void* out, float* lse, uint32_t* flags, void* stream);
+
+/*
+ * Takes an accepted path into the cache: for j < path_len[b], row len[b] + j of K and V becomes what row len[b] + path[b][j] was
+ * before the call (all rows are read before any is written), in every head, and pos[len[b] + j] = first_pos[b] + j.
+ * path       int32 [batch][n_path], draft indices in any order; an entry below 0 or with len[b] + entry >= cap is skipped (flag).
+ * path_len   int32 [batch] or NULL for n_path;  0 <= path_len <= n_path <= XKV_TREE_MAX_DRAFT.
+ * len        int32 [batch], the rows before the drafts; rows at or behind cap are not written (flag).  The caller adds path_len.
+ * pos        int32 [G][batch][H_kv][cap] or NULL (then first_pos is not read);  first_pos  int32 [batch].
+ */
+XKV_API int xkv_tree_commit(const xkv_cache_config* cfg, int layer_begin, int layer_end, void* K, void* V, const int32_t* len,
+                            const int32_t* path, const int32_t* path_len, int32_t n_path, int32_t* pos,
+                            const int32_t* first_pos, uint32_t* flags, void* stream);
+
+/*
+ * Adds to every row's weight what the attention of n_tok tokens gave it:
+ *   weights[j] = (j < seen[b] ? decay * weights[j] : 0) + sum over tokens i with j < visible[b][i] and the query heads h of the
+ *                KV head of exp(scale * q_ih . k_j - lse_ih),   for the rows j < len[b]; others are left as they were.
+ * q          bf16 [G][batch][n_tok][H_q][d_h], 1 <= n_tok <= XKV_TREE_MAX_DRAFT: with n_tok = 1 the layout of xkv_dense_attend.
+ * lse        fp32 [G][batch][n_tok][H_q] of the same attention (xkv_tree_attend, xkv_dense_attend); -inf: nothing is added.
+ * visible    int32 [batch][n_tok] or NULL for len[b]: rows that token i attended to, 0 for one that was turned down
+ *            (clamped to 0 .. len[b], flag).
+ * len        int32 [batch] or NULL for cap (clamped to 0 .. cap, flag).
+ * seen       int32 [batch] or NULL for len[b]: rows that hold an earlier weight; the rows behind them are new (clamped likewise).
+ * decay      0 <= decay <= 1; with 0 earlier weights are not read.
+ * weights    fp32 [G][batch][H_kv][cap], in and out.  Sums are fp32 in an order that does not change from call to call.
+ */
+XKV_API int xkv_cache_weigh(const xkv_cache_config* cfg, int layer_begin, int layer_end, const void* q, int32_t n_tok,
+                            const float* lse, const void* K, const int32_t* len, const int32_t* visible, const int32_t* seen,
+                            float decay, float* weights, uint32_t* flags, void* stream);
+
+/*
+ * Which `keep` of a head's len[b] rows stay: the first in the order (recent before not recent, weight descending, row
+ * ascending), where a row is recent if its position is >= since[b].  A weight that is NaN counts as -inf, -0 as 0.
+ * The result says how to close the holes: src[j] for j < keep is the row whose content row j has to get --
+ *   j itself where row j stays; else, for the i-th row below keep that does not stay, the i-th row at or behind keep that does.
+ * With len[b] <= keep every row stays: src[j] = j for j < len[b] and -1 behind.  min(len, keep) rows are left.
+ * weights    fp32 [G][batch][H_kv][cap];  pos  int32 of the same shape, or NULL: a row's index is its position.
+ * since      int32 [batch] or NULL: no row counts as recent.
+ * len        int32 [batch] or NULL for cap (clamped to 0 .. cap, flag).
+ * keep       1 <= keep <= cap;  cap <= XKV_EVICT_MAX_ROWS (else UNSUPPORTED).
+ * src        out int32 [G][batch][H_kv][keep].
+ */
+#define XKV_EVICT_MAX_ROWS (1 << 18)
+XKV_API int xkv_evict_select(const xkv_cache_config* cfg, int layer_begin, int layer_end, const float* weights,
+                             const int32_t* pos, const int32_t* since, const int32_t* len, int32_t keep, int32_t* src,
+                             uint32_t* flags, void* stream);
+
+/*
+ * Closes the holes in place: for j < keep, row j of K and V (and its weight and position) becomes row src[j].  Entries that are
+ * j or negative change nothing; the others must be >= keep and < cap (else skipped, flag), so no row is both read and
+ * written.  Rows at and behind keep are left as they were.  weights and pos may be NULL.
+ */
+XKV_API int xkv_evict_compact(const xkv_cache_config* cfg, int layer_begin, int layer_end, void* K, void* V, const int32_t* src,
+                              int32_t keep, float* weights, int32_t* pos, uint32_t* flags, void* stream);
+
+/*
  * Algorithm 1 (App. B.1), the prefill side of the selector, for every sequence, layer and KV head g:
  *   landmark[j]  = mean over the rows x of chunk j of rope(K[x]),  chunk j = rows c*j .. min(c*j+c, T)-1   (lines 1-3)
  *   min_cos[j]   = min over those rows of cos(rope(K[x]), landmark[j])  (fp32, the unrounded mean; a zero vector
@@ -345,7 +451,10 @@ XKV_API uint64_t xkv_kernel_launch_count(void);
 #define XKV_KERNEL_DENSE 9     /* merge of dense-attention partials (xkv_dense_attend) */
 #define XKV_KERNEL_CLF 10      /* cross-layer factorisation (xkv_clf_factorize) */
 #define XKV_KERNEL_MERGE_MULTI 11 /* the same merge with one CTA per group of query heads (windows of many problems) */
-#define XKV_KERNEL_FAMILIES 12
+#define XKV_KERNEL_TREE 12       /* attention of drafted tokens, its merge, the commit of a path */
+#define XKV_KERNEL_WEIGH 13      /* accumulated attention weights */
+#define XKV_KERNEL_EVICT 14      /* which rows of a cache stay, and their move */
+#define XKV_KERNEL_FAMILIES 15
 XKV_API int xkv_debug_launch_counts(uint64_t* counts);
 
 /*

@@ -17,6 +17,15 @@ static std::atomic<uint64_t> g_launches[kFamCount];
 void set_cuda_error(cudaError_t e) { g_last_cuda_error = (int)e; }
 void count_launch(KernelFamily family, int n) { g_launches[family].fetch_add((uint64_t)n, std::memory_order_relaxed); }
 
+// The current device, if it is one that the kernels run on.
+int current_sm100_device(int* device) {
+  int major = 0;
+  cudaError_t e = cudaGetDevice(device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *device);
+  if (e != cudaSuccess) { set_cuda_error(e); (void)cudaGetLastError(); return XKV_ERR_CUDA; }
+  return major == 10 ? XKV_OK : XKV_ERR_ARCH;
+}
+
 static int check_config(const xkv_group_config* c, bool need_ptrs) {
   if (!c) return XKV_ERR_INVALID_ARG;
   if (c->struct_size != sizeof(xkv_group_config)) return XKV_ERR_INVALID_ARG;
@@ -434,14 +443,6 @@ int xkv_sr_reconstruct_attend_tail(xkv_group* g, int layer_begin, int layer_end,
                                               (float*)workspace});
   if (e != cudaSuccess) { set_cuda_error(e); (void)cudaGetLastError(); return XKV_ERR_CUDA; }
   return XKV_OK;
-}
-
-static int current_sm100_device(int* device) {
-  int major = 0;
-  cudaError_t e = cudaGetDevice(device);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *device);
-  if (e != cudaSuccess) { set_cuda_error(e); (void)cudaGetLastError(); return XKV_ERR_CUDA; }
-  return major == 10 ? XKV_OK : XKV_ERR_ARCH;
 }
 
 int xkv_clf_rank_l(const xkv_clf_config* cfg, int32_t* l) {

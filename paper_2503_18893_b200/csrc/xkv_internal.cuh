@@ -76,6 +76,7 @@ struct xkv_group {
 namespace xkv {
 
 void set_cuda_error(cudaError_t e);
+int current_sm100_device(int* device);         // an xkv_status
 
 // (cos, sin) of rotary pair i in a row of the tables: a pair of frequencies is four floats {cos, cos, sin, sin}, so that
 // packed fp32 arithmetic finds its operands side by side.
@@ -105,6 +106,7 @@ enum KernelFamily {
   kFamScan = XKV_KERNEL_SCAN, kFamTopk = XKV_KERNEL_TOPK, kFamFused = XKV_KERNEL_FUSED, kFamMerge = XKV_KERNEL_MERGE,
   kFamTile = XKV_KERNEL_TILE, kFamTailTc = XKV_KERNEL_TAIL_TC, kFamTailCuda = XKV_KERNEL_TAIL_CUDA,
   kFamLandmarks = XKV_KERNEL_LANDMARKS, kFamPrep = XKV_KERNEL_PREP, kFamDense = XKV_KERNEL_DENSE, kFamClf = XKV_KERNEL_CLF, kFamMergeMulti = XKV_KERNEL_MERGE_MULTI,
+  kFamTree = XKV_KERNEL_TREE, kFamWeigh = XKV_KERNEL_WEIGH, kFamEvict = XKV_KERNEL_EVICT,
   kFamCount = XKV_KERNEL_FAMILIES
 };
 void count_launch(KernelFamily family, int n = 1);
@@ -213,6 +215,27 @@ int clf_factorize(const xkv_clf_config* c, const void* X, const void* omega, voi
                   void* A_out, void* B_out, float* sigma, int device, cudaStream_t s);
 cudaError_t clf_gemm(const void* a, const void* b, int M, int N, int K, float* C, unsigned int* flags, int device,
                      cudaStream_t s);
+
+// xkv_tree.cu
+size_t tree_part_floats(const xkv_cache_config* c, int n_draft);
+cudaError_t launch_tree_attend(const xkv_cache_config* c, int l0, int l1, const __nv_bfloat16* q, int n_draft, const uint32_t* mask,
+                               const int32_t* draft_len, const __nv_bfloat16* K, const __nv_bfloat16* V, const int32_t* len,
+                               float* workspace, __nv_bfloat16* out, float* lse, unsigned int* flags, int device, cudaStream_t s);
+
+// xkv_weigh.cu
+cudaError_t launch_cache_weigh(const xkv_cache_config* c, int l0, int l1, const __nv_bfloat16* q, int n_tok, const float* lse,
+                               const __nv_bfloat16* K, const int32_t* len, const int32_t* visible, const int32_t* seen, float decay,
+                               float* weights, unsigned int* flags, int device, cudaStream_t s);
+
+// xkv_evict.cu
+cudaError_t launch_tree_commit(const xkv_cache_config* c, int l0, int l1, __nv_bfloat16* K, __nv_bfloat16* V, const int32_t* len,
+                               const int32_t* path, const int32_t* path_len, int n_path, int32_t* pos, const int32_t* first_pos,
+                               unsigned int* flags, cudaStream_t s);
+cudaError_t launch_evict_select(const xkv_cache_config* c, int l0, int l1, const float* weights, const int32_t* pos,
+                                const int32_t* since, const int32_t* len, int keep, int32_t* src, unsigned int* flags, int device,
+                                cudaStream_t s);
+cudaError_t launch_evict_compact(const xkv_cache_config* c, int l0, int l1, __nv_bfloat16* K, __nv_bfloat16* V, const int32_t* src,
+                                 int keep, float* weights, int32_t* pos, unsigned int* flags, cudaStream_t s);
 
 // xkv_fused.cu
 int fused_slots(const xkv_group* grp);

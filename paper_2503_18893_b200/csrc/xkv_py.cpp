@@ -239,6 +239,152 @@ PyObject* dequantize_rtn(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- operators over an uncompressed cache.  Their tensors are checked here for type, layout, size and device before any address
+// reaches a kernel: the calls take many arrays whose shapes have to agree with one host struct.
+struct Checked : Args {
+  const xkv_cache_config* cfg;
+  long device;
+  Checked(PyObject* const* args, Py_ssize_t have, Py_ssize_t want) : Args(args, have, want), cfg(nullptr), device(-1) {}
+  bool config() {
+    cfg = (const xkv_cache_config*)ptr();
+    if (!bad && !cfg) {
+      PyErr_SetString(PyExc_ValueError, "no cache configuration");
+      bad = true;
+    }
+    if (bad) return false;
+    PyObject* dev = PyObject_CallNoArgs(g_get_device);
+    if (dev) {
+      device = PyLong_AsLong(dev);
+      Py_DECREF(dev);
+    }
+    bad = !dev || (device == -1 && PyErr_Occurred());
+    return !bad;
+  }
+  int64_t heads() const { return (int64_t)cfg->G * cfg->batch * cfg->H_kv; }
+  int64_t tokens(int64_t n) const { return (int64_t)cfg->G * cfg->batch * n * cfg->H_q; }
+  // at_least: the tensor may be larger (a workspace)
+  void* tensor(const char* name, at::ScalarType type, int64_t numel, bool optional = false, bool at_least = false) {
+    PyObject* o = next();
+    if (!o) return nullptr;
+    if (o == Py_None && optional) return nullptr;
+    if (!THPVariable_Check(o)) {
+      PyErr_Format(PyExc_TypeError, "%s: expected a tensor%s", name, optional ? " or None" : "");
+      bad = true;
+      return nullptr;
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    const char* what = nullptr;
+    if (t.scalar_type() != type && !(type == at::kInt && t.scalar_type() == at::kUInt32)) what = "has another type";
+    else if (!t.is_cuda() || t.get_device() != device) what = "is not on the current CUDA device";
+    else if (!t.is_contiguous()) what = "is not contiguous";
+    else if (at_least ? t.numel() < numel : t.numel() != numel) what = "has another number of elements";
+    if (what) {
+      PyErr_Format(PyExc_ValueError, "%s: the tensor %s (of type %s, %lld elements%s expected)", name, what, c10::toString(type),
+                   (long long)numel, at_least ? " at least" : "");
+      bad = true;
+      return nullptr;
+    }
+    return const_cast<void*>(t.const_data_ptr());
+  }
+  float real() {
+    PyObject* o = next();
+    if (!o) return 0.0f;
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) bad = true;
+    return (float)x;
+  }
+};
+#define XKV_CACHE_PY(name, want) \
+  PyObject* name(PyObject*, PyObject* const* args, Py_ssize_t nargs) { \
+    HANDLE_TH_ERRORS \
+    Checked a(args, nargs, want); \
+    if (a.bad || !a.config()) return nullptr; \
+    const xkv_cache_config* c = a.cfg; \
+    const int l0 = a.i32(), l1 = a.i32();
+#define XKV_CACHE_PY_END(call) \
+    if (a.bad) return nullptr; \
+    int st; \
+    { \
+      const WithoutGil no_gil; \
+      st = call; \
+    } \
+    return PyLong_FromLong(st); \
+    END_HANDLE_TH_ERRORS \
+  }
+
+XKV_CACHE_PY(tree_attend, 15)
+  const int n = a.i32();
+  const int64_t rows = a.heads() * c->cap * c->d_h, queries = a.tokens(n);
+  void* q = a.tensor("q", at::kBFloat16, queries * c->d_h);
+  const uint32_t* mask = (const uint32_t*)a.tensor("mask", at::kInt, (int64_t)c->batch * n * (((int64_t)n + 31) / 32), true);
+  const int32_t* drafts = (const int32_t*)a.tensor("draft_len", at::kInt, c->batch, true);
+  void* K = a.tensor("K", at::kBFloat16, rows);
+  void* V = a.tensor("V", at::kBFloat16, rows);
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch, true);
+  if (a.bad) return nullptr;
+  uint64_t need = 0;
+  const int refused = xkv_tree_workspace_bytes(c, n, &need);
+  if (refused != XKV_OK) return PyLong_FromLong(refused);
+  void* ws = a.tensor("workspace", at::kByte, (int64_t)need, false, true);
+  void* out = a.tensor("out", at::kBFloat16, queries * c->d_h);
+  float* lse = (float*)a.tensor("lse", at::kFloat, queries, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  void* s = a.stream();
+XKV_CACHE_PY_END(xkv_tree_attend(c, l0, l1, q, n, mask, drafts, K, V, len, ws, need, out, lse, flags, s))
+
+XKV_CACHE_PY(tree_commit, 13)
+  const int64_t rows = a.heads() * c->cap;
+  void* K = a.tensor("K", at::kBFloat16, rows * c->d_h);
+  void* V = a.tensor("V", at::kBFloat16, rows * c->d_h);
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch);
+  const int n = a.i32();
+  const int32_t* path = (const int32_t*)a.tensor("path", at::kInt, (int64_t)c->batch * n);
+  const int32_t* path_len = (const int32_t*)a.tensor("path_len", at::kInt, c->batch, true);
+  int32_t* pos = (int32_t*)a.tensor("pos", at::kInt, rows, true);
+  const int32_t* first = (const int32_t*)a.tensor("first_pos", at::kInt, c->batch, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  void* s = a.stream();
+XKV_CACHE_PY_END(xkv_tree_commit(c, l0, l1, K, V, len, path, path_len, n, pos, first, flags, s))
+
+XKV_CACHE_PY(cache_weigh, 14)
+  const int n = a.i32();
+  const int64_t rows = a.heads() * c->cap, queries = a.tokens(n);
+  void* q = a.tensor("q", at::kBFloat16, queries * c->d_h);
+  const float* lse = (const float*)a.tensor("lse", at::kFloat, queries);
+  void* K = a.tensor("K", at::kBFloat16, rows * c->d_h);
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch, true);
+  const int32_t* visible = (const int32_t*)a.tensor("visible", at::kInt, (int64_t)c->batch * n, true);
+  const int32_t* seen = (const int32_t*)a.tensor("seen", at::kInt, c->batch, true);
+  const float decay = a.real();
+  float* weights = (float*)a.tensor("weights", at::kFloat, rows);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  void* s = a.stream();
+XKV_CACHE_PY_END(xkv_cache_weigh(c, l0, l1, q, n, lse, K, len, visible, seen, decay, weights, flags, s))
+
+XKV_CACHE_PY(evict_select, 11)
+  const int64_t rows = a.heads() * c->cap;
+  const float* weights = (const float*)a.tensor("weights", at::kFloat, rows);
+  const int32_t* pos = (const int32_t*)a.tensor("pos", at::kInt, rows, true);
+  const int32_t* since = (const int32_t*)a.tensor("since", at::kInt, c->batch, true);
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch, true);
+  const int keep = a.i32();
+  int32_t* src = (int32_t*)a.tensor("src", at::kInt, a.heads() * keep);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  void* s = a.stream();
+XKV_CACHE_PY_END(xkv_evict_select(c, l0, l1, weights, pos, since, len, keep, src, flags, s))
+
+XKV_CACHE_PY(evict_compact, 10)
+  const int64_t rows = a.heads() * c->cap;
+  void* K = a.tensor("K", at::kBFloat16, rows * c->d_h);
+  void* V = a.tensor("V", at::kBFloat16, rows * c->d_h);
+  const int keep = a.i32();
+  const int32_t* src = (const int32_t*)a.tensor("src", at::kInt, a.heads() * keep);
+  float* weights = (float*)a.tensor("weights", at::kFloat, rows, true);
+  int32_t* pos = (int32_t*)a.tensor("pos", at::kInt, rows, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  void* s = a.stream();
+XKV_CACHE_PY_END(xkv_evict_compact(c, l0, l1, K, V, src, keep, weights, pos, flags, s))
+
 // torch_hooks(get_device, get_current_raw_stream): how "the current stream" is found.
 PyObject* torch_hooks(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (nargs != 2) { PyErr_SetString(PyExc_TypeError, "expected 2 arguments"); return nullptr; }
@@ -252,7 +398,8 @@ PyObject* torch_hooks(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 #define XKV_DEF(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {XKV_DEF(sr_select), XKV_DEF(sr_select_static), XKV_DEF(sr_reconstruct_attend),
                          XKV_DEF(sr_reconstruct_attend_tail), XKV_DEF(dense_attend), XKV_DEF(quantize_rtn),
-                         XKV_DEF(dequantize_rtn), XKV_DEF(torch_hooks), {nullptr, nullptr, 0, nullptr}};
+                         XKV_DEF(dequantize_rtn), XKV_DEF(tree_attend), XKV_DEF(tree_commit), XKV_DEF(cache_weigh),
+                         XKV_DEF(evict_select), XKV_DEF(evict_compact), XKV_DEF(torch_hooks), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_xkv", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

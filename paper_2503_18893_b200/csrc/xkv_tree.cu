@@ -1,0 +1,634 @@
+// Attention of drafted tokens over an uncompressed cache (xkv_tree_attend).
+//
+// A sequence has `len` committed rows, which every drafted token attends to, and behind them its drafts' own rows, which
+// token i attends to where bit j of its mask is set.  For one (layer, sequence, KV head) the queries of all tokens and of the
+// head's n_rep query heads are the rows of one matrix Q, row token * n_rep + head, and
+//   S = scale Q K^T,   p = exp2(S log2(e) - m),   O += p V,   l += sum p
+// runs over 128-row tiles of the cache with a running maximum m.  The cache is read once for up to 256 rows of Q: 256 rows
+// are 256 multiplications for every byte read, where B200's HBM and its tensor cores take about as long.
+//
+//   producer  TMA: K and V tiles through one ring of shared-memory slots, across the borders of problems
+//   issuer    tcgen05.mma: S (both operands in shared memory), then O += P V with P in tensor memory, where it lies over S
+//   softmax   a warpgroup for each 128 rows of Q: thread = row = TMEM lane, so a row's maximum and sum need no shuffle.
+//             O stays in tensor memory; it is rescaled only when a row's maximum has grown by more than 2^8 (a weight is then
+//             at most 2^8, which fp32 sums and bf16's relative precision do not notice).
+// Weights are rounded to bf16 for the tensor core (relative 2^-9, as the output's own rounding); the denominator sums them
+// unrounded in fp32.
+//
+// The tiles of all problems form one list that is cut into as many even pieces as there are CTAs, whatever the lengths of the
+// sequences: a CTA that holds a whole problem writes its output, the others leave (O, m, l) for tree_merge_kernel.  Lengths are
+// read on the device only, so a captured call serves sequences as they grow.
+//
+// Rows that a token does not attend to have no influence on it whatever they hold: logits are selected, not added to, and a
+// weight of zero meets only finite values, since value rows behind the last draft are zeroed in shared memory and elements of
+// the drafts' value rows that are not finite are taken out there and given to the rows that do attend to them at the end.
+#include <cuda.h>
+#include <math.h>
+
+#include "xkv_cache.cuh"
+
+namespace xkv {
+
+namespace {
+
+constexpr int kQRows = 128;                    // query rows per warpgroup
+constexpr float kGrow = 8.0f;                  // log2 of the growth of a maximum that makes O be rescaled
+constexpr int kMergeWarps = 8;
+
+struct TreeArgs {
+  int batch, H_kv, H_q, n_rep, cap, n_draft, words, l0, layers, min_tiles;
+  float scale2;                                // softmax scale times log2(e)
+  const __nv_bfloat16* q;
+  const uint32_t* mask;                        // nullptr: token i attends to drafts 0 .. i
+  const int32_t* draft_len;
+  const __nv_bfloat16* V;                      // (the rows of drafts that are not finite)
+  const int32_t* len;
+  float* part;                                 // [CTA][2][rows of a CTA][d_h]
+  float2* part_ml;                             // [CTA][2][rows of a CTA] (m, l)
+  __nv_bfloat16* out;
+  float* lse;
+  unsigned int* flags;
+};
+
+// Rows and drafts of a sequence, brought into range; *bad reports what was not.
+__device__ __forceinline__ void tree_lengths(const TreeArgs& a, int b, int* len, int* drafts, bool* bad) {
+  const int want_dl = a.draft_len ? a.draft_len[b] : a.n_draft, dl = min(max(want_dl, 0), a.n_draft);
+  const int want_ln = a.len ? a.len[b] : a.cap - a.n_draft, ln = min(max(want_ln, 0), a.cap - dl);
+  *len = ln;
+  *drafts = dl;
+  *bad = want_dl != dl || want_ln != ln;
+}
+
+// A place in the list of tiles: problem (l, b, g, block of query rows), tile t of nt.  Order: layer, sequence, head, block, tile.
+struct Place {
+  int l, b, g, qp, t, nt, n_qp, len, drafts;
+};
+
+template <int QT>
+__device__ __forceinline__ void load_sequence(const TreeArgs& a, Place& p) {
+  bool bad;
+  tree_lengths(a, p.b, &p.len, &p.drafts, &bad);
+  p.nt = p.drafts > 0 ? (p.len + p.drafts + kTile - 1) / kTile : 0;
+  p.n_qp = (p.drafts * a.n_rep + QT * kQRows - 1) / (QT * kQRows);
+}
+
+// Moves to the next problem that has tiles (there is one: the caller counts).
+template <int QT>
+__device__ __forceinline__ void next_problem(const TreeArgs& a, Place& p) {
+  p.t = 0;
+  if (++p.qp < p.n_qp) return;
+  p.qp = 0;
+  if (++p.g < a.H_kv) return;
+  p.g = 0;
+  do {
+    if (++p.b == a.batch) { p.b = 0; ++p.l; }
+    load_sequence<QT>(a, p);
+  } while (p.nt == 0 && p.l < a.layers);
+}
+
+// Tiles of one head, all blocks of query rows, in sequences [0, n_seq) -- by a whole warp.
+template <int QT>
+__device__ __forceinline__ int head_tiles(const TreeArgs& a, int n_seq, bool report) {
+  const int lane = threadIdx.x & 31;
+  int sum = 0;
+  for (int b = lane; b < n_seq; b += 32) {
+    Place p;
+    p.b = b;
+    load_sequence<QT>(a, p);
+    sum += p.nt * p.n_qp;
+    if (report && a.flags) {
+      int x, y;
+      bool bad;
+      tree_lengths(a, b, &x, &y, &bad);
+      if (bad) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+    }
+  }
+  return __reduce_add_sync(0xffffffffu, sum);
+}
+
+// CTAs that share `total` tiles.
+__device__ __forceinline__ int tree_ctas(const TreeArgs& a, int total, int grid) {
+  return max(1, min(grid, total / a.min_tiles));
+}
+
+// The place of tile u of the list -- by a whole warp.  per_layer: tiles of a layer.
+template <int QT>
+__device__ __forceinline__ Place find_place(const TreeArgs& a, int u, int per_layer) {
+  const int lane = threadIdx.x & 31;
+  Place p;
+  p.l = u / per_layer;
+  int rest = u - p.l * per_layer;
+  for (int b0 = 0;; b0 += 32) {                // (u is in the list: the search ends inside the batch)
+    Place s;
+    s.b = min(b0 + lane, a.batch - 1);
+    load_sequence<QT>(a, s);
+    const int mine = b0 + lane < a.batch ? s.nt * s.n_qp * a.H_kv : 0;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    const unsigned holds = __ballot_sync(0xffffffffu, rest < upto);
+    if (holds || b0 + 32 >= a.batch) {
+      const int at = holds ? __ffs(holds) - 1 : 0;
+      rest -= __shfl_sync(0xffffffffu, upto - mine, at);
+      p.b = b0 + at;
+      break;
+    }
+    rest -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  load_sequence<QT>(a, p);
+  const int per_head = p.nt * p.n_qp;
+  p.g = rest / per_head;
+  rest -= p.g * per_head;
+  p.qp = rest / p.nt;
+  p.t = rest - p.qp * p.nt;
+  return p;
+}
+
+// What rows base .. base + 31 of the cache are to a token: bit = it attends to the row.
+__device__ __forceinline__ uint32_t row_bits(const TreeArgs& a, const uint32_t* mask_row, int token, int base, int len, int drafts) {
+  const int d0 = base - len;                   // draft index of bit 0
+  if (d0 >= drafts) return 0u;
+  if (d0 <= -32) return 0xffffffffu;
+  uint32_t w;
+  if (!mask_row) {                             // a chain: drafts up to the token itself
+    const int n = token + 1 - d0;              // bits from 0 that are set
+    w = n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+  } else if (d0 < 0) {
+    w = (mask_row[0] << -d0) | ((1u << -d0) - 1u);
+  } else {
+    const int i = d0 >> 5, s = d0 & 31;
+    w = mask_row[i] >> s;
+    if (s && i + 1 < a.words) w |= mask_row[i + 1] << (32 - s);
+  }
+  const int n = drafts - d0;                   // bits behind the last draft are nobody's
+  return n >= 32 ? w : w & ((1u << n) - 1u);
+}
+
+template <int DH, int QT>
+struct TreeSmem {
+  static constexpr int kSlab = kTile * 128;                    // 128 rows x 64 columns, 128-byte swizzle
+  static constexpr int kSlot = kSlab * (DH / 64);
+  static constexpr int kSlots = DH == 128 ? (QT == 2 ? 5 : 6) : 8;
+  static constexpr int kBytes = 1024 + QT * kSlot + kSlots * kSlot;
+};
+
+template <int DH, int QT>
+__global__ void __launch_bounds__(QT * 128 + 64, 1)
+tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const TreeArgs a) {
+  using namespace ptx;
+  using L = TreeSmem<DH, QT>;
+  constexpr int NS = L::kSlots;
+  constexpr uint32_t kSlab16 = L::kSlab >> 4;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bars_s[2 * NS + 9];
+  __shared__ uint32_t tmem_s;
+  __shared__ int abort_s;
+  __shared__ Place place_s;
+  __shared__ int range_s[2];
+  __shared__ uint32_t bad_s[2][8];             // drafts with elements that are not finite, of this segment and the next
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t ring = base + QT * L::kSlot;
+  const uint32_t bars = smem_u32(bars_s);
+  const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_s = bars + 16 * NS, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16,
+                 b_drain = b_q + 16;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int kProducer = QT * 4, kIssuer = QT * 4 + 1;
+
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(b_s + 8 * i, 1);
+      mbar_init(b_p + 8 * i, 128);
+      mbar_init(b_o + 8 * i, 1);
+      mbar_init(b_q + 8 * i, 128);
+    }
+    mbar_init(b_drain, 1);
+    fence_mbar_init();
+    abort_s = 0;
+  }
+  if (tid < 16) bad_s[tid >> 3][tid & 7] = 0u;
+  if (warp == kIssuer) {
+    tmem_alloc(smem_u32(&tmem_s), 512);
+    tmem_relinquish();
+  }
+  grid_dependency_wait();                      // everything below may come from the kernel before
+  grid_dependency_launch();
+  if (warp == kProducer) {
+    const int per_layer = head_tiles<QT>(a, a.batch, blockIdx.x == 0) * a.H_kv, total = per_layer * a.layers;
+    int u0 = 0, u1 = 0;
+    if (total > 0) {
+      const int ctas = tree_ctas(a, total, gridDim.x), c = blockIdx.x;
+      if (c < ctas) { u0 = piece_begin(total, ctas, c); u1 = piece_begin(total, ctas, c + 1); }
+    }
+    if (u1 > u0) {
+      const Place p = find_place<QT>(a, u0, per_layer);
+      if (lane == 0) place_s = p;
+    }
+    if (lane == 0) { range_s[0] = u0; range_s[1] = u1; }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_s;
+  const Wait wt{&abort_s, a.flags};
+  int left = range_s[1] - range_s[0];
+  Place p = place_s;
+  uint32_t n_loaded = 0;                       // producer: tiles (K and V each) asked for
+
+  if (left > 0 && warp == kProducer) {
+    if (lane == 0) {                           // (the others of the warp wait at its end)
+      bool ok = true;
+      while (left > 0 && ok) {
+        const int t1 = min(p.nt, p.t + left);
+        const int row0 = (((a.l0 + p.l) * a.batch + p.b) * a.H_kv + p.g) * a.cap;
+        left -= t1 - p.t;
+        for (int t = p.t; t < t1 && ok; ++t) {
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t slot = n_loaded % NS;
+            if (!wait_bar(wt, b_empty + 8 * slot, ((n_loaded / NS) & 1u) ^ 1u)) { ok = false; break; }
+            mbar_expect_tx(b_full + 8 * slot, L::kSlot);
+#pragma unroll
+            for (int x = 0; x < DH / 64; ++x)
+              tma_load_2d(ring + slot * L::kSlot + x * L::kSlab, kv ? &v_map : &k_map, x * 64, row0 + t * kTile, b_full + 8 * slot);
+            ++n_loaded;
+          }
+        }
+        if (left > 0) next_problem<QT>(a, p);
+      }
+    }
+    __syncwarp();
+  } else if (left > 0 && warp == kIssuer) {
+    const uint64_t hi = smem_desc_sw128(0, 0) & 0xFFFFFFFF00000000ull;
+    constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTile);
+    constexpr uint32_t idesc_o = idesc_bf16_f32(128, DH) | (1u << 16);         // V is read along its rows (MN-major)
+    const uint32_t q_lo = (uint32_t)smem_desc_sw128(base, 0);
+    const uint32_t k_lo = (uint32_t)smem_desc_sw128(ring, 0);
+    const uint32_t v_lo = ((uint32_t)smem_desc_sw128(ring, 0) & 0xFFFFu) | (kSlab16 << 16);
+    uint32_t n = 0, it = 0, seg = 0;           // ring position of the next K tile; tiles done; segments done
+    bool ok = true;
+    // S of the tile at ring position n into its buffer
+    auto logits = [&](int qt, uint32_t it_of, uint32_t n_of) {
+      const uint32_t buf = QT == 2 ? (uint32_t)qt : (it_of & 1u);
+      const uint32_t ka = k_lo + (n_of % NS) * (uint32_t)(L::kSlot >> 4), qa = q_lo + (uint32_t)qt * (L::kSlot >> 4);
+#pragma unroll
+      for (int k = 0; k < DH / 16; ++k) {
+        const uint32_t off = (uint32_t)(k >> 2) * kSlab16 + (uint32_t)(k & 3) * 2u;
+        tc_mma_bf16(tmem + buf * 128u, hi | (qa + off), hi | (ka + off), idesc_s, k ? 1u : 0u);
+      }
+      tc_commit(b_s + 8 * buf);
+    };
+    while (left > 0 && ok) {
+      const int t1 = min(p.nt, p.t + left), cnt = t1 - p.t;
+      left -= cnt;
+      for (int qt = 0; qt < QT && ok; ++qt) ok = wait_warp(wt, b_q + 8 * qt, seg & 1u);
+      ok = ok && wait_warp(wt, b_full + 8 * (n % NS), (n / NS) & 1u);
+      if (!ok) break;
+      tc_fence_after();
+      if (elect_one()) {
+        for (int qt = 0; qt < QT; ++qt) logits(qt, it, n);
+        tc_commit(b_empty + 8 * (n % NS));
+      }
+      for (int t = 0; t < cnt; ++t, ++it, n += 2) {
+        const bool more = t + 1 < cnt;
+        if (QT == 1 && more) {                 // the next tile's logits go into the other buffer while this one's are worked on
+          if (!(ok = wait_warp(wt, b_full + 8 * ((n + 2) % NS), ((n + 2) / NS) & 1u))) break;
+          if (elect_one()) {
+            logits(0, it + 1, n + 2);
+            tc_commit(b_empty + 8 * ((n + 2) % NS));
+          }
+        }
+        if (!(ok = wait_warp(wt, b_full + 8 * ((n + 1) % NS), ((n + 1) / NS) & 1u))) break;
+        const uint32_t va = v_lo + ((n + 1) % NS) * (uint32_t)(L::kSlot >> 4);
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          const uint32_t buf = QT == 2 ? (uint32_t)qt : (it & 1u);
+          if (!(ok = wait_warp(wt, b_p + 8 * buf, QT == 2 ? (it & 1u) : ((it >> 1) & 1u)))) break;
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < kTile / 16; ++k)
+              tc_mma_bf16_ts(tmem + 256u + (uint32_t)qt * 128u, tmem + buf * 128u + 64u + (uint32_t)k * 8u,
+                             hi | (va + (uint32_t)k * (2048u >> 4)), idesc_o, (t | k) ? 1u : 0u);
+            tc_commit(b_o + 8 * qt);
+            if (qt == QT - 1) tc_commit(b_empty + 8 * ((n + 1) % NS));
+          }
+          if (QT == 2 && more) {               // S lies where P did: behind the product that reads P
+            if (qt == 0 && !(ok = wait_warp(wt, b_full + 8 * ((n + 2) % NS), ((n + 2) / NS) & 1u))) break;
+            if (elect_one()) {
+              logits(qt, it + 1, n + 2);
+              if (qt == QT - 1) tc_commit(b_empty + 8 * ((n + 2) % NS));
+            }
+          }
+        }
+        if (!ok) break;
+      }
+      ++seg;
+      if (left > 0 && ok) next_problem<QT>(a, p);
+    }
+  } else if (left > 0) {
+    const int qt = warp >> 2, row = tid & 127;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    uint8_t* q_gen = gen + qt * L::kSlot;
+    const uint32_t o_addr = tmem + lane_base + 256u + (uint32_t)qt * 128u;
+    uint32_t it = 0, seg = 0;
+    bool ok = true;
+    while (left > 0 && ok) {
+      const int t0 = p.t, t1 = min(p.nt, p.t + left);
+      left -= t1 - t0;
+      const int rows_q = p.drafts * a.n_rep;                   // rows of Q of this sequence
+      const int m0 = (p.qp * QT + qt) * kQRows;                // this warpgroup's first
+      // ---- Q as the A operand: 64-column slabs, 128-byte rows, 16-byte units swizzled by the row; rows behind the last are 0
+      for (int i = row; i < kQRows * (DH / 8); i += 128) {
+        const int r = i / (DH / 8), c = i % (DH / 8), m = m0 + r;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (m < rows_q) {
+          const int token = m / a.n_rep, h = m - token * a.n_rep;
+          const size_t at = ((((size_t)(a.l0 + p.l) * a.batch + p.b) * a.n_draft + token) * a.H_q + (size_t)p.g * a.n_rep + h) * DH + c * 8;
+          v = *reinterpret_cast<const uint4*>(a.q + at);
+        }
+        *reinterpret_cast<uint4*>(q_gen + (c >> 3) * L::kSlab + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+      }
+      fence_proxy_async();
+      mbar_arrive(b_q + 8 * qt);
+      const int m = m0 + row;
+      const bool live = m < rows_q;
+      const bool warp_live = m0 + (row & ~31) < rows_q;
+      const int token = live ? m / a.n_rep : 0;
+      const uint32_t* mask_row = a.mask ? a.mask + ((size_t)p.b * a.n_draft + token) * a.words : nullptr;
+      float m_used = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+      bool odd = false;                        // tiles of this segment held drafts
+      for (int t = t0; t < t1; ++t, ++it) {
+        const uint32_t buf = QT == 2 ? (uint32_t)qt : (it & 1u);
+        if (!(ok = wait_warp(wt, b_s + 8 * buf, QT == 2 ? (it & 1u) : ((it >> 1) & 1u)))) break;
+        tc_fence_after();
+        // the next segment's list: whoever read it last (two segments ago) has handed over this segment's queries since
+        if (qt == 0 && t == t0 && row < 8) bad_s[(seg + 1) & 1u][row] = 0u;
+        const uint32_t s_addr = tmem + lane_base + buf * 128u;
+        const bool masked = (t + 1) * kTile > p.len;
+        if (warp_live) {
+          // the maximum needs all 128 logits, the weights need them again: half of them stay in registers, half are read twice
+          uint32_t bits[4];
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits[i] = row_bits(a, mask_row, token, t * kTile + 32 * i, p.len, p.drafts);
+          }
+          float z[2][32], mx[2] = {-INFINITY, -INFINITY};
+          auto load = [&](int half) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) tmem_ld32(s_addr + 64u * half + 32u * i, z[i]);
+            tc_wait_ld();
+            if (masked) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) z[i][e] = (bits[2 * half + i] >> e) & 1u ? z[i][e] : -INFINITY;
+            }
+          };
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            load(half);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) mx[i] = fmaxf(mx[i], z[i][e]);
+          }
+          const float m_new = fmaxf(m_used, fmaxf(mx[0], mx[1]) * a.scale2);
+          if (t == t0) {
+            m_used = m_new;
+          } else {
+            const bool grow = m_new > m_used + kGrow || (m_used == -INFINITY && m_new > -INFINITY);
+            if (__any_sync(0xffffffffu, grow)) {
+              // O holds the tiles before this one once their product is done
+              if (!(ok = wait_warp(wt, b_o + 8 * qt, (it - 1u) & 1u))) break;
+              tc_fence_after();
+              const float f = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
+              if (grow) m_used = m_new;
+              l0 *= f;
+              l1 *= f;
+#pragma unroll 1
+              for (int c = 0; c < DH; c += 32) {
+                float o[32];
+                uint32_t r[32];
+                tmem_ld32(o_addr + (uint32_t)c, o);
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(o[e] * f);
+                tmem_st32(o_addr + (uint32_t)c, r);
+              }
+            }
+          }
+          const float shift = m_used == -INFINITY ? 0.0f : m_used;
+          auto weights = [&](int half) {       // P, two to a column, in the upper half of S's columns
+            uint32_t r[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float p0 = ex2_approx(fmaf(z[e >> 4][2 * (e & 15)], a.scale2, -shift));
+              const float p1 = ex2_approx(fmaf(z[e >> 4][2 * (e & 15) + 1], a.scale2, -shift));
+              l0 += p0;
+              l1 += p1;
+              r[e] = pack_bf16(p0, p1);
+            }
+            tmem_st32(s_addr + 64u + 32u * half, r);
+          };
+          weights(1);
+          load(0);
+          weights(0);
+          tc_wait_st();
+        }
+        if (masked) {
+          odd = true;
+          if (qt == 0) {
+            // thread = value row: what no token holds is zeroed, what is not finite in a draft's row is taken out
+            const uint32_t nv = 2u * it + 1u, slot = nv % NS;
+            if (!(ok = wait_warp(wt, b_full + 8 * slot, (nv / NS) & 1u))) break;
+            const int draft = t * kTile + row - p.len;
+            if (draft >= 0) {
+              uint8_t* v = gen + QT * L::kSlot + slot * L::kSlot + row * 128;
+              bool hit = false;
+              for (int c = 0; c < DH / 8; ++c) {
+                uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * L::kSlab + (((c & 7) ^ (row & 7)) << 4));
+                uint4 x = draft < p.drafts ? *at : make_uint4(0u, 0u, 0u, 0u);
+                uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
+                  if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+                }
+                *at = x;
+              }
+              if (hit) atomicOr(&bad_s[seg & 1u][draft >> 5], 1u << (draft & 31));
+            }
+            fence_proxy_async();
+          }
+        }
+        tc_fence_before();
+        mbar_arrive(b_p + 8 * buf);
+      }
+      if (!ok) break;
+      // ---- the segment's result
+      if (!(ok = wait_warp(wt, b_o + 8 * qt, (it - 1u) & 1u))) break;
+      tc_fence_after();
+      const bool whole = t0 == 0 && t1 == p.nt;
+      const float l = l0 + l1;
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      const size_t qh = (((size_t)(a.l0 + p.l) * a.batch + p.b) * a.n_draft + token) * a.H_q + (size_t)p.g * a.n_rep + (m - token * a.n_rep);
+      const size_t pr = ((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * (QT * kQRows) + qt * kQRows + row;
+      if (warp_live) {
+#pragma unroll 1
+        for (int c = 0; c < DH; c += 32) {
+          float o[32];
+          tmem_ld32(o_addr + (uint32_t)c, o);
+          tc_wait_ld();
+          if (odd) {
+#pragma unroll 1
+            for (int w = 0; w < a.words; ++w) {
+              uint32_t bad = bad_s[seg & 1u][w];               // (entered before the product that this result waited for)
+              while (bad) {
+                const int j = 32 * w + __ffs(bad) - 1;
+                bad &= bad - 1u;
+                if (!(row_bits(a, mask_row, token, p.len + 32 * w, p.len, p.drafts) >> (j & 31) & 1u)) continue;
+                const __nv_bfloat16* v = a.V + ((((size_t)(a.l0 + p.l) * a.batch + p.b) * a.H_kv + p.g) * (size_t)a.cap + p.len + j) * DH + c;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  const float x = __bfloat162float(v[e]);
+                  if (!isfinite(x)) o[e] += x;
+                }
+              }
+            }
+          }
+          if (live && whole) {
+            uint4* dst = reinterpret_cast<uint4*>(a.out + qh * DH + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              dst[e] = make_uint4(pack_bf16(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                  pack_bf16(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+          } else if (live) {
+            float4* dst = reinterpret_cast<float4*>(a.part + pr * DH + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+        }
+        if (live && whole && a.lse) a.lse[qh] = l == 0.0f ? -INFINITY : (m_used + log2f(l)) * 0.6931471805599453f;
+        if (live && !whole) a.part_ml[pr] = make_float2(m_used, l);
+      }
+      tc_fence_before();
+      ++seg;
+      if (left > 0) next_problem<QT>(a, p);
+    }
+  }
+
+  // wind down: nothing of this CTA may still touch shared or tensor memory
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kIssuer) {
+    tc_fence_after();
+    if (abort_s) {                             // given up: nothing may still write tensor memory when it is freed
+      if (elect_one()) tc_commit(b_drain);
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(b_drain, 0))) break;
+    }
+    tmem_dealloc(tmem, 512);
+  }
+  if (abort_s && warp == kProducer && lane == 0) {
+    // given up: tiles may still be on their way into this CTA's shared memory; stay (with a limit) for them
+    for (uint32_t n = n_loaded > NS ? n_loaded - NS : 0u; n < n_loaded; ++n)
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (mbar_try_wait(b_full + 8 * (n % NS), (n / NS) & 1u)) break;
+  }
+}
+
+// Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A warp per query row, lane = d_h / 32 columns.
+template <int DH, int QT>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+tree_merge_kernel(const TreeArgs a, int attend_grid) {
+  constexpr int V = DH / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int py = blockIdx.x, l = py / (a.batch * a.H_kv), b = (py / a.H_kv) % a.batch, g = py % a.H_kv;
+  ptx::grid_dependency_wait();                 // the pieces come from the kernel before
+  ptx::grid_dependency_launch();
+  const int m = blockIdx.y * kMergeWarps + warp;               // row of Q
+  Place p;
+  p.b = b;
+  load_sequence<QT>(a, p);
+  if (m >= p.drafts * a.n_rep) return;
+  const int head = head_tiles<QT>(a, a.batch, false), before = head_tiles<QT>(a, b, false);
+  const int total = head * a.H_kv * a.layers, ctas = tree_ctas(a, total, attend_grid);
+  const int qp = m / (QT * kQRows);
+  const int u0 = (l * head + before) * a.H_kv + (g * p.n_qp + qp) * p.nt, u1 = u0 + p.nt;
+  const int c0 = piece_of(total, ctas, u0), c1 = piece_of(total, ctas, u1 - 1);
+  if (c0 == c1) return;                        // one piece: written where it was computed
+  const int r = m - qp * QT * kQRows;
+  // a problem that begins inside a piece is that piece's last one
+  const int first_slot = piece_begin(total, ctas, c0) == u0 ? 0 : 1;
+  auto slot = [&](int c) { return ((size_t)c * 2 + (c == c0 ? first_slot : 0)) * (QT * kQRows) + r; };
+  float M = -INFINITY;
+  for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, a.part_ml[slot(c)].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  float acc[V], sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+  for (int c = c0; c <= c1; ++c) {
+    const float2 ml = a.part_ml[slot(c)];
+    const float f = ml.x == -INFINITY ? (ml.y == 0.0f ? 0.0f : 1.0f) : exp2f(ml.x - M);       // (a piece of NaNs stays one)
+    const float* src = a.part + slot(c) * DH + lane * V;
+    sum = fmaf(f, ml.y, sum);
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = fmaf(f, src[i], acc[i]);
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const int token = m / a.n_rep;
+  const size_t qh = (((size_t)(a.l0 + l) * a.batch + b) * a.n_draft + token) * a.H_q + (size_t)g * a.n_rep + (m - token * a.n_rep);
+  uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + qh * DH + lane * V);
+#pragma unroll
+  for (int i = 0; i < V; i += 2) dst[i / 2] = ptx::pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+  if (a.lse && lane == 0) a.lse[qh] = sum == 0.0f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
+}
+
+template <int DH, int QT>
+cudaError_t launch_tree_as(const CUtensorMap& k_map, const CUtensorMap& v_map, const TreeArgs& a, int grid, int device, cudaStream_t s) {
+  cudaError_t e = ensure_dyn_smem<tree_attend_kernel<DH, QT>>(TreeSmem<DH, QT>::kBytes, device);
+  if (e == cudaSuccess) e = launch_pdl(tree_attend_kernel<DH, QT>, dim3(grid), dim3(QT * 128 + 64), TreeSmem<DH, QT>::kBytes, s, k_map, v_map, a);
+  if (e != cudaSuccess) return e;
+  const int rows = a.n_draft * a.n_rep;
+  e = launch_pdl(tree_merge_kernel<DH, QT>, dim3(a.layers * a.batch * a.H_kv, (rows + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, s,
+                 a, grid);
+  count_launch(kFamTree, 2);
+  return e;
+}
+
+}  // namespace
+
+// Floats of workspace: a piece leaves at most two results (its first and its last problem) of a CTA's query rows.
+size_t tree_part_floats(const xkv_cache_config* c, int n_draft) {
+  const int rows = n_draft * (c->H_q / c->H_kv) > kQRows ? 2 * kQRows : kQRows;
+  return (size_t)kPlanSms * 2 * rows * (c->d_h + 2);
+}
+
+cudaError_t launch_tree_attend(const xkv_cache_config* c, int l0, int l1, const __nv_bfloat16* q, int n_draft, const uint32_t* mask,
+                               const int32_t* draft_len, const __nv_bfloat16* K, const __nv_bfloat16* V, const int32_t* len,
+                               float* workspace, __nv_bfloat16* out, float* lse, unsigned int* flags, int device, cudaStream_t s) {
+  CUtensorMap k_map, v_map;
+  const uint64_t rows = (uint64_t)c->G * c->batch * c->H_kv * c->cap;
+  if (!encode_bf16_map(&k_map, K, rows, c->d_h, c->d_h, kTile) || !encode_bf16_map(&v_map, V, rows, c->d_h, c->d_h, kTile))
+    return cudaErrorInvalidValue;
+  int sms = 0;
+  const cudaError_t e = device_sms(device, &sms);
+  if (e != cudaSuccess) return e;
+  TreeArgs a;
+  a.batch = c->batch; a.H_kv = c->H_kv; a.H_q = c->H_q; a.n_rep = c->H_q / c->H_kv; a.cap = c->cap; a.n_draft = n_draft;
+  a.words = (n_draft + 31) / 32; a.l0 = l0; a.layers = l1 - l0; a.min_tiles = 1;
+  a.scale2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / sqrtf((float)c->d_h)) * kLog2e;
+  a.q = q; a.mask = mask; a.draft_len = draft_len; a.V = V; a.len = len; a.out = out; a.lse = lse; a.flags = flags;
+  const int rows_q = n_draft * a.n_rep, qt = rows_q > kQRows ? 2 : 1;
+  const int grid = sms < kPlanSms ? sms : kPlanSms;
+  a.part = workspace;
+  a.part_ml = reinterpret_cast<float2*>(workspace + (size_t)kPlanSms * 2 * qt * kQRows * c->d_h);
+  if (c->d_h == 128) return qt == 2 ? launch_tree_as<128, 2>(k_map, v_map, a, grid, device, s) : launch_tree_as<128, 1>(k_map, v_map, a, grid, device, s);
+  return qt == 2 ? launch_tree_as<64, 2>(k_map, v_map, a, grid, device, s) : launch_tree_as<64, 1>(k_map, v_map, a, grid, device, s);
+}
+
+}  // namespace xkv

@@ -126,7 +126,7 @@ _lib.xkv_debug_set_fault_injection.argtypes = [_P, ctypes.c_uint32]
 _lib.xkv_debug_set_fault_injection.restype = ctypes.c_int
 
 XKV_KERNEL_FAMILIES = ("scan", "topk", "fused", "merge", "tile", "tail_tc", "tail_cuda", "landmarks", "prep", "dense",
-                       "clf", "merge_multi")
+                       "clf", "merge_multi", "tree", "weigh", "evict")
 XKV_FLAG_CLF_BREAKDOWN = 4
 XKV_INJECT_SCAN_NO_LOAD = 1
 XKV_INJECT_FUSED_NO_B = 2
@@ -400,6 +400,92 @@ def xkv_dense_attend(grp: Group, layer_begin: int, layer_end: int, q, K, V, leng
                            stream)
     if st != XKV_OK:
         raise XKVError(st, "xkv_dense_attend")
+
+
+class xkv_cache_config(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("G", ctypes.c_int32), ("batch", ctypes.c_int32), ("H_kv", ctypes.c_int32),
+                ("H_q", ctypes.c_int32), ("d_h", ctypes.c_int32), ("cap", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+XKV_CACHE_MAX_ROWS = 1 << 22
+XKV_TREE_MAX_DRAFT = 256
+XKV_EVICT_MAX_ROWS = 1 << 18
+_CFG, _I, _F = ctypes.POINTER(xkv_cache_config), ctypes.c_int32, ctypes.c_float
+_lib.xkv_tree_workspace_bytes.argtypes = [_CFG, _I, ctypes.POINTER(ctypes.c_uint64)]
+_lib.xkv_tree_workspace_bytes.restype = ctypes.c_int
+_lib.xkv_tree_attend.argtypes = [_CFG, _I, _I, _P, _I, _P, _P, _P, _P, _P, _P, ctypes.c_uint64, _P, _P, _P, _P]
+_lib.xkv_tree_attend.restype = ctypes.c_int
+_lib.xkv_tree_commit.argtypes = [_CFG, _I, _I, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P]
+_lib.xkv_tree_commit.restype = ctypes.c_int
+_lib.xkv_cache_weigh.argtypes = [_CFG, _I, _I, _P, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P]
+_lib.xkv_cache_weigh.restype = ctypes.c_int
+_lib.xkv_evict_select.argtypes = [_CFG, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P]
+_lib.xkv_evict_select.restype = ctypes.c_int
+_lib.xkv_evict_compact.argtypes = [_CFG, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P]
+_lib.xkv_evict_compact.restype = ctypes.c_int
+
+
+def make_cache_config(*, G, batch, H_kv, H_q, d_h, cap, softmax_scale=0.0) -> xkv_cache_config:
+    """Sizes of an uncompressed cache K, V bf16 [G][batch][H_kv][cap][d_h] (include/xkv.h)."""
+    return xkv_cache_config(ctypes.sizeof(xkv_cache_config), G, batch, H_kv, H_q, d_h, cap, softmax_scale)
+
+
+# The calls below check their tensors (type, contiguity, number of elements, the current device) and raise ValueError or
+# TypeError for one that does not fit `cfg`, XKVError for sizes that the library refuses.  `flags`: None or an int32 device
+# tensor into which the kernels OR XKV_FLAG_* bits.
+
+
+def xkv_tree_workspace_bytes(cfg: xkv_cache_config, n_draft: int) -> int:
+    b = ctypes.c_uint64()
+    st = _lib.xkv_tree_workspace_bytes(ctypes.byref(cfg), n_draft, ctypes.byref(b))
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_tree_workspace_bytes")
+    return b.value
+
+
+def xkv_tree_attend(cfg: xkv_cache_config, layer_begin: int, layer_end: int, q, n_draft: int, mask, draft_len, K, V, length,
+                    workspace, out, lse=None, flags=None, stream=None) -> None:
+    """Attention of drafted tokens q [G][batch][n_draft][H_q][d_h] over the cache and, by `mask` (int32 words
+    [batch][n_draft][ceil(n_draft/32)], or None for a chain), over one another.  `workspace`: a uint8 device tensor of at least
+    xkv_tree_workspace_bytes(cfg, n_draft) bytes."""
+    st = _xkv.tree_attend(ctypes.addressof(cfg), layer_begin, layer_end, n_draft, q, mask, draft_len, K, V, length, workspace,
+                          out, lse, flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_tree_attend")
+
+
+def xkv_tree_commit(cfg: xkv_cache_config, layer_begin: int, layer_end: int, K, V, length, path, path_len, n_path: int,
+                    pos=None, first_pos=None, flags=None, stream=None) -> None:
+    """Rows length + j of the cache become the drafts path[b][j], j < path_len[b]; their positions first_pos[b] + j."""
+    st = _xkv.tree_commit(ctypes.addressof(cfg), layer_begin, layer_end, K, V, length, n_path, path, path_len, pos, first_pos,
+                          flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_tree_commit")
+
+
+def xkv_cache_weigh(cfg: xkv_cache_config, layer_begin: int, layer_end: int, q, n_tok: int, lse, K, length, visible, seen,
+                    decay: float, weights, flags=None, stream=None) -> None:
+    """Adds the attention weights of n_tok tokens to `weights` fp32 [G][batch][H_kv][cap]."""
+    st = _xkv.cache_weigh(ctypes.addressof(cfg), layer_begin, layer_end, n_tok, q, lse, K, length, visible, seen, decay,
+                          weights, flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_cache_weigh")
+
+
+def xkv_evict_select(cfg: xkv_cache_config, layer_begin: int, layer_end: int, weights, pos, since, length, keep: int, src,
+                     flags=None, stream=None) -> None:
+    """`src` int32 [G][batch][H_kv][keep]: the row whose content each of the first `keep` rows has to get."""
+    st = _xkv.evict_select(ctypes.addressof(cfg), layer_begin, layer_end, weights, pos, since, length, keep, src, flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_evict_select")
+
+
+def xkv_evict_compact(cfg: xkv_cache_config, layer_begin: int, layer_end: int, K, V, src, keep: int, weights=None, pos=None,
+                      flags=None, stream=None) -> None:
+    """Moves row src[j] to row j of K, V, weights and pos, in place."""
+    st = _xkv.evict_compact(ctypes.addressof(cfg), layer_begin, layer_end, K, V, keep, src, weights, pos, flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_evict_compact")
 
 
 def xkv_group_status(grp: Group, stream=None):
