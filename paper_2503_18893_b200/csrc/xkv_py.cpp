@@ -251,14 +251,23 @@ struct Checked : Args {
       PyErr_SetString(PyExc_ValueError, "no cache configuration");
       bad = true;
     }
-    if (bad) return false;
-    PyObject* dev = PyObject_CallNoArgs(g_get_device);
-    if (dev) {
-      device = PyLong_AsLong(dev);
-      Py_DECREF(dev);
-    }
-    bad = !dev || (device == -1 && PyErr_Occurred());
     return !bad;
+  }
+  // The current device, asked for once (there may be none: a call without a CUDA tensor never gets here).
+  bool on_device(const at::Tensor& t) {
+    if (!t.is_cuda()) return false;
+    if (device < 0) {
+      PyObject* dev = PyObject_CallNoArgs(g_get_device);
+      if (dev) {
+        device = PyLong_AsLong(dev);
+        Py_DECREF(dev);
+      }
+      if (device < 0) {
+        PyErr_Clear();
+        return false;
+      }
+    }
+    return t.get_device() == device;
   }
   int64_t heads() const { return (int64_t)cfg->G * cfg->batch * cfg->H_kv; }
   int64_t tokens(int64_t n) const { return (int64_t)cfg->G * cfg->batch * n * cfg->H_q; }
@@ -275,7 +284,7 @@ struct Checked : Args {
     const at::Tensor& t = THPVariable_Unpack(o);
     const char* what = nullptr;
     if (t.scalar_type() != type && !(type == at::kInt && t.scalar_type() == at::kUInt32)) what = "has another type";
-    else if (!t.is_cuda() || t.get_device() != device) what = "is not on the current CUDA device";
+    else if (!on_device(t)) what = "is not on the current CUDA device";
     else if (!t.is_contiguous()) what = "is not contiguous";
     else if (at_least ? t.numel() < numel : t.numel() != numel) what = "has another number of elements";
     if (what) {
@@ -373,7 +382,7 @@ XKV_CACHE_PY(evict_select, 11)
   void* s = a.stream();
 XKV_CACHE_PY_END(xkv_evict_select(c, l0, l1, weights, pos, since, len, keep, src, flags, s))
 
-XKV_CACHE_PY(evict_compact, 10)
+XKV_CACHE_PY(evict_compact, 11)
   const int64_t rows = a.heads() * c->cap;
   void* K = a.tensor("K", at::kBFloat16, rows * c->d_h);
   void* V = a.tensor("V", at::kBFloat16, rows * c->d_h);
