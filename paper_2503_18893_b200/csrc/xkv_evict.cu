@@ -124,171 +124,298 @@ evict_compact_kernel(int cap, size_t head0, __nv_bfloat16* K, __nv_bfloat16* V, 
 }
 
 // ---------------------------------------------------------------------------------------------
-// Selection.  A cluster of CTAs per head, each with an even slice of the rows in shared memory as 32-bit keys that order
-// like the weights.  The recent rows are counted first: either they fill `keep` and are the only candidates, or they all stay
-// and the others compete for the rest.  The key of the last row that stays is found digit by digit (11, 11, 10 bits) from
-// histograms summed over the cluster; rows with that very key stay in row order as far as there is room.  Ranks of holes and of
-// the rows that fill them are prefix sums in row order, so the map does not depend on timing.
+// Selection.  A cluster of CTAs per head; every thread holds the weights of ITEMS rows, 1024 apart, in registers as 32-bit keys
+// that order like the weights.  The recent rows are counted with the first digit: either they fill `keep` and are the only
+// candidates, or they all stay and the others compete for the rest.  The key of the last row that stays is found digit by
+// digit (11, 11, 10 bits) from histograms in shared memory, which a warp of every CTA adds up over the cluster: first 64 sums
+// of 32 bins, then the bins of one of them, so that little crosses between SMs.  Rows with that very key stay in row order as
+// far as there is room.  Ranks in row order -- of ties, of holes, of the rows that fill them -- are ballots and a prefix sum
+// over (round, warp), so the map does not depend on timing.
 constexpr int kSelThreads = 1024;
 constexpr int kSelBins = 2048;
 constexpr int kSelMaxCluster = 8;
 constexpr uint32_t kOut = 0u, kStays = 0xffffffffu;      // no weight maps to these (they would be NaNs)
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  if (w != w) w = -INFINITY;
-  if (w == 0.0f) w = 0.0f;                               // -0 orders like 0
-  const uint32_t u = __float_as_uint(w);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(fmaxf(w + 0.0f, -INFINITY));              // -0 becomes 0, NaN the lowest weight
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 struct SelShared {
-  uint32_t hist[kSelBins];
+  uint32_t hist[4][kSelBins];                            // first digit of other rows, of recent rows; second; third
+  uint32_t coarse[4][64];                                // sums of 32 bins
+  uint32_t table[kSelThreads];                           // per (round, warp): counts, then their exclusive prefix
   uint32_t warp[32];
-  uint32_t count[4];                                     // what the cluster adds up: recent rows, ties, holes, movers
-  uint32_t pick[2];                                      // digit, what is still needed inside it
+  uint32_t count;                                        // holes | movers << 16 of this CTA
+  uint32_t digit, need, recent_only, ties_before, all_ties, holes_before, movers_upto[kSelMaxCluster];
 };
 
-// Sum over the CTA, for every thread.
-__device__ __forceinline__ uint32_t block_sum(SelShared& s, uint32_t v) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  v = __reduce_add_sync(0xffffffffu, v);
+// table[] becomes its exclusive prefix; returns the sum.
+__device__ __forceinline__ uint32_t scan_table(SelShared& s) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   __syncthreads();
-  if (lane == 0) s.warp[warp] = v;
-  __syncthreads();
-  return __reduce_add_sync(0xffffffffu, s.warp[lane]);
-}
-// Exclusive prefix over the CTA's threads; *all: the sum.
-__device__ __forceinline__ uint32_t block_prefix(SelShared& s, uint32_t v, uint32_t* all) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t v = s.table[tid];
   uint32_t upto = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
-  __syncthreads();
   if (lane == 31) s.warp[warp] = upto;
   __syncthreads();
   const uint32_t w = s.warp[lane];
-  const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u);
-  *all = __reduce_add_sync(0xffffffffu, w);
-  return before + upto - v;
+  s.table[tid] = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u) + upto - v;
+  __syncthreads();
+  return __reduce_add_sync(0xffffffffu, w);
 }
 
-__global__ void __launch_bounds__(kSelThreads)
-evict_select_kernel(int batch, int H_kv, int cap, int per_cta, int l0, const float* __restrict__ weights,
-                    const int32_t* __restrict__ pos, const int32_t* __restrict__ since, const int32_t* __restrict__ len, int keep,
-                    int32_t* src, unsigned int* flags) {
-  extern __shared__ uint32_t key_s[];                    // [per_cta] keys, then one bit per row: recent
-  __shared__ SelShared s;
+// By a whole warp: the bin from the top of histogram h, summed over the cluster, that holds the need-th entry (from 1), what is
+// needed inside it, and its entries.
+__device__ __forceinline__ void find_bin(cg::cluster_group& cl, SelShared& s, int h, int n_cta, uint32_t need, uint32_t* bin, uint32_t* rest,
+                                         uint32_t* entries) {
+  const int lane = threadIdx.x & 31;
+  auto locate = [&](uint32_t v, uint32_t* before) {      // lane whose running sum reaches `need`
+    uint32_t upto = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    const unsigned holds = __ballot_sync(0xffffffffu, upto >= need);
+    const int at = holds ? __ffs(holds) - 1 : 31;
+    *before = __shfl_sync(0xffffffffu, upto - v, at);
+    return at;
+  };
+  uint32_t hi = 0, lo = 0, before;
+#pragma unroll
+  for (int c = 0; c < kSelMaxCluster; ++c) {             // (unrolled: the reads of other SMs' memory are all in flight at once)
+    if (c < n_cta) {
+      const uint2 v = *reinterpret_cast<const uint2*>(&cl.map_shared_rank(&s, c)->coarse[h][62 - 2 * lane]);
+      hi += v.y;
+      lo += v.x;
+    }
+  }
+  const int at = locate(hi + lo, &before);
+  need -= before;
+  const uint32_t top = __shfl_sync(0xffffffffu, hi, at);
+  int group = 63 - 2 * at;
+  if (need > top) { need -= top; --group; }
+  uint32_t v = 0;
+#pragma unroll
+  for (int c = 0; c < kSelMaxCluster; ++c)
+    if (c < n_cta) v += cl.map_shared_rank(&s, c)->hist[h][group * 32 + 31 - lane];
+  const int b = locate(v, &before);
+  *bin = (uint32_t)(group * 32 + 31 - b);
+  *rest = need - before;
+  *entries = __shfl_sync(0xffffffffu, v, b);
+}
+
+template <int ITEMS>
+__global__ void __launch_bounds__(kSelThreads, 1)
+evict_select_kernel(int batch, int H_kv, int cap, int l0, const float* __restrict__ weights, const int32_t* __restrict__ pos,
+                    const int32_t* __restrict__ since, const int32_t* __restrict__ len, int keep, int32_t* __restrict__ src,
+                    unsigned int* flags) {
+  extern __shared__ int list_s[];                        // rows at or behind `keep` that stay, ascending
+  __shared__ __align__(16) SelShared s;
   cg::cluster_group cl = cg::this_cluster();
   const int n_cta = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  const int tid = threadIdx.x, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int py = blockIdx.x / n_cta, b = (py / H_kv) % batch;
   const size_t head = (size_t)l0 * batch * H_kv + py, rows0 = head * (size_t)cap;
-  uint32_t* bit_s = key_s + per_cta;
+  auto cluster_sync = [&] {
+    if (n_cta > 1) cl.sync(); else __syncthreads();
+  };
+  for (int i = tid; i < 4 * kSelBins; i += kSelThreads) s.hist[0][i] = 0u;
   ptx::grid_dependency_wait();
   ptx::grid_dependency_launch();
   const int want = len ? len[b] : cap, ln = min(max(want, 0), cap);
   if (want != ln && blockIdx.x % (n_cta * H_kv) == 0 && tid == 0) raise(flags, XKV_FLAG_INDEX_RANGE);
   int32_t* dst = src + head * (size_t)keep;
-  const int r0 = rank * per_cta;                         // this CTA's rows: r0 .. r0 + n - 1
-  const int n = max(0, min(ln - r0, per_cta)), n_up = (n + kSelThreads - 1) / kSelThreads * kSelThreads;
   if (ln <= keep) {
     for (int j = rank * kSelThreads + tid; j < keep; j += n_cta * kSelThreads) dst[j] = j < ln ? j : -1;
     return;                                              // (the whole cluster does: ln and keep are the same for all)
   }
-
-  // ---- keys and recent rows
-  const int since_b = since ? since[b] : INT32_MAX;
-  uint32_t recent = 0;
-  for (int i = tid; i < n_up; i += kSelThreads) {
-    bool rec = false;
-    if (i < n) {
-      const int row = r0 + i;
-      key_s[i] = weight_key(weights[rows0 + row]);
-      if (since) rec = (pos ? pos[rows0 + row] : row) >= since_b;
+  // rounds that this length needs (the head's rows are spread evenly over the cluster); this thread's rows: r0 + 1024 k, of
+  // which the first `held` exist, and the first `front` are before `keep`
+  const int items = (ln + n_cta * kSelThreads - 1) / (n_cta * kSelThreads);
+  const int r0 = rank * (kSelThreads * items) + tid;
+  auto rounds_below = [&](int end) { return min(max((end - r0 + kSelThreads - 1) / kSelThreads, 0), items); };
+  const int held = r0 < ln ? rounds_below(ln) : 0, front = r0 < keep ? rounds_below(keep) : 0;
+  // ---- keys, the recent rows, the first digit of both kinds
+  uint32_t key[ITEMS], recent = 0;
+  {
+    const float* wp = weights + rows0 + r0;
+    constexpr int U = ITEMS < 16 ? ITEMS : 16;           // rounds whose loads are in flight at once
+#pragma unroll
+    for (int k0 = 0; k0 < ITEMS; k0 += U) {
+      float w[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) w[k] = k0 + k < held ? __ldg(wp + (k0 + k) * kSelThreads) : 0.0f;
+#pragma unroll
+      for (int k = 0; k < U; ++k) key[k0 + k] = k0 + k < held ? weight_key(w[k]) : kOut;
     }
-    const uint32_t bits = __ballot_sync(0xffffffffu, rec);
-    if (lane == 0) bit_s[i >> 5] = bits;
-    recent += rec ? 1u : 0u;
+    if (since) {
+      const int since_b = since[b];
+      const int32_t* pp = pos ? pos + rows0 + r0 : nullptr;
+#pragma unroll
+      for (int k0 = 0; k0 < ITEMS; k0 += U) {
+        int at[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) at[k] = pp && k0 + k < held ? __ldg(pp + (k0 + k) * kSelThreads) : r0 + (k0 + k) * kSelThreads;
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+          if (k0 + k < held && at[k] >= since_b) recent |= 1u << (k0 + k);
+      }
+    }
   }
-  recent = block_sum(s, recent);
-  if (tid == 0) s.count[0] = recent;
-  cl.sync();
-  uint32_t all_recent = 0;
-  for (int c = 0; c < n_cta; ++c) all_recent += cl.map_shared_rank(&s, c)->count[0];
-  const bool only_recent = all_recent >= (uint32_t)keep;
-  uint32_t need = only_recent ? (uint32_t)keep : (uint32_t)keep - all_recent;  // at least one, at most the candidates
-  for (int i = tid; i < n; i += kSelThreads) {
-    const bool rec = (bit_s[i >> 5] >> (i & 31)) & 1u;
-    if (only_recent && !rec) key_s[i] = kOut;
-    if (!only_recent && rec) key_s[i] = kStays;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    if (k >= items) break;
+    if (k < held) atomicAdd(&s.hist[0][((recent >> k) & 1u) * kSelBins + (key[k] >> 21)], 1u);
   }
-  // ---- the key of the last row that stays
-  uint32_t prefix = 0, known = 0;                        // digits found, as bits and as a mask
-#pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const uint32_t digits = pass == 2 ? 1023u : 2047u;
-    for (int i = tid; i < kSelBins; i += kSelThreads) s.hist[i] = 0u;
+  auto sum_bins = [&](int h) {                           // a warp sums two groups of 32 bins
+    const uint32_t x = __reduce_add_sync(0xffffffffu, s.hist[h][warp * 64 + lane]);
+    const uint32_t y = __reduce_add_sync(0xffffffffu, s.hist[h][warp * 64 + 32 + lane]);
+    if (lane == 0) { s.coarse[h][2 * warp] = x; s.coarse[h][2 * warp + 1] = y; }
+  };
+  __syncthreads();
+  sum_bins(0);
+  sum_bins(1);
+  cluster_sync();
+  if (warp == 0) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int c = 0; c < kSelMaxCluster; ++c) {
+      if (c < n_cta) {
+        const uint32_t* g = cl.map_shared_rank(&s, c)->coarse[1];
+        n += g[lane] + g[lane + 32];
+      }
+    }
+    n = __reduce_add_sync(0xffffffffu, n);
+    const bool only = n >= (uint32_t)keep;
+    uint32_t bin, rest, entries;
+    find_bin(cl, s, only ? 1 : 0, n_cta, only ? (uint32_t)keep : (uint32_t)keep - n, &bin, &rest, &entries);   // (at least one is needed)
+    if (lane == 0) { s.digit = bin; s.need = rest; s.recent_only = only; }
+  }
+  __syncthreads();
+  uint32_t prefix = s.digit << 21;
+  if (since) {
+    const bool only = s.recent_only != 0;
+    const uint32_t set = only ? ~recent : recent, to = only ? kOut : kStays;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+      if ((set >> k) & 1u && k < held) key[k] = to;
+  }
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    if (k >= items) break;
+    if (key[k] - prefix < 1u << 21) atomicAdd(&s.hist[2][(key[k] >> 10) & 2047u], 1u);         // (kOut and kStays have other digits)
+  }
+  __syncthreads();
+  sum_bins(2);
+  cluster_sync();
+  if (warp == 0) {
+    uint32_t bin, rest, entries;
+    find_bin(cl, s, 2, n_cta, s.need, &bin, &rest, &entries);
+    if (lane == 0) { s.digit = bin; s.need = rest; }
+  }
+  __syncthreads();
+  prefix |= s.digit << 10;
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    if (k >= items) break;
+    if (key[k] - prefix < 1u << 10) atomicAdd(&s.hist[3][key[k] & 1023u], 1u);
+  }
+  __syncthreads();
+  sum_bins(3);
+  cluster_sync();
+  if (warp == 0) {
+    uint32_t bin, rest, entries;
+    find_bin(cl, s, 3, n_cta, s.need, &bin, &rest, &entries);
+    const uint32_t t = __reduce_add_sync(0xffffffffu, lane < rank ? cl.map_shared_rank(&s, lane)->hist[3][bin] : 0u);
+    if (lane == 0) { s.digit = bin; s.need = rest; s.ties_before = t; s.all_ties = entries == rest; }
+  }
+  s.table[tid] = 0u;
+  __syncthreads();
+  prefix |= s.digit;
+  // ---- who stays: all keys above the last one's, and its ties, in row order if there is not room for all of them
+  const uint32_t below = (1u << lane) - 1u;
+  uint32_t stays = 0;
+  if (s.all_ties) {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+      if (key[k] >= prefix) stays |= 1u << k;            // (kStays is above every key, kOut below)
+  } else {
+    const uint32_t need = s.need, ties_before = s.ties_before;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      if (k >= items) break;
+      const unsigned t = __ballot_sync(0xffffffffu, key[k] == prefix);
+      if (lane == 0) s.table[k * 32 + warp] = __popc(t);
+    }
+    scan_table(s);
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      if (k >= items) break;
+      const bool tie = key[k] == prefix;
+      const unsigned t = __ballot_sync(0xffffffffu, tie);
+      const uint32_t nth = ties_before + s.table[k * 32 + warp] + __popc(t & below);
+      if (key[k] > prefix || (tie && nth < need)) stays |= 1u << k;
+    }
     __syncthreads();
-    for (int i = tid; i < n; i += kSelThreads) {
-      const uint32_t k = key_s[i];
-      if (k != kOut && k != kStays && (k & known) == prefix) atomicAdd(&s.hist[(k >> shift) & digits], 1u);
+    if (tid >= items * 32) s.table[tid] = 0u;            // (the scan left its sum there)
+  }
+  // ---- holes and movers in row order: a row before `keep` that does not stay, a row behind that does.  (From here on bits of
+  // rounds, not keys: the loops need not be unrolled.)
+  const uint32_t fronts = front == 32 ? 0xffffffffu : (1u << front) - 1u;
+  const uint32_t hole = fronts & ~stays, mover = stays & ~fronts;
+#pragma unroll 4
+  for (int k = 0; k < items; ++k) {
+    const unsigned ho = __ballot_sync(0xffffffffu, (hole >> k) & 1u), mo = __ballot_sync(0xffffffffu, (mover >> k) & 1u);
+    if (lane == 0) s.table[k * 32 + warp] = __popc(ho) | __popc(mo) << 16;     // (at most 32768 of each in a CTA)
+  }
+  const uint32_t sums = scan_table(s);
+  if (tid == 0) s.count = sums;
+  const int k_back = __reduce_min_sync(0xffffffffu, front), k_front = __reduce_max_sync(0xffffffffu, front);
+#pragma unroll 4
+  for (int k = k_back; k < items; ++k) {
+    const bool mv = (mover >> k) & 1u;
+    const unsigned mo = __ballot_sync(0xffffffffu, mv);
+    if (mv) list_s[(s.table[k * 32 + warp] >> 16) + __popc(mo & below)] = r0 + k * kSelThreads;
+  }
+  cluster_sync();
+  if (warp == 0) {
+    const uint32_t c = lane < n_cta ? cl.map_shared_rank(&s, lane)->count : 0u;
+    const uint32_t holes = __reduce_add_sync(0xffffffffu, lane < rank ? c & 0xffffu : 0u);
+    uint32_t upto = c >> 16;
+#pragma unroll
+    for (int o = 1; o < kSelMaxCluster; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
     }
-    cl.sync();
-    // thread t: bins 2t and 2t + 1 of the cluster, from the top
-    const int hi = kSelBins - 1 - 2 * tid;
-    uint32_t a0 = 0, a1 = 0;
-    for (int c = 0; c < n_cta; ++c) {
-      const uint32_t* h = cl.map_shared_rank(&s, c)->hist;
-      a0 += h[hi];
-      a1 += h[hi - 1];
+    if (lane < kSelMaxCluster) s.movers_upto[lane] = upto;
+    if (lane == 0) s.holes_before = holes;
+  }
+  __syncthreads();
+  const uint32_t holes_before = s.holes_before;
+#pragma unroll 4
+  for (int k = 0; k < k_front; ++k) {
+    const int row = r0 + k * kSelThreads;
+    const bool ho = (hole >> k) & 1u;
+    const unsigned hs = __ballot_sync(0xffffffffu, ho);
+    int from = row;
+    if (ho) {                                            // the i-th hole takes the i-th mover, which some CTA has listed
+      const uint32_t i = holes_before + (s.table[k * 32 + warp] & 0xffffu) + __popc(hs & below);
+      uint32_t of = 0;
+      int c = 0;
+      for (int d = 0; d < n_cta - 1; ++d)
+        if (i >= s.movers_upto[d]) { c = d + 1; of = s.movers_upto[d]; }
+      from = cl.map_shared_rank(list_s, c)[i - of];
     }
-    uint32_t all;
-    const uint32_t before = block_prefix(s, a0 + a1, &all);
-    if (before < need && need <= before + a0) { s.pick[0] = (uint32_t)hi; s.pick[1] = need - before; }
-    else if (before + a0 < need && need <= before + a0 + a1) { s.pick[0] = (uint32_t)hi - 1u; s.pick[1] = need - before - a0; }
-    cl.sync();                                           // everyone has read the histograms
-    prefix |= s.pick[0] << shift;
-    known |= digits << shift;
-    need = s.pick[1];
+    if (k < front) dst[row] = from;
   }
-  // ---- ties in row order: a thread's rows are consecutive
-  const int each = (n + kSelThreads - 1) / kSelThreads, i0 = min(n, tid * each), i1 = min(n, i0 + each);
-  uint32_t ties = 0;
-  for (int i = i0; i < i1; ++i) ties += key_s[i] == prefix ? 1u : 0u;
-  uint32_t all_ties;
-  uint32_t tie = block_prefix(s, ties, &all_ties);
-  if (tid == 0) s.count[1] = all_ties;
-  cl.sync();
-  for (int c = 0; c < rank; ++c) tie += cl.map_shared_rank(&s, c)->count[1];
-  uint32_t holes = 0, movers = 0;
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t k = key_s[i];
-    const bool stays = k > prefix || (k == prefix && tie++ < need);            // (kStays is above every key, kOut below)
-    key_s[i] = stays ? kStays : kOut;
-    if (r0 + i < keep) holes += stays ? 0u : 1u;
-    else movers += stays ? 1u : 0u;
-  }
-  uint32_t all_holes, all_movers;
-  uint32_t hole = block_prefix(s, holes, &all_holes), mover = block_prefix(s, movers, &all_movers);
-  if (tid == 0) { s.count[2] = all_holes; s.count[3] = all_movers; }
-  cl.sync();
-  for (int c = 0; c < rank; ++c) {
-    hole += cl.map_shared_rank(&s, c)->count[2];
-    mover += cl.map_shared_rank(&s, c)->count[3];
-  }
-  // ---- the i-th mover goes through entry i of the map to the i-th hole (which is at or behind entry i)
-  for (int i = i0; i < i1; ++i)
-    if (r0 + i >= keep && key_s[i] == kStays) dst[mover++] = r0 + i;
-  __threadfence();
-  cl.sync();
-  for (int i = i0; i < i1; ++i)
-    if (r0 + i < keep && key_s[i] == kOut) key_s[i] = (uint32_t)__ldcg(dst + hole++);
-  cl.sync();
-  for (int i = tid; i < n && r0 + i < keep; i += kSelThreads) dst[r0 + i] = key_s[i] == kStays ? r0 + i : (int32_t)key_s[i];
+  cluster_sync();                                        // no CTA's lists go before they have been read
 }
 
 }  // namespace
@@ -315,14 +442,11 @@ cudaError_t launch_evict_compact(const xkv_cache_config* c, int l0, int l1, __nv
   return e;
 }
 
-cudaError_t launch_evict_select(const xkv_cache_config* c, int l0, int l1, const float* weights, const int32_t* pos,
-                                const int32_t* since, const int32_t* len, int keep, int32_t* src, unsigned int* flags, int device,
-                                cudaStream_t s) {
-  int n_cta = 1;
-  while (n_cta < kSelMaxCluster && c->cap > 4 * kSelThreads * n_cta) n_cta *= 2;
-  const int per_cta = ((c->cap + n_cta - 1) / n_cta + kSelThreads - 1) / kSelThreads * kSelThreads;
-  const size_t smem = (size_t)per_cta * 4 + (size_t)per_cta / 8;
-  cudaError_t e = ensure_dyn_smem<evict_select_kernel>(smem, device);
+template <int ITEMS>
+static cudaError_t launch_select_as(const xkv_cache_config* c, int l0, int l1, int n_cta, size_t smem, const float* weights, const int32_t* pos,
+                                    const int32_t* since, const int32_t* len, int keep, int32_t* src, unsigned int* flags, int device,
+                                    cudaStream_t s) {
+  cudaError_t e = ensure_dyn_smem<evict_select_kernel<ITEMS>>(smem, device);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((l1 - l0) * c->batch * c->H_kv * n_cta);
@@ -338,9 +462,31 @@ cudaError_t launch_evict_select(const xkv_cache_config* c, int l0, int l1, const
   at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 2;
-  e = cudaLaunchKernelEx(&cfg, evict_select_kernel, (int)c->batch, (int)c->H_kv, (int)c->cap, per_cta, l0, weights, pos, since, len, keep, src, flags);
+  e = cudaLaunchKernelEx(&cfg, evict_select_kernel<ITEMS>, (int)c->batch, (int)c->H_kv, (int)c->cap, l0, weights, pos, since, len, keep, src, flags);
   count_launch(kFamEvict);
   return e;
+}
+
+cudaError_t launch_evict_select(const xkv_cache_config* c, int l0, int l1, const float* weights, const int32_t* pos,
+                                const int32_t* since, const int32_t* len, int keep, int32_t* src, unsigned int* flags, int device,
+                                cudaStream_t s) {
+  // CTAs per head.  A CTA holds 1024 rows a round in its registers, up to 32 rounds, and is alone on its SM.  Measured: 6.5 us and
+  // 0.56 us a round for one CTA; 9 us and 0.8 us a round in a cluster, whose barriers cross SMs; 148 CTAs, 74 pairs, 32 clusters
+  // of four and 14 of eight run at once.  32 heads of 65500 rows: 35 us in pairs, 23 in fours, 48 in eights; 128 of them: 77, 96, 152;
+  // 32 of 4200 rows: 9.0 us alone, 10.6 in pairs.
+  const int heads = (l1 - l0) * c->batch * c->H_kv;
+  int n_cta = 0, rounds = 0;
+  float least = 0.0f;
+  for (int n = 1, at_once = 148; n <= kSelMaxCluster; n *= 2) {
+    const int r = (c->cap + n * kSelThreads - 1) / (n * kSelThreads);
+    const float cost = (float)((heads + at_once - 1) / at_once) * (n == 1 ? 6.5f + 0.56f * r : 9.0f + 0.8f * r);
+    if (r <= 32 && (n_cta == 0 || cost < least)) { n_cta = n; rounds = r; least = cost; }
+    at_once = n == 1 ? 74 : n == 2 ? 32 : 14;
+  }
+  const size_t smem = (size_t)rounds * kSelThreads * sizeof(int);
+  if (rounds <= 8) return launch_select_as<8>(c, l0, l1, n_cta, smem, weights, pos, since, len, keep, src, flags, device, s);
+  if (rounds <= 16) return launch_select_as<16>(c, l0, l1, n_cta, smem, weights, pos, since, len, keep, src, flags, device, s);
+  return launch_select_as<32>(c, l0, l1, n_cta, smem, weights, pos, since, len, keep, src, flags, device, s);
 }
 
 }  // namespace xkv
