@@ -15,7 +15,7 @@ struct Wait {
   volatile int* abort;
   unsigned int* flags;
 };
-static __device__ __noinline__ bool wait_slow(volatile int* abort, unsigned int* flags, uint32_t bar, uint32_t parity) {
+static __device__ __forceinline__ bool wait_slow(volatile int* abort, unsigned int* flags, uint32_t bar, uint32_t parity) {
   unsigned long long t0, t;
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
   do {

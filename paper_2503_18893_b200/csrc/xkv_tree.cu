@@ -37,6 +37,7 @@ constexpr int kMergeWarps = 8;
 
 struct TreeArgs {
   int batch, H_kv, H_q, n_rep, cap, n_draft, words, l0, layers, min_tiles;
+  uint32_t rep_inv;                            // ceil(2^16 / n_rep)
   float scale2;                                // softmax scale times log2(e)
   const __nv_bfloat16* q;
   const uint32_t* mask;                        // nullptr: token i attends to drafts 0 .. i
@@ -49,6 +50,9 @@ struct TreeArgs {
   float* lse;
   unsigned int* flags;
 };
+
+// m / n_rep for rows of Q: m < 4096, n_rep <= 16 and rep_inv = ceil(2^16 / n_rep), so the product's excess stays below one.
+__device__ __forceinline__ int token_of(const TreeArgs& a, int m) { return (int)(((uint32_t)m * a.rep_inv) >> 16); }
 
 // Rows and drafts of a sequence, brought into range; *bad reports what was not.
 __device__ __forceinline__ void tree_lengths(const TreeArgs& a, int b, int* len, int* drafts, bool* bad) {
@@ -86,59 +90,86 @@ __device__ __forceinline__ void next_problem(const TreeArgs& a, Place& p) {
   } while (p.nt == 0 && p.l < a.layers);
 }
 
-// Tiles of one head, all blocks of query rows, in sequences [0, n_seq) -- by a whole warp.
-template <int QT>
-__device__ __forceinline__ int head_tiles(const TreeArgs& a, int n_seq, bool report) {
-  const int lane = threadIdx.x & 31;
-  int sum = 0;
-  for (int b = lane; b < n_seq; b += 32) {
-    Place p;
-    p.b = b;
-    load_sequence<QT>(a, p);
-    sum += p.nt * p.n_qp;
-    if (report && a.flags) {
-      int x, y;
-      bool bad;
-      tree_lengths(a, b, &x, &y, &bad);
-      if (bad) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
-    }
-  }
-  return __reduce_add_sync(0xffffffffu, sum);
-}
-
 // CTAs that share `total` tiles.
 __device__ __forceinline__ int tree_ctas(const TreeArgs& a, int total, int grid) {
   return max(1, min(grid, total / a.min_tiles));
 }
 
-// The place of tile u of the list -- by a whole warp.  per_layer: tiles of a layer.
-template <int QT>
-__device__ __forceinline__ Place find_place(const TreeArgs& a, int u, int per_layer) {
-  const int lane = threadIdx.x & 31;
-  Place p;
-  p.l = u / per_layer;
-  int rest = u - p.l * per_layer;
-  for (int b0 = 0;; b0 += 32) {                // (u is in the list: the search ends inside the batch)
-    Place s;
-    s.b = min(b0 + lane, a.batch - 1);
-    load_sequence<QT>(a, s);
-    const int mine = b0 + lane < a.batch ? s.nt * s.n_qp * a.H_kv : 0;
-    int upto = mine;
+// Inclusive prefix sum over a warp.
+__device__ __forceinline__ int warp_prefix(int v) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += v;
-    }
-    const unsigned holds = __ballot_sync(0xffffffffu, rest < upto);
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, v, o);
+    if ((int)(threadIdx.x & 31) >= o) v += x;
+  }
+  return v;
+}
+
+// Lane: tiles of one head, all blocks of query rows, in sequence b0 + lane.
+template <int QT>
+__device__ __forceinline__ int lane_tiles(const TreeArgs& a, int b0, Place& s, bool report) {
+  s.b = b0 + (int)(threadIdx.x & 31);
+  if (s.b >= a.batch) return 0;
+  load_sequence<QT>(a, s);
+  if (report && a.flags) {
+    int x, y;
+    bool bad;
+    tree_lengths(a, s.b, &x, &y, &bad);
+    if (bad) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+  }
+  return s.nt * s.n_qp;
+}
+
+// By a whole warp: tiles of one head over the batch, and over the sequences before b.
+template <int QT>
+__device__ __forceinline__ int head_tiles(const TreeArgs& a, int b, int* before) {
+  int all = 0;
+  *before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    Place s;
+    const int v = lane_tiles<QT>(a, b0, s, false);
+    all += __reduce_add_sync(0xffffffffu, v);
+    *before += __reduce_add_sync(0xffffffffu, s.b < b ? v : 0);
+  }
+  return all;
+}
+
+// By a whole warp: the tiles [range[0], range[1]) of CTA c, and the place of the first.
+template <int QT>
+__device__ __forceinline__ Place find_piece(const TreeArgs& a, int c, int grid, int* range, bool report) {
+  const int lane = threadIdx.x & 31;
+  Place s;                                     // of this lane's sequence
+  const int mine = lane_tiles<QT>(a, 0, s, report);
+  int upto = warp_prefix(mine), head = __shfl_sync(0xffffffffu, upto, 31);
+  for (int b0 = 32; b0 < a.batch; b0 += 32) {
+    Place x;
+    head += __reduce_add_sync(0xffffffffu, lane_tiles<QT>(a, b0, x, report));
+  }
+  const int per_layer = head * a.H_kv, total = per_layer * a.layers, ctas = total > 0 ? tree_ctas(a, total, grid) : 0;
+  int u0 = 0, u1 = 0;
+  if (c < ctas) { u0 = piece_begin(total, ctas, c); u1 = piece_begin(total, ctas, c + 1); }
+  if (lane == 0) { range[0] = u0; range[1] = u1; }
+  Place p = s;
+  if (u1 == u0) return p;
+  p.l = u0 / per_layer;
+  int rest = u0 - p.l * per_layer, own = mine;
+  for (int b0 = 0;; ) {                        // (u0 is in the list: the search ends inside the batch)
+    const unsigned holds = __ballot_sync(0xffffffffu, rest < upto * a.H_kv);
     if (holds || b0 + 32 >= a.batch) {
       const int at = holds ? __ffs(holds) - 1 : 0;
-      rest -= __shfl_sync(0xffffffffu, upto - mine, at);
+      rest -= __shfl_sync(0xffffffffu, upto - own, at) * a.H_kv;
       p.b = b0 + at;
+      p.len = __shfl_sync(0xffffffffu, s.len, at);
+      p.drafts = __shfl_sync(0xffffffffu, s.drafts, at);
+      p.nt = __shfl_sync(0xffffffffu, s.nt, at);
+      p.n_qp = __shfl_sync(0xffffffffu, s.n_qp, at);
       break;
     }
-    rest -= __shfl_sync(0xffffffffu, upto, 31);
+    rest -= __shfl_sync(0xffffffffu, upto, 31) * a.H_kv;
+    b0 += 32;
+    own = lane_tiles<QT>(a, b0, s, false);
+    upto = warp_prefix(own);
   }
-  load_sequence<QT>(a, p);
   const int per_head = p.nt * p.n_qp;
   p.g = rest / per_head;
   rest -= p.g * per_head;
@@ -175,42 +206,51 @@ struct TreeSmem {
   static constexpr int kBytes = 1024 + QT * kSlot + kSlots * kSlot;
 };
 
+// One warpgroup of query rows: 192 threads, 255 registers each.  Two: the control warps fill a warpgroup (two of them idle), which
+// gives back registers that the others take: 384 * 168 at launch = 256 * 224 + 128 * 56.
+template <int QT>
+constexpr int tree_threads() { return QT == 2 ? 384 : 192; }
+
 template <int DH, int QT>
-__global__ void __launch_bounds__(QT * 128 + 64, 1)
+__global__ void __launch_bounds__(tree_threads<QT>(), 1)
 tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const TreeArgs a) {
   using namespace ptx;
   using L = TreeSmem<DH, QT>;
   constexpr int NS = L::kSlots;
   constexpr uint32_t kSlab16 = L::kSlab >> 4;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars_s[2 * NS + 9];
+  __shared__ uint64_t bars_s[2 * NS + 11];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   __shared__ Place place_s;
   __shared__ int range_s[2];
-  __shared__ uint32_t bad_s[2][8];             // drafts with elements that are not finite, of this segment and the next
+  // Drafts with elements that are not finite, by segment: a warpgroup is ahead of the other by a ring of tiles at most, so by
+  // less than eight segments.
+  __shared__ uint32_t bad_s[16][8];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t ring = base + QT * L::kSlot;
   const uint32_t bars = smem_u32(bars_s);
   const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_s = bars + 16 * NS, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16,
-                 b_drain = b_q + 16;
+                 b_drain = b_q + 16, b_turn = b_drain + 16;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kProducer = QT * 4, kIssuer = QT * 4 + 1;
 
   if (tid == 0) {
-    for (int i = 0; i < NS; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
+    for (int i = 0; i < NS; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, QT); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(b_s + 8 * i, 1);
-      mbar_init(b_p + 8 * i, 128);
+      mbar_init(b_p + 8 * i, 4);               // (a warp arrives once: 128 arrivals at one word take their time)
       mbar_init(b_o + 8 * i, 1);
-      mbar_init(b_q + 8 * i, 128);
+      mbar_init(b_q + 8 * i, 4);
     }
     mbar_init(b_drain, 1);
+    mbar_init(b_drain + 8, 1);
+    mbar_init(b_turn, 4);
     fence_mbar_init();
     abort_s = 0;
   }
-  if (tid < 16) bad_s[tid >> 3][tid & 7] = 0u;
+  if (tid < 128) bad_s[tid >> 3][tid & 7] = 0u;
   if (warp == kIssuer) {
     tmem_alloc(smem_u32(&tmem_s), 512);
     tmem_relinquish();
@@ -218,17 +258,8 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   grid_dependency_wait();                      // everything below may come from the kernel before
   grid_dependency_launch();
   if (warp == kProducer) {
-    const int per_layer = head_tiles<QT>(a, a.batch, blockIdx.x == 0) * a.H_kv, total = per_layer * a.layers;
-    int u0 = 0, u1 = 0;
-    if (total > 0) {
-      const int ctas = tree_ctas(a, total, gridDim.x), c = blockIdx.x;
-      if (c < ctas) { u0 = piece_begin(total, ctas, c); u1 = piece_begin(total, ctas, c + 1); }
-    }
-    if (u1 > u0) {
-      const Place p = find_place<QT>(a, u0, per_layer);
-      if (lane == 0) place_s = p;
-    }
-    if (lane == 0) { range_s[0] = u0; range_s[1] = u1; }
+    const Place p = find_piece<QT>(a, blockIdx.x, gridDim.x, range_s, blockIdx.x == 0);
+    if (lane == 0) place_s = p;
   }
   tc_fence_before();
   __syncthreads();
@@ -239,6 +270,8 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   Place p = place_s;
   uint32_t n_loaded = 0;                       // producer: tiles (K and V each) asked for
 
+  if (warp >= QT * 4) {
+  if constexpr (QT == 2) regs_release<72>();
   if (left > 0 && warp == kProducer) {
     if (lane == 0) {                           // (the others of the warp wait at its end)
       bool ok = true;
@@ -250,6 +283,8 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t slot = n_loaded % NS;
+            // the first queries come before the rest of the ring, which takes the memory a while
+            if (n_loaded == 2 && !(wait_bar(wt, b_q, 0u) && (QT == 1 || wait_bar(wt, b_q + 8, 0u)))) { ok = false; break; }
             if (!wait_bar(wt, b_empty + 8 * slot, ((n_loaded / NS) & 1u) ^ 1u)) { ok = false; break; }
             mbar_expect_tx(b_full + 8 * slot, L::kSlot);
 #pragma unroll
@@ -262,75 +297,90 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       }
     }
     __syncwarp();
-  } else if (left > 0 && warp == kIssuer) {
-    const uint64_t hi = smem_desc_sw128(0, 0) & 0xFFFFFFFF00000000ull;
+  } else if (left > 0 && warp < kIssuer + QT) {
+    // ---- an issuing warp for each 128 rows of Q (a thread spends 70 to 130 cycles on an MMA and 235 on a commit).  Branches
+    // outside the issue are taken on a vote and descriptors differ by constants, so that they stay in uniform registers.
+    const int qt = warp - kIssuer;
     constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTile);
     constexpr uint32_t idesc_o = idesc_bf16_f32(128, DH) | (1u << 16);         // V is read along its rows (MN-major)
-    const uint32_t q_lo = (uint32_t)smem_desc_sw128(base, 0);
-    const uint32_t k_lo = (uint32_t)smem_desc_sw128(ring, 0);
-    const uint32_t v_lo = ((uint32_t)smem_desc_sw128(ring, 0) & 0xFFFFu) | (kSlab16 << 16);
+    const uint64_t q_desc = smem_desc_sw128(base + qt * L::kSlot, 0), k_desc = smem_desc_sw128(ring, 0);
+    const uint64_t v_desc = (k_desc & ~(0xFFFFull << 16)) | ((uint64_t)kSlab16 << 16);
     uint32_t n = 0, it = 0, seg = 0;           // ring position of the next K tile; tiles done; segments done
     bool ok = true;
-    // S of the tile at ring position n into its buffer
-    auto logits = [&](int qt, uint32_t it_of, uint32_t n_of) {
-      const uint32_t buf = QT == 2 ? (uint32_t)qt : (it_of & 1u);
-      const uint32_t ka = k_lo + (n_of % NS) * (uint32_t)(L::kSlot >> 4), qa = q_lo + (uint32_t)qt * (L::kSlot >> 4);
+    auto logits = [&](uint32_t d, uint32_t n_of) {
+      const uint64_t kd = k_desc + (uint64_t)((n_of % NS) * (uint32_t)(L::kSlot >> 4));
 #pragma unroll
       for (int k = 0; k < DH / 16; ++k) {
-        const uint32_t off = (uint32_t)(k >> 2) * kSlab16 + (uint32_t)(k & 3) * 2u;
-        tc_mma_bf16(tmem + buf * 128u, hi | (qa + off), hi | (ka + off), idesc_s, k ? 1u : 0u);
+        const uint64_t off = (uint64_t)((k >> 2) * (int)kSlab16 + (k & 3) * 2);
+        tc_mma_bf16(d, q_desc + off, kd + off, idesc_s, k ? 1u : 0u);
       }
-      tc_commit(b_s + 8 * buf);
     };
+    auto values = [&](uint32_t d, uint32_t p_addr, uint32_t n_of, uint32_t accumulate) {
+      const uint64_t vd = v_desc + (uint64_t)((n_of % NS) * (uint32_t)(L::kSlot >> 4));
+#pragma unroll
+      for (int k = 0; k < kTile / 16; ++k)
+        tc_mma_bf16_ts(d, p_addr + (uint32_t)k * 8u, vd + (uint64_t)(k * (2048 >> 4)), idesc_o, k ? 1u : accumulate);
+    };
+    auto wait_slot = [&](uint32_t n_of) { return wait_warp(wt, b_full + 8 * (n_of % NS), (n_of / NS) & 1u); };
+    const uint32_t o_tmem = tmem + 256u + (uint32_t)qt * 128u;
     while (left > 0 && ok) {
       const int t1 = min(p.nt, p.t + left), cnt = t1 - p.t;
       left -= cnt;
-      for (int qt = 0; qt < QT && ok; ++qt) ok = wait_warp(wt, b_q + 8 * qt, seg & 1u);
-      ok = ok && wait_warp(wt, b_full + 8 * (n % NS), (n / NS) & 1u);
+      ok = wait_warp(wt, b_q + 8 * qt, seg & 1u) && wait_slot(n);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
-        for (int qt = 0; qt < QT; ++qt) logits(qt, it, n);
-        tc_commit(b_empty + 8 * (n % NS));
+        const uint32_t buf = QT == 2 ? (uint32_t)qt : (it & 1u);
+        logits(tmem + buf * 128u, n);
+        tc_commit(b_s + 8 * buf);
+        if (QT == 1) tc_commit(b_empty + 8 * (n % NS));
       }
+      __syncwarp();
       for (int t = 0; t < cnt; ++t, ++it, n += 2) {
         const bool more = t + 1 < cnt;
-        if (QT == 1 && more) {                 // the next tile's logits go into the other buffer while this one's are worked on
-          if (!(ok = wait_warp(wt, b_full + 8 * ((n + 2) % NS), ((n + 2) / NS) & 1u))) break;
-          if (elect_one()) {
-            logits(0, it + 1, n + 2);
-            tc_commit(b_empty + 8 * ((n + 2) % NS));
-          }
-        }
-        if (!(ok = wait_warp(wt, b_full + 8 * ((n + 1) % NS), ((n + 1) / NS) & 1u))) break;
-        const uint32_t va = v_lo + ((n + 1) % NS) * (uint32_t)(L::kSlot >> 4);
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          const uint32_t buf = QT == 2 ? (uint32_t)qt : (it & 1u);
-          if (!(ok = wait_warp(wt, b_p + 8 * buf, QT == 2 ? (it & 1u) : ((it >> 1) & 1u)))) break;
+        if constexpr (QT == 2) {
+          // S lies where P did: its product follows the one that reads P.  One commit tells that this tile's values and the next
+          // one's logits are done; whoever waits for it gives their slots back.
+          if (!(ok = wait_slot(n + 1))) break;
+          if (more && !(ok = wait_slot(n + 2))) break;
+          if (!(ok = wait_warp(wt, b_p + 8 * qt, it & 1u))) break;
           tc_fence_after();
           if (elect_one()) {
-#pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-              tc_mma_bf16_ts(tmem + 256u + (uint32_t)qt * 128u, tmem + buf * 128u + 64u + (uint32_t)k * 8u,
-                             hi | (va + (uint32_t)k * (2048u >> 4)), idesc_o, (t | k) ? 1u : 0u);
-            tc_commit(b_o + 8 * qt);
-            if (qt == QT - 1) tc_commit(b_empty + 8 * ((n + 1) % NS));
+            values(o_tmem, tmem + (uint32_t)qt * 128u + 64u, n + 1, t ? 1u : 0u);
+            if (more) logits(tmem + (uint32_t)qt * 128u, n + 2);
+            tc_commit(more ? b_s + 8 * qt : b_o + 8 * qt);
           }
-          if (QT == 2 && more) {               // S lies where P did: behind the product that reads P
-            if (qt == 0 && !(ok = wait_warp(wt, b_full + 8 * ((n + 2) % NS), ((n + 2) / NS) & 1u))) break;
+          __syncwarp();
+        } else {
+          // the next tile's logits go into the other buffer while this one's are worked on
+          const uint32_t buf = it & 1u;
+          if (more) {
+            if (!(ok = wait_slot(n + 2))) break;
             if (elect_one()) {
-              logits(qt, it + 1, n + 2);
-              if (qt == QT - 1) tc_commit(b_empty + 8 * ((n + 2) % NS));
+              logits(tmem + (buf ^ 1u) * 128u, n + 2);
+              tc_commit(b_s + 8 * (buf ^ 1u));
+              tc_commit(b_empty + 8 * ((n + 2) % NS));
             }
+            __syncwarp();
           }
+          if (!(ok = wait_slot(n + 1))) break;
+          if (!(ok = wait_warp(wt, b_p + 8 * buf, (it >> 1) & 1u))) break;
+          tc_fence_after();
+          if (elect_one()) {
+            values(o_tmem, tmem + buf * 128u + 64u, n + 1, t ? 1u : 0u);
+            tc_commit(b_o);
+            tc_commit(b_empty + 8 * ((n + 1) % NS));
+          }
+          __syncwarp();
         }
-        if (!ok) break;
       }
       ++seg;
       if (left > 0 && ok) next_problem<QT>(a, p);
     }
-  } else if (left > 0) {
+  }
+  } else {
+  if constexpr (QT == 2) regs_take<216>();
+  if (left > 0) {
     const int qt = warp >> 2, row = tid & 127;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     uint8_t* q_gen = gen + qt * L::kSlot;
@@ -343,138 +393,158 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       const int rows_q = p.drafts * a.n_rep;                   // rows of Q of this sequence
       const int m0 = (p.qp * QT + qt) * kQRows;                // this warpgroup's first
       // ---- Q as the A operand: 64-column slabs, 128-byte rows, 16-byte units swizzled by the row; rows behind the last are 0
-      for (int i = row; i < kQRows * (DH / 8); i += 128) {
-        const int r = i / (DH / 8), c = i % (DH / 8), m = m0 + r;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (m < rows_q) {
-          const int token = m / a.n_rep, h = m - token * a.n_rep;
-          const size_t at = ((((size_t)(a.l0 + p.l) * a.batch + p.b) * a.n_draft + token) * a.H_q + (size_t)p.g * a.n_rep + h) * DH + c * 8;
-          v = *reinterpret_cast<const uint4*>(a.q + at);
+      // (a warp brings its own 32 rows, and their place is its own in the epilogue too)
+      {
+        constexpr int C = DH / 8, STEP = 32 / C, U = 8;        // 16-byte units of a row; rows per round; rounds in flight
+        const int c = lane % C, r0 = (warp & 3) * 32 + lane / C;
+        const __nv_bfloat16* q0 = a.q + (((size_t)(a.l0 + p.l) * a.batch + p.b) * a.n_draft * a.H_q + (size_t)p.g * a.n_rep) * DH + c * 8;
+#pragma unroll
+        for (int i0 = 0; i0 < C; i0 += U) {
+          uint4 v[U];
+#pragma unroll
+          for (int i = 0; i < U; ++i) {
+            const int mm = m0 + r0 + (i0 + i) * STEP, token = token_of(a, mm);
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (mm < rows_q) v[i] = *reinterpret_cast<const uint4*>(q0 + ((size_t)token * a.H_q + (mm - token * a.n_rep)) * DH);
+          }
+#pragma unroll
+          for (int i = 0; i < U; ++i) {
+            const int r = r0 + (i0 + i) * STEP;
+            *reinterpret_cast<uint4*>(q_gen + (c >> 3) * L::kSlab + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
+          }
         }
-        *reinterpret_cast<uint4*>(q_gen + (c >> 3) * L::kSlab + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
       }
       fence_proxy_async();
-      mbar_arrive(b_q + 8 * qt);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b_q + 8 * qt);
       const int m = m0 + row;
       const bool live = m < rows_q;
       const bool warp_live = m0 + (row & ~31) < rows_q;
-      const int token = live ? m / a.n_rep : 0;
+      const int token = live ? token_of(a, m) : 0;
       const uint32_t* mask_row = a.mask ? a.mask + ((size_t)p.b * a.n_draft + token) * a.words : nullptr;
-      float m_used = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+      float m_used = -INFINITY;
+      u64 l2[2] = {0ull, 0ull};                // four partial sums of the weights
       bool odd = false;                        // tiles of this segment held drafts
       for (int t = t0; t < t1; ++t, ++it) {
         const uint32_t buf = QT == 2 ? (uint32_t)qt : (it & 1u);
         if (!(ok = wait_warp(wt, b_s + 8 * buf, QT == 2 ? (it & 1u) : ((it >> 1) & 1u)))) break;
         tc_fence_after();
-        // the next segment's list: whoever read it last (two segments ago) has handed over this segment's queries since
-        if (qt == 0 && t == t0 && row < 8) bad_s[(seg + 1) & 1u][row] = 0u;
+        // The second warpgroup begins when the first one is done with its first tile: from then on one's exponentials run beside the
+        // other's products.
+        if (QT == 2 && qt == 1 && it == 0 && !(ok = wait_warp(wt, b_turn, 0u))) break;
+        if (QT == 2 && row == 0) {             // done with: this tile's keys, the values of the one before
+          mbar_arrive(b_empty + 8 * ((2u * it) % NS));
+          if (t > t0) mbar_arrive(b_empty + 8 * ((2u * it - 1u) % NS));
+        }
+        if (qt == 0 && t == t0 && row < 8) bad_s[(seg + 8) & 15u][row] = 0u;
         const uint32_t s_addr = tmem + lane_base + buf * 128u;
         const bool masked = (t + 1) * kTile > p.len;
         if (warp_live) {
-          // the maximum needs all 128 logits, the weights need them again: half of them stay in registers, half are read twice
-          uint32_t bits[4];
-          if (masked) {
+          uint32_t z[4][32];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) bits[i] = row_bits(a, mask_row, token, t * kTile + 32 * i, p.len, p.drafts);
-          }
-          float z[2][32], mx[2] = {-INFINITY, -INFINITY};
-          auto load = [&](int half) {
+          for (int i = 0; i < 4; ++i) tmem_ld32_nb(s_addr + 32u * i, z[i]);
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) tmem_ld32(s_addr + 64u * half + 32u * i, z[i]);
-            tc_wait_ld();
+          for (int i = 0; i < 4; ++i) {
+            tc_wait_ld32_nb(z[i]);
             if (masked) {
+              const uint32_t w = row_bits(a, mask_row, token, t * kTile + 32 * i, p.len, p.drafts);
 #pragma unroll
-              for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int e = 0; e < 32; ++e) z[i][e] = (bits[2 * half + i] >> e) & 1u ? z[i][e] : -INFINITY;
+              for (int e = 0; e < 32; ++e) z[i][e] = (w >> e) & 1u ? z[i][e] : 0xff800000u;
             }
-          };
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            load(half);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int e = 0; e < 32; ++e) mx[i] = fmaxf(mx[i], z[i][e]);
+            for (int e = 0; e < 32; e += 2)
+              mx[(e >> 1) & 3] = fmaxf(fmaxf(mx[(e >> 1) & 3], __uint_as_float(z[i][e])), __uint_as_float(z[i][e + 1]));
           }
-          const float m_new = fmaxf(m_used, fmaxf(mx[0], mx[1]) * a.scale2);
+          const float m_new = fmaxf(m_used, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2);
           if (t == t0) {
             m_used = m_new;
           } else {
             const bool grow = m_new > m_used + kGrow || (m_used == -INFINITY && m_new > -INFINITY);
             if (__any_sync(0xffffffffu, grow)) {
-              // O holds the tiles before this one once their product is done
-              if (!(ok = wait_warp(wt, b_o + 8 * qt, (it - 1u) & 1u))) break;
-              tc_fence_after();
+              // O holds the tiles before this one once their product is done (two warpgroups: it is, before these logits)
+              if (QT == 1) {
+                if (!(ok = wait_warp(wt, b_o, (it - 1u) & 1u))) break;
+                tc_fence_after();
+              }
               const float f = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
               if (grow) m_used = m_new;
-              l0 *= f;
-              l1 *= f;
+              const u64 f2 = pack2(f, f);
+              l2[0] = mul2(l2[0], f2);
+              l2[1] = mul2(l2[1], f2);
 #pragma unroll 1
-              for (int c = 0; c < DH; c += 32) {
-                float o[32];
-                uint32_t r[32];
-                tmem_ld32(o_addr + (uint32_t)c, o);
+              for (int c = 0; c < DH; c += 16) {
+                float o[16];
+                uint32_t r[16];
+                tmem_ld<16>(o_addr + (uint32_t)c, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(o[e] * f);
-                tmem_st32(o_addr + (uint32_t)c, r);
+                for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(o[e] * f);
+                tmem_st16(o_addr + (uint32_t)c, r);
               }
             }
           }
           const float shift = m_used == -INFINITY ? 0.0f : m_used;
-          auto weights = [&](int half) {       // P, two to a column, in the upper half of S's columns
-            uint32_t r[32];
+          const u64 scale_2 = pack2(a.scale2, a.scale2), shift_2 = pack2(-shift, -shift);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float p0 = ex2_approx(fmaf(z[e >> 4][2 * (e & 15)], a.scale2, -shift));
-              const float p1 = ex2_approx(fmaf(z[e >> 4][2 * (e & 15) + 1], a.scale2, -shift));
-              l0 += p0;
-              l1 += p1;
-              r[e] = pack_bf16(p0, p1);
+          for (int i = 0; i < 4; ++i) {        // P, two to a column, in the upper half of S's columns
+            uint32_t r[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float2 w = unpack2(fma2(pack2u(z[i][2 * e], z[i][2 * e + 1]), scale_2, shift_2));
+              w.x = ex2_approx(w.x);
+              w.y = ex2_approx(w.y);
+              l2[e & 1] = add2(l2[e & 1], pack2(w.x, w.y));
+              r[e] = pack_bf16(w.x, w.y);
             }
-            tmem_st32(s_addr + 64u + 32u * half, r);
-          };
-          weights(1);
-          load(0);
-          weights(0);
+            tmem_st16(s_addr + 64u + 16u * i, r);
+          }
           tc_wait_st();
         }
         if (masked) {
           odd = true;
-          if (qt == 0) {
-            // thread = value row: what no token holds is zeroed, what is not finite in a draft's row is taken out
-            const uint32_t nv = 2u * it + 1u, slot = nv % NS;
-            if (!(ok = wait_warp(wt, b_full + 8 * slot, (nv / NS) & 1u))) break;
-            const int draft = t * kTile + row - p.len;
-            if (draft >= 0) {
-              uint8_t* v = gen + QT * L::kSlot + slot * L::kSlot + row * 128;
-              bool hit = false;
-              for (int c = 0; c < DH / 8; ++c) {
-                uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * L::kSlab + (((c & 7) ^ (row & 7)) << 4));
-                uint4 x = draft < p.drafts ? *at : make_uint4(0u, 0u, 0u, 0u);
-                uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+          // thread = value row: what no token holds is zeroed, what is not finite in a draft's row is taken out.  Both warpgroups do
+          // it, to the same effect; one that finds a row cleared finds it listed, too.
+          const uint32_t nv = 2u * it + 1u, slot = nv % NS;
+          if (!(ok = wait_warp(wt, b_full + 8 * slot, (nv / NS) & 1u))) break;
+          const int draft = t * kTile + row - p.len;
+          if (draft >= 0) {
+            uint8_t* v = gen + QT * L::kSlot + slot * L::kSlot + row * 128;
+#pragma unroll 1
+            for (int c = 0; c < DH / 8; ++c) {
+              uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * L::kSlab + (((c & 7) ^ (row & 7)) << 4));
+              uint4 x = draft < p.drafts ? *at : make_uint4(0u, 0u, 0u, 0u);
+              uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+              bool hit = draft >= p.drafts;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
-                  if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+              for (int e = 0; e < 4; ++e) {
+                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
+                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+              }
+              if (hit) {
+                if (draft < p.drafts) {
+                  atomicOr(&bad_s[seg & 15u][draft >> 5], 1u << (draft & 31));
+                  __threadfence_block();
                 }
                 *at = x;
               }
-              if (hit) atomicOr(&bad_s[seg & 1u][draft >> 5], 1u << (draft & 31));
             }
-            fence_proxy_async();
           }
+          fence_proxy_async();
         }
         tc_fence_before();
-        mbar_arrive(b_p + 8 * buf);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_p + 8 * buf);
+        if (QT == 2 && qt == 0 && it == 0 && lane == 0) mbar_arrive(b_turn);
       }
       if (!ok) break;
       // ---- the segment's result
-      if (!(ok = wait_warp(wt, b_o + 8 * qt, (it - 1u) & 1u))) break;
+      if (!(ok = wait_warp(wt, b_o + 8 * qt, (QT == 2 ? seg : it - 1u) & 1u))) break;
       tc_fence_after();
+      if (QT == 2 && row == 0) mbar_arrive(b_empty + 8 * ((2u * it - 1u) % NS));
       const bool whole = t0 == 0 && t1 == p.nt;
-      const float l = l0 + l1;
+      const float2 la = unpack2(add2(l2[0], l2[1]));
+      const float l = la.x + la.y;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       const size_t qh = (((size_t)(a.l0 + p.l) * a.batch + p.b) * a.n_draft + token) * a.H_q + (size_t)p.g * a.n_rep + (m - token * a.n_rep);
       const size_t pr = ((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * (QT * kQRows) + qt * kQRows + row;
@@ -487,7 +557,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           if (odd) {
 #pragma unroll 1
             for (int w = 0; w < a.words; ++w) {
-              uint32_t bad = bad_s[seg & 1u][w];               // (entered before the product that this result waited for)
+              uint32_t bad = bad_s[seg & 15u][w];              // (entered before the product that this result waited for)
               while (bad) {
                 const int j = 32 * w + __ffs(bad) - 1;
                 bad &= bad - 1u;
@@ -507,10 +577,19 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             for (int e = 0; e < 4; ++e)
               dst[e] = make_uint4(pack_bf16(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
                                   pack_bf16(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
-          } else if (live) {
-            float4* dst = reinterpret_cast<float4*>(a.part + pr * DH + c);
+          } else if (!whole) {
+            // through the place of this warp's rows of Q, so that a store writes whole lines
+            float4* st = reinterpret_cast<float4*>(q_gen + (warp & 3) * 4096);
+            __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 8; ++e) st[lane * 8 + (e ^ (lane & 7))] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            __syncwarp();
+            float* dst = a.part + (pr - row + (warp & 3) * 32) * DH + c + (lane & 7) * 4;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = 4 * i + (lane >> 3);
+              *reinterpret_cast<float4*>(dst + (size_t)r * DH) = st[r * 8 + ((lane & 7) ^ (r & 7))];
+            }
           }
         }
         if (live && whole && a.lse) a.lse[qh] = l == 0.0f ? -INFINITY : (m_used + log2f(l)) * 0.6931471805599453f;
@@ -522,15 +601,20 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     }
   }
 
+  }
   // wind down: nothing of this CTA may still touch shared or tensor memory
   tc_fence_before();
   __syncthreads();
+  if (abort_s) {                               // given up: nothing may still write tensor memory when it is freed
+    if (warp >= kIssuer && warp < kIssuer + QT) {
+      const uint32_t bar = b_drain + 8 * (warp - kIssuer);
+      if (elect_one()) tc_commit(bar);
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(bar, 0))) break;
+    }
+    __syncthreads();
+  }
   if (warp == kIssuer) {
     tc_fence_after();
-    if (abort_s) {                             // given up: nothing may still write tensor memory when it is freed
-      if (elect_one()) tc_commit(b_drain);
-      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(b_drain, 0))) break;
-    }
     tmem_dealloc(tmem, 512);
   }
   if (abort_s && warp == kProducer && lane == 0) {
@@ -554,33 +638,54 @@ tree_merge_kernel(const TreeArgs a, int attend_grid) {
   p.b = b;
   load_sequence<QT>(a, p);
   if (m >= p.drafts * a.n_rep) return;
-  const int head = head_tiles<QT>(a, a.batch, false), before = head_tiles<QT>(a, b, false);
+  int before;
+  const int head = head_tiles<QT>(a, b, &before);
   const int total = head * a.H_kv * a.layers, ctas = tree_ctas(a, total, attend_grid);
   const int qp = m / (QT * kQRows);
   const int u0 = (l * head + before) * a.H_kv + (g * p.n_qp + qp) * p.nt, u1 = u0 + p.nt;
   const int c0 = piece_of(total, ctas, u0), c1 = piece_of(total, ctas, u1 - 1);
   if (c0 == c1) return;                        // one piece: written where it was computed
-  const int r = m - qp * QT * kQRows;
-  // a problem that begins inside a piece is that piece's last one
-  const int first_slot = piece_begin(total, ctas, c0) == u0 ? 0 : 1;
-  auto slot = [&](int c) { return ((size_t)c * 2 + (c == c0 ? first_slot : 0)) * (QT * kQRows) + r; };
-  float M = -INFINITY;
-  for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, a.part_ml[slot(c)].x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  float acc[V], sum = 0.0f;
+  // a problem that begins inside a piece is that piece's last one, and in the others the first
+  const size_t r = (size_t)(m - qp * QT * kQRows), first = (size_t)c0 * 2 + (piece_begin(total, ctas, c0) == u0 ? 0 : 1);
+  auto slot = [&](int c) { return (c == c0 ? first : (size_t)c * 2) * (QT * kQRows) + r; };
+  float M = -INFINITY, acc[V], sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-  for (int c = c0; c <= c1; ++c) {
-    const float2 ml = a.part_ml[slot(c)];
-    const float f = ml.x == -INFINITY ? (ml.y == 0.0f ? 0.0f : 1.0f) : exp2f(ml.x - M);       // (a piece of NaNs stays one)
-    const float* src = a.part + slot(c) * DH + lane * V;
-    sum = fmaf(f, ml.y, sum);
+  for (int cb = c0; cb <= c1; cb += 32) {      // lane: the weight of one piece of 32
+    const int n = min(32, c1 - cb + 1);
+    const float2 ml = lane < n ? a.part_ml[slot(cb + lane)] : make_float2(-INFINITY, 0.0f);
+    float top = ml.x;
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = fmaf(f, src[i], acc[i]);
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float M_new = fmaxf(M, top), old = M == -INFINITY ? 1.0f : exp2f(M - M_new);
+    const float f = ml.x == -INFINITY ? (ml.y == 0.0f ? 0.0f : 1.0f) : exp2f(ml.x - M_new);           // (a piece of NaNs stays one)
+    M = M_new;
+    float part = f * ml.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+    sum = fmaf(sum, old, part);
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] *= old;
+    for (int j0 = 0; j0 < n; j0 += 8) {        // eight pieces' rows in flight
+      float x[8][V];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float* src = a.part + slot(cb + min(j0 + j, n - 1)) * DH + lane * V;
+        if constexpr (V == 4) *reinterpret_cast<float4*>(x[j]) = *reinterpret_cast<const float4*>(src);
+        else *reinterpret_cast<float2*>(x[j]) = *reinterpret_cast<const float2*>(src);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float w = __shfl_sync(0xffffffffu, f, (j0 + j) & 31);
+        if (j0 + j < n) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) acc[i] = fmaf(w, x[j][i], acc[i]);
+        }
+      }
+    }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const int token = m / a.n_rep;
+  const int token = token_of(a, m);
   const size_t qh = (((size_t)(a.l0 + l) * a.batch + b) * a.n_draft + token) * a.H_q + (size_t)g * a.n_rep + (m - token * a.n_rep);
   uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + qh * DH + lane * V);
 #pragma unroll
@@ -591,7 +696,7 @@ tree_merge_kernel(const TreeArgs a, int attend_grid) {
 template <int DH, int QT>
 cudaError_t launch_tree_as(const CUtensorMap& k_map, const CUtensorMap& v_map, const TreeArgs& a, int grid, int device, cudaStream_t s) {
   cudaError_t e = ensure_dyn_smem<tree_attend_kernel<DH, QT>>(TreeSmem<DH, QT>::kBytes, device);
-  if (e == cudaSuccess) e = launch_pdl(tree_attend_kernel<DH, QT>, dim3(grid), dim3(QT * 128 + 64), TreeSmem<DH, QT>::kBytes, s, k_map, v_map, a);
+  if (e == cudaSuccess) e = launch_pdl(tree_attend_kernel<DH, QT>, dim3(grid), dim3(tree_threads<QT>()), TreeSmem<DH, QT>::kBytes, s, k_map, v_map, a);
   if (e != cudaSuccess) return e;
   const int rows = a.n_draft * a.n_rep;
   e = launch_pdl(tree_merge_kernel<DH, QT>, dim3(a.layers * a.batch * a.H_kv, (rows + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, s,
@@ -621,6 +726,7 @@ cudaError_t launch_tree_attend(const xkv_cache_config* c, int l0, int l1, const 
   TreeArgs a;
   a.batch = c->batch; a.H_kv = c->H_kv; a.H_q = c->H_q; a.n_rep = c->H_q / c->H_kv; a.cap = c->cap; a.n_draft = n_draft;
   a.words = (n_draft + 31) / 32; a.l0 = l0; a.layers = l1 - l0; a.min_tiles = 1;
+  a.rep_inv = (65536u + a.n_rep - 1u) / a.n_rep;
   a.scale2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / sqrtf((float)c->d_h)) * kLog2e;
   a.q = q; a.mask = mask; a.draft_len = draft_len; a.V = V; a.len = len; a.out = out; a.lse = lse; a.flags = flags;
   const int rows_q = n_draft * a.n_rep, qt = rows_q > kQRows ? 2 : 1;
