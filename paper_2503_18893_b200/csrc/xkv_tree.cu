@@ -206,20 +206,21 @@ struct TreeSmem {
   static constexpr int kBytes = 1024 + QT * kSlot + kSlots * kSlot;
 };
 
-// One warpgroup of query rows: 192 threads, 255 registers each.  Two: the control warps fill a warpgroup (two of them idle), which
-// gives back registers that the others take: 384 * 168 at launch = 256 * 224 + 128 * 56.
+// Warpgroups of query rows, the producer, an issuer for each warpgroup.
 template <int QT>
-constexpr int tree_threads() { return QT == 2 ? 384 : 192; }
+constexpr int tree_threads() { return QT * 128 + 32 + QT * 32; }
 
 template <int DH, int QT>
 __global__ void __launch_bounds__(tree_threads<QT>(), 1)
 tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const TreeArgs a) {
   using namespace ptx;
   using L = TreeSmem<DH, QT>;
+  // A step is KW rows of a tile, and S has room for two steps (512 columns of tensor memory: S and O of QT * 128 rows).
+  constexpr int KW = QT == 2 ? 64 : 128, SPT = kTile / KW;
   constexpr int NS = L::kSlots;
   constexpr uint32_t kSlab16 = L::kSlab >> 4;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars_s[2 * NS + 11];
+  __shared__ uint64_t bars_s[2 * NS + 17];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   __shared__ Place place_s;
@@ -231,22 +232,18 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t ring = base + QT * L::kSlot;
   const uint32_t bars = smem_u32(bars_s);
-  const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_s = bars + 16 * NS, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16,
-                 b_drain = b_q + 16, b_turn = b_drain + 16;
+  const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_s = bars + 16 * NS, b_p = b_s + 32, b_o = b_p + 32, b_q = b_o + 32,
+                 b_drain = b_q + 16, b_first = b_drain + 16;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kProducer = QT * 4, kIssuer = QT * 4 + 1;
 
   if (tid == 0) {
     for (int i = 0; i < NS; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, QT); }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(b_s + 8 * i, 1);
-      mbar_init(b_p + 8 * i, 4);               // (a warp arrives once: 128 arrivals at one word take their time)
-      mbar_init(b_o + 8 * i, 1);
-      mbar_init(b_q + 8 * i, 4);
-    }
+    for (int i = 0; i < 4; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_p + 8 * i, 4); mbar_init(b_o + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) mbar_init(b_q + 8 * i, 4);      // (a warp arrives once: 128 arrivals take their time)
+    mbar_init(b_first, QT * 4);
     mbar_init(b_drain, 1);
     mbar_init(b_drain + 8, 1);
-    mbar_init(b_turn, 4);
     fence_mbar_init();
     abort_s = 0;
   }
@@ -271,7 +268,6 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   uint32_t n_loaded = 0;                       // producer: tiles (K and V each) asked for
 
   if (warp >= QT * 4) {
-  if constexpr (QT == 2) regs_release<72>();
   if (left > 0 && warp == kProducer) {
     if (lane == 0) {                           // (the others of the warp wait at its end)
       bool ok = true;
@@ -284,7 +280,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           for (int kv = 0; kv < 2; ++kv) {
             const uint32_t slot = n_loaded % NS;
             // the first queries come before the rest of the ring, which takes the memory a while
-            if (n_loaded == 2 && !(wait_bar(wt, b_q, 0u) && (QT == 1 || wait_bar(wt, b_q + 8, 0u)))) { ok = false; break; }
+            if (n_loaded == 2 && !wait_bar(wt, b_first, 0u)) { ok = false; break; }
             if (!wait_bar(wt, b_empty + 8 * slot, ((n_loaded / NS) & 1u) ^ 1u)) { ok = false; break; }
             mbar_expect_tx(b_full + 8 * slot, L::kSlot);
 #pragma unroll
@@ -301,91 +297,65 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     // ---- an issuing warp for each 128 rows of Q (a thread spends 70 to 130 cycles on an MMA and 235 on a commit).  Branches
     // outside the issue are taken on a vote and descriptors differ by constants, so that they stay in uniform registers.
     const int qt = warp - kIssuer;
-    constexpr uint32_t idesc_s = idesc_bf16_f32(128, kTile);
+    constexpr uint32_t idesc_s = idesc_bf16_f32(128, KW);
     constexpr uint32_t idesc_o = idesc_bf16_f32(128, DH) | (1u << 16);         // V is read along its rows (MN-major)
     const uint64_t q_desc = smem_desc_sw128(base + qt * L::kSlot, 0), k_desc = smem_desc_sw128(ring, 0);
     const uint64_t v_desc = (k_desc & ~(0xFFFFull << 16)) | ((uint64_t)kSlab16 << 16);
-    uint32_t n = 0, it = 0, seg = 0;           // ring position of the next K tile; tiles done; segments done
+    const uint32_t s_tmem = tmem + (uint32_t)qt * 128u, o_tmem = tmem + 256u + (uint32_t)qt * 128u;
+    uint32_t n = 0, st = 0, n_o = 0, seg = 0;  // ring position of the segment's first K tile; steps, commits on b_o, segments so far
     bool ok = true;
-    auto logits = [&](uint32_t d, uint32_t n_of) {
-      const uint64_t kd = k_desc + (uint64_t)((n_of % NS) * (uint32_t)(L::kSlot >> 4));
+    auto logits = [&](uint32_t buf, uint32_t n_of, int half) {
+      const uint64_t kd = k_desc + (uint64_t)((n_of % NS) * (uint32_t)(L::kSlot >> 4) + (uint32_t)half * (KW * 8));
 #pragma unroll
       for (int k = 0; k < DH / 16; ++k) {
         const uint64_t off = (uint64_t)((k >> 2) * (int)kSlab16 + (k & 3) * 2);
-        tc_mma_bf16(d, q_desc + off, kd + off, idesc_s, k ? 1u : 0u);
+        tc_mma_bf16(s_tmem + buf * KW, q_desc + off, kd + off, idesc_s, k ? 1u : 0u);
       }
-    };
-    auto values = [&](uint32_t d, uint32_t p_addr, uint32_t n_of, uint32_t accumulate) {
-      const uint64_t vd = v_desc + (uint64_t)((n_of % NS) * (uint32_t)(L::kSlot >> 4));
-#pragma unroll
-      for (int k = 0; k < kTile / 16; ++k)
-        tc_mma_bf16_ts(d, p_addr + (uint32_t)k * 8u, vd + (uint64_t)(k * (2048 >> 4)), idesc_o, k ? 1u : accumulate);
+      tc_commit(b_s + 16 * qt + 8 * buf);
     };
     auto wait_slot = [&](uint32_t n_of) { return wait_warp(wt, b_full + 8 * (n_of % NS), (n_of / NS) & 1u); };
-    const uint32_t o_tmem = tmem + 256u + (uint32_t)qt * 128u;
     while (left > 0 && ok) {
-      const int t1 = min(p.nt, p.t + left), cnt = t1 - p.t;
-      left -= cnt;
-      ok = wait_warp(wt, b_q + 8 * qt, seg & 1u) && wait_slot(n);
-      if (!ok) break;
-      tc_fence_after();
-      if (elect_one()) {
-        const uint32_t buf = QT == 2 ? (uint32_t)qt : (it & 1u);
-        logits(tmem + buf * 128u, n);
-        tc_commit(b_s + 8 * buf);
-        if (QT == 1) tc_commit(b_empty + 8 * (n % NS));
+      const int t1 = min(p.nt, p.t + left), steps = (t1 - p.t) * SPT;
+      left -= t1 - p.t;
+      ok = wait_warp(wt, b_q + 8 * qt, seg & 1u);
+      for (int s = 0; s < min(2, steps) && ok; ++s) {          // two steps of logits ahead
+        if (s % SPT == 0 && !(ok = wait_slot(n + 2 * (s / SPT)))) break;
+        tc_fence_after();
+        if (elect_one()) logits((st + s) & 1u, n + 2 * (s / SPT), s % SPT);
+        __syncwarp();
       }
-      __syncwarp();
-      for (int t = 0; t < cnt; ++t, ++it, n += 2) {
-        const bool more = t + 1 < cnt;
-        if constexpr (QT == 2) {
-          // S lies where P did: its product follows the one that reads P.  One commit tells that this tile's values and the next
-          // one's logits are done; whoever waits for it gives their slots back.
-          if (!(ok = wait_slot(n + 1))) break;
-          if (more && !(ok = wait_slot(n + 2))) break;
-          if (!(ok = wait_warp(wt, b_p + 8 * qt, it & 1u))) break;
-          tc_fence_after();
-          if (elect_one()) {
-            values(o_tmem, tmem + (uint32_t)qt * 128u + 64u, n + 1, t ? 1u : 0u);
-            if (more) logits(tmem + (uint32_t)qt * 128u, n + 2);
-            tc_commit(more ? b_s + 8 * qt : b_o + 8 * qt);
-          }
-          __syncwarp();
-        } else {
-          // the next tile's logits go into the other buffer while this one's are worked on
-          const uint32_t buf = it & 1u;
-          if (more) {
-            if (!(ok = wait_slot(n + 2))) break;
-            if (elect_one()) {
-              logits(tmem + (buf ^ 1u) * 128u, n + 2);
-              tc_commit(b_s + 8 * (buf ^ 1u));
-              tc_commit(b_empty + 8 * ((n + 2) % NS));
-            }
-            __syncwarp();
-          }
-          if (!(ok = wait_slot(n + 1))) break;
-          if (!(ok = wait_warp(wt, b_p + 8 * buf, (it >> 1) & 1u))) break;
-          tc_fence_after();
-          if (elect_one()) {
-            values(o_tmem, tmem + buf * 128u + 64u, n + 1, t ? 1u : 0u);
-            tc_commit(b_o);
-            tc_commit(b_empty + 8 * ((n + 1) % NS));
-          }
-          __syncwarp();
+      for (int s = 0; s < steps && ok; ++s) {
+        const uint32_t buf = (st + s) & 1u, nv = n + 2 * (s / SPT) + 1, nk = n + 2 * ((s + 2) / SPT);
+        const bool more = s + 2 < steps;
+        if (s % SPT == 0 && !(ok = wait_slot(nv))) break;
+        if (more && s % SPT == 0 && !(ok = wait_slot(nk))) break;
+        if (!(ok = wait_warp(wt, b_p + 16 * qt + 8 * buf, ((st + s) >> 1) & 1u))) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t vd = v_desc + (uint64_t)((nv % NS) * (uint32_t)(L::kSlot >> 4) + (uint32_t)(s % SPT) * (KW * 8));
+#pragma unroll
+          for (int k = 0; k < KW / 16; ++k)
+            tc_mma_bf16_ts(o_tmem, s_tmem + buf * KW + KW / 2 + (uint32_t)k * 8u, vd + (uint64_t)(k * (2048 >> 4)), idesc_o, (s | k) ? 1u : 0u);
+          if (s % SPT == SPT - 1) tc_commit(b_empty + 8 * (nv % NS));
+          // the logits after the next follow the product that reads P, which lies where they go; their commit tells of both
+          if (more) logits(buf, nk, (s + 2) % SPT); else tc_commit(b_o + 16 * qt + 8 * (n_o & 1u));
         }
+        __syncwarp();
+        n_o += more ? 0u : 1u;
       }
+      st += steps;
+      n += 2 * (t1 - p.t);
       ++seg;
       if (left > 0 && ok) next_problem<QT>(a, p);
     }
   }
   } else {
-  if constexpr (QT == 2) regs_take<216>();
   if (left > 0) {
     const int qt = warp >> 2, row = tid & 127;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     uint8_t* q_gen = gen + qt * L::kSlot;
     const uint32_t o_addr = tmem + lane_base + 256u + (uint32_t)qt * 128u;
-    uint32_t it = 0, seg = 0;
+    uint32_t it = 0, st = 0, n_o = 0, seg = 0; // tiles, steps, commits on b_o and segments so far
     bool ok = true;
     while (left > 0 && ok) {
       const int t0 = p.t, t1 = min(p.nt, p.t + left);
@@ -416,7 +386,10 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       }
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(b_q + 8 * qt);
+      if (lane == 0) {
+        mbar_arrive(b_q + 8 * qt);
+        if (seg == 0) mbar_arrive(b_first);
+      }
       const int m = m0 + row;
       const bool live = m < rows_q;
       const bool warp_live = m0 + (row & ~31) < rows_q;
@@ -425,30 +398,28 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       float m_used = -INFINITY;
       u64 l2[2] = {0ull, 0ull};                // four partial sums of the weights
       bool odd = false;                        // tiles of this segment held drafts
-      for (int t = t0; t < t1; ++t, ++it) {
-        const uint32_t buf = QT == 2 ? (uint32_t)qt : (it & 1u);
-        if (!(ok = wait_warp(wt, b_s + 8 * buf, QT == 2 ? (it & 1u) : ((it >> 1) & 1u)))) break;
+      const int steps = (t1 - t0) * SPT;
+      for (int s = 0; s < steps; ++s, ++st) {
+        const int t = t0 + s / SPT, half = s % SPT;
+        const uint32_t buf = st & 1u, nk = 2u * (it + (uint32_t)(s / SPT));    // ring position of the tile's keys
+        if (!(ok = wait_warp(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
         tc_fence_after();
-        // The second warpgroup begins when the first one is done with its first tile: from then on one's exponentials run beside the
-        // other's products.
-        if (QT == 2 && qt == 1 && it == 0 && !(ok = wait_warp(wt, b_turn, 0u))) break;
-        if (QT == 2 && row == 0) {             // done with: this tile's keys, the values of the one before
-          mbar_arrive(b_empty + 8 * ((2u * it) % NS));
-          if (t > t0) mbar_arrive(b_empty + 8 * ((2u * it - 1u) % NS));
-        }
-        if (qt == 0 && t == t0 && row < 8) bad_s[(seg + 8) & 15u][row] = 0u;
-        const uint32_t s_addr = tmem + lane_base + buf * 128u;
-        const bool masked = (t + 1) * kTile > p.len;
+        if (half == SPT - 1 && row == 0) mbar_arrive(b_empty + 8 * (nk % NS));               // done with the tile's keys
+        if (qt == 0 && s == 0 && row < 8) bad_s[(seg + 8) & 15u][row] = 0u;
+        const uint32_t s_addr = tmem + lane_base + (uint32_t)qt * 128u + buf * KW;
+        const int j0 = t * kTile + half * KW;  // first row of the step
         if (warp_live) {
-          uint32_t z[4][32];
+          constexpr int NC = KW / 32;
+          const bool masked = j0 + KW > p.len;
+          uint32_t z[NC][32];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_ld32_nb(s_addr + 32u * i, z[i]);
+          for (int i = 0; i < NC; ++i) tmem_ld32_nb(s_addr + 32u * i, z[i]);
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < NC; ++i) {
             tc_wait_ld32_nb(z[i]);
             if (masked) {
-              const uint32_t w = row_bits(a, mask_row, token, t * kTile + 32 * i, p.len, p.drafts);
+              const uint32_t w = row_bits(a, mask_row, token, j0 + 32 * i, p.len, p.drafts);
 #pragma unroll
               for (int e = 0; e < 32; ++e) z[i][e] = (w >> e) & 1u ? z[i][e] : 0xff800000u;
             }
@@ -457,16 +428,15 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               mx[(e >> 1) & 3] = fmaxf(fmaxf(mx[(e >> 1) & 3], __uint_as_float(z[i][e])), __uint_as_float(z[i][e + 1]));
           }
           const float m_new = fmaxf(m_used, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale2);
-          if (t == t0) {
+          if (s == 0) {
             m_used = m_new;
           } else {
             const bool grow = m_new > m_used + kGrow || (m_used == -INFINITY && m_new > -INFINITY);
             if (__any_sync(0xffffffffu, grow)) {
-              // O holds the tiles before this one once their product is done (two warpgroups: it is, before these logits)
-              if (QT == 1) {
-                if (!(ok = wait_warp(wt, b_o, (it - 1u) & 1u))) break;
-                tc_fence_after();
-              }
+              // O holds the steps before this one once the last product is done, which the next logits' commit tells, or its own
+              const bool next = s + 1 < steps;
+              if (!(ok = wait_warp(wt, (next ? b_s + 8 * (buf ^ 1u) : b_o + 8 * (n_o & 1u)) + 16 * qt, ((next ? st + 1 : n_o) >> 1) & 1u))) break;
+              tc_fence_after();
               const float f = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
               if (grow) m_used = m_new;
               const u64 f2 = pack2(f, f);
@@ -487,7 +457,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           const float shift = m_used == -INFINITY ? 0.0f : m_used;
           const u64 scale_2 = pack2(a.scale2, a.scale2), shift_2 = pack2(-shift, -shift);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {        // P, two to a column, in the upper half of S's columns
+          for (int i = 0; i < NC; ++i) {       // P, two to a column, in the upper half of S's columns
             uint32_t r[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -497,15 +467,15 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               l2[e & 1] = add2(l2[e & 1], pack2(w.x, w.y));
               r[e] = pack_bf16(w.x, w.y);
             }
-            tmem_st16(s_addr + 64u + 16u * i, r);
+            tmem_st16(s_addr + KW / 2 + 16u * i, r);
           }
           tc_wait_st();
         }
-        if (masked) {
+        if (half == 0 && (t + 1) * kTile > p.len) {
           odd = true;
           // thread = value row: what no token holds is zeroed, what is not finite in a draft's row is taken out.  Both warpgroups do
           // it, to the same effect; one that finds a row cleared finds it listed, too.
-          const uint32_t nv = 2u * it + 1u, slot = nv % NS;
+          const uint32_t nv = nk + 1u, slot = nv % NS;
           if (!(ok = wait_warp(wt, b_full + 8 * slot, (nv / NS) & 1u))) break;
           const int draft = t * kTile + row - p.len;
           if (draft >= 0) {
@@ -534,14 +504,15 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(b_p + 8 * buf);
-        if (QT == 2 && qt == 0 && it == 0 && lane == 0) mbar_arrive(b_turn);
+        if (lane == 0) mbar_arrive(b_p + 16 * qt + 8 * buf);
       }
       if (!ok) break;
       // ---- the segment's result
-      if (!(ok = wait_warp(wt, b_o + 8 * qt, (QT == 2 ? seg : it - 1u) & 1u))) break;
+      // (the last two products commit to two barriers in turn: by now both may be done)
+      n_o += (uint32_t)min(2, steps);
+      if (!(ok = wait_warp(wt, b_o + 16 * qt + 8 * ((n_o - 1u) & 1u), ((n_o - 1u) >> 1) & 1u))) break;
+      it += (uint32_t)(t1 - t0);
       tc_fence_after();
-      if (QT == 2 && row == 0) mbar_arrive(b_empty + 8 * ((2u * it - 1u) % NS));
       const bool whole = t0 == 0 && t1 == p.nt;
       const float2 la = unpack2(add2(l2[0], l2[1]));
       const float l = la.x + la.y;
@@ -579,16 +550,16 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                                   pack_bf16(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
           } else if (!whole) {
             // through the place of this warp's rows of Q, so that a store writes whole lines
-            float4* st = reinterpret_cast<float4*>(q_gen + (warp & 3) * 4096);
+            float4* own = reinterpret_cast<float4*>(q_gen + (warp & 3) * 4096);
             __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) st[lane * 8 + (e ^ (lane & 7))] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 8; ++e) own[lane * 8 + (e ^ (lane & 7))] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
             __syncwarp();
             float* dst = a.part + (pr - row + (warp & 3) * 32) * DH + c + (lane & 7) * 4;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int r = 4 * i + (lane >> 3);
-              *reinterpret_cast<float4*>(dst + (size_t)r * DH) = st[r * 8 + ((lane & 7) ^ (r & 7))];
+              *reinterpret_cast<float4*>(dst + (size_t)r * DH) = own[r * 8 + ((lane & 7) ^ (r & 7))];
             }
           }
         }
