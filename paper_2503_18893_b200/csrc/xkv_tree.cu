@@ -312,6 +312,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         tc_mma_bf16(s_tmem + buf * KW, q_desc + off, kd + off, idesc_s, k ? 1u : 0u);
       }
       tc_commit(b_s + 16 * qt + 8 * buf);
+      if (half == SPT - 1) tc_commit(b_empty + 8 * (n_of % NS));
     };
     auto wait_slot = [&](uint32_t n_of) { return wait_warp(wt, b_full + 8 * (n_of % NS), (n_of / NS) & 1u); };
     while (left > 0 && ok) {
@@ -404,7 +405,6 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const uint32_t buf = st & 1u, nk = 2u * (it + (uint32_t)(s / SPT));    // ring position of the tile's keys
         if (!(ok = wait_warp(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
         tc_fence_after();
-        if (half == SPT - 1 && row == 0) mbar_arrive(b_empty + 8 * (nk % NS));               // done with the tile's keys
         if (qt == 0 && s == 0 && row < 8) bad_s[(seg + 8) & 15u][row] = 0u;
         const uint32_t s_addr = tmem + lane_base + (uint32_t)qt * 128u + buf * KW;
         const int j0 = t * kTile + half * KW;  // first row of the step

@@ -105,7 +105,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s, range_s[2];
   __shared__ Spot spot_s;
-  __shared__ __align__(16) float bias_s[kCols];               // lse log2(e) of a column; +inf: it adds nothing
+  __shared__ __align__(16) float bias_s[kCols];               // -lse log2(e) of a column; -inf: it adds nothing
   __shared__ int vis_s[kCols];                 // rows that a column's token saw
   __shared__ uint8_t list_s[8][kMaxTokens];    // every warp's own copy of the tokens that saw a row
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -119,9 +119,9 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
 
   if (tid == 0) {
     for (int i = 0; i < NS; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_free + 8 * i, 128); }
-    mbar_init(b_done, 256);
-    mbar_init(b_q, 256);
+    for (int i = 0; i < 2; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_free + 8 * i, 4); }     // (a warp arrives once)
+    mbar_init(b_done, 8);
+    mbar_init(b_q, 8);
     mbar_init(b_drain, 1);
     fence_mbar_init();
     abort_s = 0;
@@ -270,7 +270,8 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
       for (int c0 = 0; c0 < max(cols, 1) && ok; c0 += kCols, ++chunk) {
         const int nc = min(cols - c0, kCols), n16 = max(16, (nc + 15) & ~15);
         // both warpgroups are done with the columns before (and with them the tensor core is with their queries)
-        mbar_arrive(b_done);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_done);
         if (!(ok = wait_warp(wt, b_done, chunk & 1u))) break;
         for (int i = tid; i < n16 * (DH / 8); i += 256) {
           const int r = i / (DH / 8), c = i % (DH / 8);
@@ -282,19 +283,20 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
           *reinterpret_cast<uint4*>(q_gen + (c >> 3) * (kCols * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
         }
         if (tid < n16) {
-          float bias = INFINITY;
+          float bias = -INFINITY;
           int vis = 0;
           if (tid < nc) {
             const int at = (c0 + tid) / a.n_rep, h = c0 + tid - at * a.n_rep, tok = list[at];
             const float l = a.lse[(tok0 + tok) * a.H_q + (size_t)p.g * a.n_rep + h];
-            bias = l == -INFINITY ? INFINITY : l * kLog2e;
+            bias = l == -INFINITY ? -INFINITY : -l * kLog2e;
             vis = a.visible ? clamp_to(a.visible[(size_t)p.b * a.n_tok + tok], p.len, &bad) : p.len;
           }
           bias_s[tid] = bias;
           vis_s[tid] = vis;
         }
         fence_proxy_async();
-        mbar_arrive(b_q);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_q);
         if (!(ok = wait_warp(wt, b_q, chunk & 1u))) break;
         for (int t = t0; t < t1; ++t, ++it) {
           if ((int)(it & 1u) != wg) continue;
@@ -305,31 +307,50 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
           if (!(ok = wait_warp(wt, b_s + 8 * wg, (it >> 1) & 1u))) break;
           tc_fence_after();
           const bool all_see = (t + 1) * kTile <= least;       // every column's token saw every row of the tile
-          for (int g = 0; g < n16; g += 16) {
-            float z[16];
-            tmem_ld<16>(acc + (uint32_t)g, z);
+          // 32 columns at a time that every token saw, the next 32 on their way meanwhile
+          const int full = all_see ? nc >> 5 : 0;
+          if (full > 0) {
+            const u64 scale_2 = pack2(a.scale2, a.scale2);
+            u64 acc2[2] = {0ull, 0ull};
+            auto add32 = [&](const uint32_t (&z)[32], int g) {
+              const ulonglong2* bias = reinterpret_cast<const ulonglong2*>(bias_s + 32 * g);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const ulonglong2 bb = bias[e];
+                const float2 x = unpack2(fma2(pack2u(z[4 * e], z[4 * e + 1]), scale_2, bb.x));
+                const float2 y = unpack2(fma2(pack2u(z[4 * e + 2], z[4 * e + 3]), scale_2, bb.y));
+                acc2[0] = add2(acc2[0], pack2(ex2_approx(x.x), ex2_approx(x.y)));
+                acc2[1] = add2(acc2[1], pack2(ex2_approx(y.x), ex2_approx(y.y)));
+              }
+            };
+            uint32_t za[32], zb[32];
+            tmem_ld32_nb(acc, za);
+            for (int g = 0; g < full; g += 2) {
+              tc_wait_ld32_nb(za);
+              if (g + 1 < full) tmem_ld32_nb(acc + 32u * (g + 1), zb);
+              add32(za, g);
+              if (g + 1 < full) {
+                tc_wait_ld32_nb(zb);
+                if (g + 2 < full) tmem_ld32_nb(acc + 32u * (g + 2), za);
+                add32(zb, g + 1);
+              }
+            }
+            const float2 s2 = unpack2(add2(acc2[0], acc2[1]));
+            sum = s2.x + s2.y;
+          }
+          for (int g = 32 * full; g < nc; g += 8) {            // (columns behind the last have seen nothing)
+            float z[8];
+            tmem_ld<8>(acc + (uint32_t)g, z);
             tc_wait_ld();
-            if (all_see && g + 16 <= nc) {
-              float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-              for (int e = 0; e < 16; e += 4) {
-                const float4 bb = *reinterpret_cast<const float4*>(bias_s + g + e);
-                s0 += ex2_approx(fmaf(z[e], a.scale2, -bb.x));
-                s1 += ex2_approx(fmaf(z[e + 1], a.scale2, -bb.y));
-                s0 += ex2_approx(fmaf(z[e + 2], a.scale2, -bb.z));
-                s1 += ex2_approx(fmaf(z[e + 3], a.scale2, -bb.w));
-              }
-              sum += s0 + s1;
-            } else {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float x = ex2_approx(fmaf(z[e], a.scale2, -bias_s[g + e]));
-                sum += j < vis_s[g + e] ? x : 0.0f;
-              }
+            for (int e = 0; e < 8; ++e) {
+              const float x = ex2_approx(fmaf(z[e], a.scale2, bias_s[g + e]));
+              sum += j < vis_s[g + e] ? x : 0.0f;
             }
           }
           tc_fence_before();
-          mbar_arrive(b_free + 8 * wg);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_free + 8 * wg);
           if (j < p.len) w_head[j] = has_old ? fmaf(old, c0 ? 1.0f : a.decay, sum) : sum;
         }
       }
