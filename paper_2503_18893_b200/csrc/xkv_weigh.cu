@@ -3,14 +3,16 @@
 // The log-sum-exp is known, so a weight needs no maximum and no second pass: the cache's keys are read once.
 //
 // Rows of the cache are the rows of the tensor core's product and queries its columns, S[row][query] = K Q^T (tcgen05.mma,
-// M = 128 rows, N up to 256 queries of one KV head, in tensor memory): a thread then owns a row, adds up its columns in
+// M = 128 rows, N up to 128 queries of one KV head, in tensor memory): a thread then owns a row, adds up its columns in
 // registers and writes one weight, without a shuffle and in the same order in every call.  Only queries of tokens that saw a
-// row at all become columns.  More than 256 are taken 256 at a time, with another pass over the keys (there the exponentials
+// row at all become columns.  More than 128 are taken 128 at a time, with another pass over the keys (there the exponentials
 // bound the kernel, not the reads).
 //
 //   producer  TMA: K tiles through a ring of shared-memory slots
-//   issuer    tcgen05.mma into two accumulators in turn
-//   2 warpgroups, one for each accumulator: the exponentials and their sums
+//   issuer    tcgen05.mma into four accumulators in turn
+//   4 warpgroups, one for each accumulator: the exponentials and their sums.  The special-function unit takes 8 cycles for a
+//             warp's exponentials, one warp alone spends 10 and as long again on its loads and waits: four to a scheduler
+//             keep it fed (two, with accumulators of 256 columns: 224 us at 131072 rows, 32 tokens, four layers of eight heads).
 // As in the attention of drafted tokens, the tiles of all problems are one list in even pieces, one per CTA.
 #include <cuda.h>
 #include <math.h>
@@ -21,7 +23,8 @@ namespace xkv {
 
 namespace {
 
-constexpr int kCols = 256;                     // queries per pass over the keys
+constexpr int kCols = 128;                     // queries per pass over the keys, columns of an accumulator
+constexpr int kGroups = 4;                     // accumulators, and warpgroups that sum them up
 constexpr int kMaxTokens = XKV_TREE_MAX_DRAFT;
 
 struct WeighArgs {
@@ -87,11 +90,11 @@ template <int DH>
 struct WeighSmem {
   static constexpr int kSlab = kTile * 128;                    // 128 rows x 64 columns, 128-byte swizzle
   static constexpr int kSlot = kSlab * (DH / 64);
-  static constexpr int kSlots = DH == 128 ? 4 : 8;
+  static constexpr int kSlots = DH == 128 ? 5 : 8;
   static constexpr int kQ = kCols * DH * 2;
   static constexpr int kBytes = 1024 + kQ + kSlots * kSlot;
 };
-constexpr int kWeighThreads = 256 + 64;
+constexpr int kWeighThreads = kGroups * 128 + 64;
 
 template <int DH>
 __global__ void __launch_bounds__(kWeighThreads, 1)
@@ -101,27 +104,27 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
   constexpr int NS = L::kSlots;
   constexpr uint32_t kSlab16 = L::kSlab >> 4;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars_s[2 * NS + 7];
+  __shared__ uint64_t bars_s[2 * NS + 2 * kGroups + 3];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s, range_s[2];
   __shared__ Spot spot_s;
   __shared__ __align__(16) float bias_s[kCols];               // -lse log2(e) of a column; -inf: it adds nothing
   __shared__ int vis_s[kCols];                 // rows that a column's token saw
-  __shared__ uint8_t list_s[8][kMaxTokens];    // every warp's own copy of the tokens that saw a row
+  __shared__ uint8_t list_s[4 * kGroups][kMaxTokens];    // every warp's own copy of the tokens that saw a row
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* q_gen = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t ring = base + L::kQ;
   const uint32_t bars = smem_u32(bars_s);
-  const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_s = bars + 16 * NS, b_free = b_s + 16, b_done = b_free + 16, b_q = b_done + 8,
+  const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_s = bars + 16 * NS, b_free = b_s + 8 * kGroups, b_done = b_free + 8 * kGroups, b_q = b_done + 8,
                  b_drain = b_q + 8;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  constexpr int kProducer = 8, kIssuer = 9;
+  constexpr int kProducer = 4 * kGroups, kIssuer = kProducer + 1;
 
   if (tid == 0) {
     for (int i = 0; i < NS; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_free + 8 * i, 4); }     // (a warp arrives once)
-    mbar_init(b_done, 8);
-    mbar_init(b_q, 8);
+    for (int i = 0; i < kGroups; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_free + 8 * i, 4); }     // (a warp arrives once)
+    mbar_init(b_done, 4 * kGroups);
+    mbar_init(b_q, 4 * kGroups);
     mbar_init(b_drain, 1);
     fence_mbar_init();
     abort_s = 0;
@@ -233,15 +236,15 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
         if (!(ok = wait_warp(wt, b_q, chunk & 1u))) break;
         tc_fence_after();
         for (int t = 0; t < cnt; ++t, ++it) {
-          const uint32_t slot = it % NS, buf = it & 1u;
+          const uint32_t slot = it % NS, buf = it % kGroups;
           if (!(ok = wait_warp(wt, b_full + 8 * slot, (it / NS) & 1u))) break;
-          if (!(ok = wait_warp(wt, b_free + 8 * buf, ((it >> 1) & 1u) ^ 1u))) break;
+          if (!(ok = wait_warp(wt, b_free + 8 * buf, ((it / kGroups) & 1u) ^ 1u))) break;
           tc_fence_after();
           if (elect_one()) {
             const uint32_t ka = k_lo + slot * (uint32_t)(L::kSlot >> 4);
 #pragma unroll
             for (int k = 0; k < DH / 16; ++k)
-              tc_mma_bf16(tmem + buf * 256u, hi | (ka + (uint32_t)(k >> 2) * kSlab16 + (uint32_t)(k & 3) * 2u),
+              tc_mma_bf16(tmem + buf * kCols, hi | (ka + (uint32_t)(k >> 2) * kSlab16 + (uint32_t)(k & 3) * 2u),
                           hi | (q_lo + (uint32_t)(k >> 2) * (uint32_t)(kCols * 128 >> 4) + (uint32_t)(k & 3) * 2u), idesc, k ? 1u : 0u);
             tc_commit(b_s + 8 * buf);
             tc_commit(b_empty + 8 * slot);
@@ -252,7 +255,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
     }
   } else if (left > 0) {
     const int wg = warp >> 2, row = tid & 127;
-    const uint32_t acc = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)wg * 256u;
+    const uint32_t acc = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)wg * kCols;
     uint8_t* list = list_s[warp];
     uint32_t it = 0, chunk = 0;
     bool ok = true;
@@ -273,7 +276,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
         __syncwarp();
         if (lane == 0) mbar_arrive(b_done);
         if (!(ok = wait_warp(wt, b_done, chunk & 1u))) break;
-        for (int i = tid; i < n16 * (DH / 8); i += 256) {
+        for (int i = tid; i < n16 * (DH / 8); i += kGroups * 128) {
           const int r = i / (DH / 8), c = i % (DH / 8);
           uint4 v = make_uint4(0u, 0u, 0u, 0u);
           if (r < nc) {
@@ -299,20 +302,24 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
         if (lane == 0) mbar_arrive(b_q);
         if (!(ok = wait_warp(wt, b_q, chunk & 1u))) break;
         for (int t = t0; t < t1; ++t, ++it) {
-          if ((int)(it & 1u) != wg) continue;
+          if ((int)(it % kGroups) != wg) continue;
           const int j = t * kTile + row;
           float sum = 0.0f;
           const bool has_old = j < (c0 ? p.len : old_rows);
           const float old = has_old ? w_head[j] : 0.0f;        // (asked for before the wait)
-          if (!(ok = wait_warp(wt, b_s + 8 * wg, (it >> 1) & 1u))) break;
+          if (!(ok = wait_warp(wt, b_s + 8 * wg, (it / kGroups) & 1u))) break;
           tc_fence_after();
           const bool all_see = (t + 1) * kTile <= least;       // every column's token saw every row of the tile
-          // 32 columns at a time that every token saw, the next 32 on their way meanwhile
+          // 32 columns at a time that every token saw
           const int full = all_see ? nc >> 5 : 0;
           if (full > 0) {
             const u64 scale_2 = pack2(a.scale2, a.scale2);
             u64 acc2[2] = {0ull, 0ull};
-            auto add32 = [&](const uint32_t (&z)[32], int g) {
+#pragma unroll 1
+            for (int g = 0; g < full; ++g) {
+              uint32_t z[32];
+              tmem_ld32_nb(acc + 32u * g, z);
+              tc_wait_ld32_nb(z);
               const ulonglong2* bias = reinterpret_cast<const ulonglong2*>(bias_s + 32 * g);
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
@@ -321,18 +328,6 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
                 const float2 y = unpack2(fma2(pack2u(z[4 * e + 2], z[4 * e + 3]), scale_2, bb.y));
                 acc2[0] = add2(acc2[0], pack2(ex2_approx(x.x), ex2_approx(x.y)));
                 acc2[1] = add2(acc2[1], pack2(ex2_approx(y.x), ex2_approx(y.y)));
-              }
-            };
-            uint32_t za[32], zb[32];
-            tmem_ld32_nb(acc, za);
-            for (int g = 0; g < full; g += 2) {
-              tc_wait_ld32_nb(za);
-              if (g + 1 < full) tmem_ld32_nb(acc + 32u * (g + 1), zb);
-              add32(za, g);
-              if (g + 1 < full) {
-                tc_wait_ld32_nb(zb);
-                if (g + 2 < full) tmem_ld32_nb(acc + 32u * (g + 2), za);
-                add32(zb, g + 1);
               }
             }
             const float2 s2 = unpack2(add2(acc2[0], acc2[1]));
