@@ -56,8 +56,8 @@ __device__ __forceinline__ int token_of(const TreeArgs& a, int m) { return (int)
 
 // Rows and drafts of a sequence, brought into range; *bad reports what was not.
 __device__ __forceinline__ void tree_lengths(const TreeArgs& a, int b, int* len, int* drafts, bool* bad) {
-  const int want_dl = a.draft_len ? a.draft_len[b] : a.n_draft, dl = min(max(want_dl, 0), a.n_draft);
-  const int want_ln = a.len ? a.len[b] : a.cap - a.n_draft, ln = min(max(want_ln, 0), a.cap - dl);
+  const int want_dl = a.draft_len ? __ldcg(a.draft_len + b) : a.n_draft, dl = min(max(want_dl, 0), a.n_draft);
+  const int want_ln = a.len ? __ldcg(a.len + b) : a.cap - a.n_draft, ln = min(max(want_ln, 0), a.cap - dl);
   *len = ln;
   *drafts = dl;
   *bad = want_dl != dl || want_ln != ln;
@@ -602,19 +602,21 @@ tree_merge_kernel(const TreeArgs a, int attend_grid) {
   constexpr int V = DH / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int py = blockIdx.x, l = py / (a.batch * a.H_kv), b = (py / a.H_kv) % a.batch, g = py % a.H_kv;
-  ptx::grid_dependency_wait();                 // the pieces come from the kernel before
-  ptx::grid_dependency_launch();
+  // The lengths come from before the kernel that this one waits for, which had waited for them before it let this one start: they
+  // are read (past L1) while that kernel runs.
   const int m = blockIdx.y * kMergeWarps + warp;               // row of Q
   Place p;
   p.b = b;
   load_sequence<QT>(a, p);
-  if (m >= p.drafts * a.n_rep) return;
   int before;
   const int head = head_tiles<QT>(a, b, &before);
   const int total = head * a.H_kv * a.layers, ctas = tree_ctas(a, total, attend_grid);
   const int qp = m / (QT * kQRows);
   const int u0 = (l * head + before) * a.H_kv + (g * p.n_qp + qp) * p.nt, u1 = u0 + p.nt;
-  const int c0 = piece_of(total, ctas, u0), c1 = piece_of(total, ctas, u1 - 1);
+  const bool row = m < p.drafts * a.n_rep;     // (else there may be no tiles at all)
+  const int c0 = row ? piece_of(total, ctas, u0) : 0, c1 = row ? piece_of(total, ctas, u1 - 1) : 0;
+  ptx::grid_dependency_wait();                 // the pieces come from the kernel before; every CTA waits, so that who waits for this
+  ptx::grid_dependency_launch();               // kernel has waited for that one
   if (c0 == c1) return;                        // one piece: written where it was computed
   // a problem that begins inside a piece is that piece's last one, and in the others the first
   const size_t r = (size_t)(m - qp * QT * kQRows), first = (size_t)c0 * 2 + (piece_begin(total, ctas, c0) == u0 ? 0 : 1);
