@@ -595,75 +595,96 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   }
 }
 
-// Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A warp per query row, lane = d_h / 32 columns.
-template <int DH, int QT>
+// Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A warp has ROWS query rows, lane = d_h / 32 columns; a
+// step takes 8 / ROWS pieces of each, so eight loads of 512 bytes are in flight.
+template <int DH, int QT, int ROWS>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 tree_merge_kernel(const TreeArgs a, int attend_grid) {
-  constexpr int V = DH / 32;
+  constexpr int V = DH / 32, AT_ONCE = 8 / ROWS;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int py = blockIdx.x, l = py / (a.batch * a.H_kv), b = (py / a.H_kv) % a.batch, g = py % a.H_kv;
   // The lengths come from before the kernel that this one waits for, which had waited for them before it let this one start: they
   // are read (past L1) while that kernel runs.
-  const int m = blockIdx.y * kMergeWarps + warp;               // row of Q
+  const int m0 = (blockIdx.y * kMergeWarps + warp) * ROWS;     // first row of Q (32 rows of a CTA lie in one block of rows)
   Place p;
   p.b = b;
   load_sequence<QT>(a, p);
   int before;
   const int head = head_tiles<QT>(a, b, &before);
   const int total = head * a.H_kv * a.layers, ctas = tree_ctas(a, total, attend_grid);
-  const int qp = m / (QT * kQRows);
+  const int qp = m0 / (QT * kQRows), live = p.drafts * a.n_rep - m0;
   const int u0 = (l * head + before) * a.H_kv + (g * p.n_qp + qp) * p.nt, u1 = u0 + p.nt;
-  const bool row = m < p.drafts * a.n_rep;     // (else there may be no tiles at all)
-  const int c0 = row ? piece_of(total, ctas, u0) : 0, c1 = row ? piece_of(total, ctas, u1 - 1) : 0;
+  const int c0 = live > 0 ? piece_of(total, ctas, u0) : 0, c1 = live > 0 ? piece_of(total, ctas, u1 - 1) : 0;  // (else there may be no tiles)
   ptx::grid_dependency_wait();                 // the pieces come from the kernel before; every CTA waits, so that who waits for this
   ptx::grid_dependency_launch();               // kernel has waited for that one
   if (c0 == c1) return;                        // one piece: written where it was computed
   // a problem that begins inside a piece is that piece's last one, and in the others the first
-  const size_t r = (size_t)(m - qp * QT * kQRows), first = (size_t)c0 * 2 + (piece_begin(total, ctas, c0) == u0 ? 0 : 1);
-  auto slot = [&](int c) { return (c == c0 ? first : (size_t)c * 2) * (QT * kQRows) + r; };
-  float M = -INFINITY, acc[V], sum = 0.0f;
+  const size_t r0 = (size_t)(m0 - qp * QT * kQRows), first = (size_t)c0 * 2 + (piece_begin(total, ctas, c0) == u0 ? 0 : 1);
+  auto slot = [&](int c) { return (c == c0 ? first : (size_t)c * 2) * (QT * kQRows) + r0; };
+  float M[ROWS], sum[ROWS], acc[ROWS][V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-  for (int cb = c0; cb <= c1; cb += 32) {      // lane: the weight of one piece of 32
+  for (int k = 0; k < ROWS; ++k) {
+    M[k] = -INFINITY;
+    sum[k] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[k][i] = 0.0f;
+  }
+  for (int cb = c0; cb <= c1; cb += 32) {      // lane: the weight of one piece of 32, for every row
     const int n = min(32, c1 - cb + 1);
-    const float2 ml = lane < n ? a.part_ml[slot(cb + lane)] : make_float2(-INFINITY, 0.0f);
-    float top = ml.x;
+    float2 ml[ROWS];
+    float f[ROWS];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float M_new = fmaxf(M, top), old = M == -INFINITY ? 1.0f : exp2f(M - M_new);
-    const float f = ml.x == -INFINITY ? (ml.y == 0.0f ? 0.0f : 1.0f) : exp2f(ml.x - M_new);           // (a piece of NaNs stays one)
-    M = M_new;
-    float part = f * ml.y;
+    for (int k = 0; k < ROWS; ++k) ml[k] = lane < n && k < live ? a.part_ml[slot(cb + lane) + k] : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
-    sum = fmaf(sum, old, part);
+    for (int k = 0; k < ROWS; ++k) {
+      float top = ml[k].x;
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] *= old;
-    for (int j0 = 0; j0 < n; j0 += 8) {        // eight pieces' rows in flight
-      float x[8][V];
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float M_new = fmaxf(M[k], top), old = M[k] == -INFINITY ? 1.0f : exp2f(M[k] - M_new);
+      f[k] = ml[k].x == -INFINITY ? (ml[k].y == 0.0f ? 0.0f : 1.0f) : exp2f(ml[k].x - M_new);         // (a piece of NaNs stays one)
+      M[k] = M_new;
+      float part = f[k] * ml[k].y;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float* src = a.part + slot(cb + min(j0 + j, n - 1)) * DH + lane * V;
-        if constexpr (V == 4) *reinterpret_cast<float4*>(x[j]) = *reinterpret_cast<const float4*>(src);
-        else *reinterpret_cast<float2*>(x[j]) = *reinterpret_cast<const float2*>(src);
+      for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+      sum[k] = fmaf(sum[k], old, part);
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[k][i] *= old;
+    }
+    for (int j0 = 0; j0 < n; j0 += AT_ONCE) {
+      float x[AT_ONCE][ROWS][V];
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+          const float* src = a.part + (slot(cb + min(j0 + j, n - 1)) + min(k, live - 1)) * DH + lane * V;
+          if constexpr (V == 4) *reinterpret_cast<float4*>(x[j][k]) = *reinterpret_cast<const float4*>(src);
+          else *reinterpret_cast<float2*>(x[j][k]) = *reinterpret_cast<const float2*>(src);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float w = __shfl_sync(0xffffffffu, f, (j0 + j) & 31);
-        if (j0 + j < n) {
+      for (int j = 0; j < AT_ONCE; ++j) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) acc[i] = fmaf(w, x[j][i], acc[i]);
+        for (int k = 0; k < ROWS; ++k) {
+          const float w = __shfl_sync(0xffffffffu, f[k], (j0 + j) & 31);
+          if (j0 + j < n) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[k][i] = fmaf(w, x[j][k][i], acc[k][i]);
+          }
         }
       }
     }
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const int token = token_of(a, m);
-  const size_t qh = (((size_t)(a.l0 + l) * a.batch + b) * a.n_draft + token) * a.H_q + (size_t)g * a.n_rep + (m - token * a.n_rep);
-  uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + qh * DH + lane * V);
 #pragma unroll
-  for (int i = 0; i < V; i += 2) dst[i / 2] = ptx::pack_bf16(acc[i] * inv, acc[i + 1] * inv);
-  if (a.lse && lane == 0) a.lse[qh] = sum == 0.0f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
+  for (int k = 0; k < ROWS; ++k) {
+    if (k >= live) break;
+    const float inv = sum[k] == 0.0f ? 0.0f : 1.0f / sum[k];
+    const int m = m0 + k, token = token_of(a, m);
+    const size_t qh = (((size_t)(a.l0 + l) * a.batch + b) * a.n_draft + token) * a.H_q + (size_t)g * a.n_rep + (m - token * a.n_rep);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + qh * DH + lane * V);
+#pragma unroll
+    for (int i = 0; i < V; i += 2) dst[i / 2] = ptx::pack_bf16(acc[k][i] * inv, acc[k][i + 1] * inv);
+    if (a.lse && lane == 0) a.lse[qh] = sum[k] == 0.0f ? -INFINITY : (M[k] + log2f(sum[k])) * 0.6931471805599453f;
+  }
 }
 
 template <int DH, int QT>
@@ -671,9 +692,13 @@ cudaError_t launch_tree_as(const CUtensorMap& k_map, const CUtensorMap& v_map, c
   cudaError_t e = ensure_dyn_smem<tree_attend_kernel<DH, QT>>(TreeSmem<DH, QT>::kBytes, device);
   if (e == cudaSuccess) e = launch_pdl(tree_attend_kernel<DH, QT>, dim3(grid), dim3(tree_threads<QT>()), TreeSmem<DH, QT>::kBytes, s, k_map, v_map, a);
   if (e != cudaSuccess) return e;
-  const int rows = a.n_draft * a.n_rep;
-  e = launch_pdl(tree_merge_kernel<DH, QT>, dim3(a.layers * a.batch * a.H_kv, (rows + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, s,
-                 a, grid);
+  // Few rows are a matter of latency: a warp each.  Many are one of the CTAs that they take.
+  const int rows = a.n_draft * a.n_rep, problems = a.layers * a.batch * a.H_kv;
+  auto merge = [&](auto kernel, int per_warp) {
+    const int per_cta = kMergeWarps * per_warp;
+    return launch_pdl(kernel, dim3(problems, (rows + per_cta - 1) / per_cta), dim3(kMergeWarps * 32), 0, s, a, grid);
+  };
+  e = (long long)rows * problems <= 8192 ? merge(tree_merge_kernel<DH, QT, 1>, 1) : merge(tree_merge_kernel<DH, QT, 4>, 4);
   count_launch(kFamTree, 2);
   return e;
 }
