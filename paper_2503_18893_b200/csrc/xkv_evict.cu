@@ -470,18 +470,18 @@ static cudaError_t launch_select_as(const xkv_cache_config* c, int l0, int l1, i
 cudaError_t launch_evict_select(const xkv_cache_config* c, int l0, int l1, const float* weights, const int32_t* pos,
                                 const int32_t* since, const int32_t* len, int keep, int32_t* src, unsigned int* flags, int device,
                                 cudaStream_t s) {
-  // CTAs per head.  A CTA holds 1024 rows a round in its registers, up to 32 rounds, and is alone on its SM.  Measured: 6.5 us and
-  // 0.56 us a round for one CTA; 9 us and 0.8 us a round in a cluster, whose barriers cross SMs; 148 CTAs, 74 pairs, 32 clusters
-  // of four and 14 of eight run at once.  32 heads of 65500 rows: 35 us in pairs, 23 in fours, 48 in eights; 128 of them: 77, 96, 152;
-  // 32 of 4200 rows: 9.0 us alone, 10.6 in pairs.
+  // CTAs per head.  A CTA holds 1024 rows a round in its registers, up to 32 rounds, and is alone on its SM.  Measured: 7 us and
+  // 0.55 us a round for one CTA; 9.3 us and 0.8 us a round in a cluster, whose barriers cross SMs; and so many clusters of n at
+  // once.  32 heads of 65500 rows: 35 us in pairs, 23 in fours, 48 in eights; 128 of them: 77, 96, 152; 128 of up to 65539 rows, which
+  // two CTAs do not hold: 85 in threes, 104 in fours; 32 of 4200 rows: 9.0 us alone, 10.6 in pairs.
+  constexpr int kAtOnce[kSelMaxCluster] = {148, 74, 43, 32, 26, 21, 14, 14};
   const int heads = (l1 - l0) * c->batch * c->H_kv;
   int n_cta = 0, rounds = 0;
   float least = 0.0f;
-  for (int n = 1, at_once = 148; n <= kSelMaxCluster; n *= 2) {
-    const int r = (c->cap + n * kSelThreads - 1) / (n * kSelThreads);
-    const float cost = (float)((heads + at_once - 1) / at_once) * (n == 1 ? 6.5f + 0.56f * r : 9.0f + 0.8f * r);
+  for (int n = 1; n <= kSelMaxCluster; ++n) {
+    const int r = (c->cap + n * kSelThreads - 1) / (n * kSelThreads), waves = (heads + kAtOnce[n - 1] - 1) / kAtOnce[n - 1];
+    const float cost = (float)waves * (n == 1 ? 7.0f + 0.55f * (float)r : 9.3f + 0.8f * (float)r);
     if (r <= 32 && (n_cta == 0 || cost < least)) { n_cta = n; rounds = r; least = cost; }
-    at_once = n == 1 ? 74 : n == 2 ? 32 : 14;
   }
   const size_t smem = (size_t)rounds * kSelThreads * sizeof(int);
   if (rounds <= 8) return launch_select_as<8>(c, l0, l1, n_cta, smem, weights, pos, since, len, keep, src, flags, device, s);
