@@ -18,7 +18,8 @@ __device__ __forceinline__ void raise(unsigned int* flags, unsigned int bit) {
 
 // ---------------------------------------------------------------------------------------------
 // Commit.  A path may read a row that it also writes, so every row is in registers before the first store: a CTA takes 64
-// bytes of every row of one head's K or V, four lanes to a row.
+// bytes of every row of one head's K or V, four lanes to a row.  Bound by latency: four sequences, up to 8 of 64 drafts, four layers of
+// eight heads 3.2 us; eight sequences, up to 200 of 256 drafts (20.6 MB) 5.3 us.
 constexpr int kCommitThreads = 256;
 constexpr int kCommitRows = XKV_TREE_MAX_DRAFT / (kCommitThreads / 4);         // rows per thread
 
@@ -66,7 +67,8 @@ tree_commit_kernel(int batch, int H_kv, int cap, int l0, __nv_bfloat16* K, __nv_
 
 // ---------------------------------------------------------------------------------------------
 // Compaction.  Sources are at or behind `keep`, destinations before it, so rows move independently.  A CTA looks at 256
-// entries of a head's map, lists those that move, and copies their rows in 16-byte pieces, several in flight per thread.
+// entries of a head's map, lists those that move, and copies their rows in 16-byte pieces, several in flight per thread.  Bound by
+// HBM where many rows move: 65531 rows to 16384, four layers of eight heads (411 MB) 70 us, 5.9 TB/s; 4224 to 4096 2.4 us.
 constexpr int kCompactThreads = 256;
 
 template <int DH>
@@ -131,6 +133,9 @@ evict_compact_kernel(int cap, size_t head0, __nv_bfloat16* K, __nv_bfloat16* V, 
 // of 32 bins, then the bins of one of them, so that little crosses between SMs.  Rows with that very key stay in row order as
 // far as there is room.  Ranks in row order -- of ties, of holes, of the rows that fill them -- are ballots and a prefix sum
 // over (round, warp), so the map does not depend on timing.
+// Bound by latency (11 barriers of the CTA or the cluster) and, where heads take several waves of CTAs, by instructions, about 130 a
+// row and lane: 32 heads of 4224 rows 9.9 us, 128 heads of 32768 to 65536 rows 85 us (9.6 for their bytes).  With keys in shared
+// memory, all 2048 bins read from every CTA and a thread's rows side by side it took 16.7 and 304.
 constexpr int kSelThreads = 1024;
 constexpr int kSelBins = 2048;
 constexpr int kSelMaxCluster = 8;

@@ -8,12 +8,20 @@
 // are 256 multiplications for every byte read, where B200's HBM and its tensor cores take about as long.
 //
 //   producer  TMA: K and V tiles through one ring of shared-memory slots, across the borders of problems
-//   issuer    tcgen05.mma: S (both operands in shared memory), then O += P V with P in tensor memory, where it lies over S
+//   issuer    tcgen05.mma, a warp for each 128 rows of Q: S (both operands in shared memory) two steps ahead, and O += P V with
+//             P in tensor memory, where it lies over S
 //   softmax   a warpgroup for each 128 rows of Q: thread = row = TMEM lane, so a row's maximum and sum need no shuffle.
 //             O stays in tensor memory; it is rescaled only when a row's maximum has grown by more than 2^8 (a weight is then
 //             at most 2^8, which fp32 sums and bf16's relative precision do not notice).
-// Weights are rounded to bf16 for the tensor core (relative 2^-9, as the output's own rounding); the denominator sums them
-// unrounded in fp32.
+// Weights are rounded to bf16 for the tensor core (by half a step, relative 2^-8 at most, as the output is); the denominator
+// sums them unrounded in fp32.
+//
+// Up to 128 query rows a step is a tile of 128 cache rows; a CTA with 256 has the tensor memory for two steps of 64.  Measured on a
+// B200: 131072 rows, 64 query rows a head, four layers of eight heads 332-352 us, 6.1-6.5 TB/s (bound by HBM; 410 after a thousand
+// such calls in a row, at the power limit); eight sequences of up to 16411 rows, 231 query rows a head 231 us, 3.7 TB/s and 0.68
+// PFLOP/s of products (tensor cores 44 % busy, special-function units 35 %: bound by the hand-overs between the two, see the steps
+// that did not help: one step of 128 rows 245, exponentials in turns 256, two warpgroups per 128 rows in turns 256, the next
+// step's logits loaded part by part 240); 300 rows, one small window 9.9 us, of which the merge is 4 (latencies of two kernels).
 //
 // The tiles of all problems form one list that is cut into as many even pieces as there are CTAs, whatever the lengths of the
 // sequences: a CTA that holds a whole problem writes its output, the others leave (O, m, l) for tree_merge_kernel.  Lengths are
@@ -125,6 +133,7 @@ template <int QT>
 __device__ __forceinline__ int head_tiles(const TreeArgs& a, int b, int* before) {
   int all = 0;
   *before = 0;
+#pragma unroll 4
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     Place s;
     const int v = lane_tiles<QT>(a, b0, s, false);
@@ -141,6 +150,7 @@ __device__ __forceinline__ Place find_piece(const TreeArgs& a, int c, int grid, 
   Place s;                                     // of this lane's sequence
   const int mine = lane_tiles<QT>(a, 0, s, report);
   int upto = warp_prefix(mine), head = __shfl_sync(0xffffffffu, upto, 31);
+#pragma unroll 4
   for (int b0 = 32; b0 < a.batch; b0 += 32) {
     Place x;
     head += __reduce_add_sync(0xffffffffu, lane_tiles<QT>(a, b0, x, report));
@@ -267,7 +277,6 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   Place p = place_s;
   uint32_t n_loaded = 0;                       // producer: tiles (K and V each) asked for
 
-  if (warp >= QT * 4) {
   if (left > 0 && warp == kProducer) {
     if (lane == 0) {                           // (the others of the warp wait at its end)
       bool ok = true;
@@ -293,7 +302,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       }
     }
     __syncwarp();
-  } else if (left > 0 && warp < kIssuer + QT) {
+  } else if (left > 0 && warp >= kIssuer) {
     // ---- an issuing warp for each 128 rows of Q (a thread spends 70 to 130 cycles on an MMA and 235 on a commit).  Branches
     // outside the issue are taken on a vote and descriptors differ by constants, so that they stay in uniform registers.
     const int qt = warp - kIssuer;
@@ -349,9 +358,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       ++seg;
       if (left > 0 && ok) next_problem<QT>(a, p);
     }
-  }
-  } else {
-  if (left > 0) {
+  } else if (left > 0) {
     const int qt = warp >> 2, row = tid & 127;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     uint8_t* q_gen = gen + qt * L::kSlot;
@@ -572,7 +579,6 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     }
   }
 
-  }
   // wind down: nothing of this CTA may still touch shared or tensor memory
   tc_fence_before();
   __syncthreads();

@@ -14,6 +14,10 @@
 //             warp's exponentials, one warp alone spends 10 and as long again on its loads and waits: four to a scheduler
 //             keep it fed (two, with accumulators of 256 columns: 224 us at 131072 rows, 32 tokens, four layers of eight heads).
 // As in the attention of drafted tokens, the tiles of all problems are one list in even pieces, one per CTA.
+//
+// Measured on a B200, four layers of eight heads: 131072 rows, one token 170 us, 16 tokens 174 (6.5 and 6.4 TB/s: HBM), 32 tokens
+// 200 (5.5 TB/s; 537 M exponentials a call, for which the special-function units need 120 at the clock that the call runs at);
+// one layer of 8192 rows, one token 7.8 us, of which 3 are its bytes.
 #include <cuda.h>
 #include <math.h>
 
@@ -179,9 +183,9 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
       if (lane == 0) spot_s = p;
     }
     if (lane == 0) { range_s[0] = u0; range_s[1] = u1; }
-  } else if (warp == 0 && blockIdx.x == 0 && a.flags) {
+  } else if (warp == 0 && a.flags) {           // (every CTA looks at its share)
     bool bad = false;
-    for (int i = lane; i < a.batch * a.n_tok; i += 32) {
+    for (int i = blockIdx.x * 32 + lane; i < a.batch * a.n_tok; i += gridDim.x * 32) {
       const int b = i / a.n_tok, ln = weigh_length(a, b, &bad);
       if (a.visible) clamp_to(a.visible[i], ln, &bad);
       if (a.seen) clamp_to(a.seen[b], ln, &bad);
