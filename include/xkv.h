@@ -486,6 +486,16 @@ XKV_API int xkv_debug_set_fault_injection(xkv_group* grp, uint32_t mask);
 #define XKV_INJECT_CLF_BARRIER 4u
 #define XKV_INJECT_CLF_CHOLESKY 8u
 XKV_API int xkv_debug_set_clf_fault_injection(uint32_t mask);
+/*
+ * The same for xkv_tree_attend and xkv_cache_weigh, for every later call of the process until the mask is set back to 0; waits
+ * are shortened to two milliseconds, the call's flag word gets XKV_FLAG_TIMEOUT and its outputs are unspecified.
+ *   XKV_INJECT_CACHE_NO_LOAD      no tile is asked for.
+ *   XKV_INJECT_CACHE_NO_HANDOVER  tiles are loaded and multiplied, but no warp hands its results on: the kernel gives up while
+ *                                 copies of its own are outstanding.
+ */
+#define XKV_INJECT_CACHE_NO_LOAD 32u
+#define XKV_INJECT_CACHE_NO_HANDOVER 64u
+XKV_API int xkv_debug_set_cache_fault_injection(uint32_t mask);
 
 /*
  * Chunk selection for callers that must not allocate device memory.  (The paper has no counterpart: this is a

@@ -1,9 +1,14 @@
 // C entry points of the operators over an uncompressed cache: argument checking and dispatch.
 #include <math.h>
 
+#include <atomic>
+
 #include "xkv_internal.cuh"
 
 namespace xkv {
+
+static std::atomic<unsigned int> g_inject{0};
+unsigned int cache_fault_injection() { return g_inject.load(std::memory_order_relaxed); }
 
 namespace {
 
@@ -123,6 +128,12 @@ int xkv_evict_compact(const xkv_cache_config* cfg, int layer_begin, int layer_en
   if ((st = current_sm100_device(&device)) != XKV_OK) return st;
   return finish(launch_evict_compact(cfg, layer_begin, layer_end, (__nv_bfloat16*)K, (__nv_bfloat16*)V, src, keep, weights, pos, flags,
                                      (cudaStream_t)stream));
+}
+
+int xkv_debug_set_cache_fault_injection(uint32_t mask) {
+  if (mask & ~(XKV_INJECT_CACHE_NO_LOAD | XKV_INJECT_CACHE_NO_HANDOVER)) return XKV_ERR_INVALID_ARG;
+  g_inject.store(mask, std::memory_order_relaxed);
+  return XKV_OK;
 }
 
 }  // extern "C"

@@ -14,24 +14,26 @@ constexpr unsigned long long kCacheWaitNs = 250000000ull;      // a wait that la
 struct Wait {
   volatile int* abort;
   unsigned int* flags;
+  unsigned long long limit_ns;
 };
-static __device__ __forceinline__ bool wait_slow(volatile int* abort, unsigned int* flags, uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ unsigned long long wait_limit(unsigned int inject) { return inject ? 2000000ull : kCacheWaitNs; }
+static __device__ __forceinline__ bool wait_slow(const Wait& w, uint32_t bar, uint32_t parity) {
   unsigned long long t0, t;
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
   do {
     for (int i = 0; i < 64; ++i) {
       if (ptx::mbar_try_wait(bar, parity)) return true;
-      if (*abort) return false;
+      if (*w.abort) return false;
     }
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  } while (t - t0 < kCacheWaitNs);
-  *abort = 1;
-  if (flags) atomicOr(flags, XKV_FLAG_TIMEOUT);
+  } while (t - t0 < w.limit_ns);
+  *w.abort = 1;
+  if (w.flags) atomicOr(w.flags, XKV_FLAG_TIMEOUT);
   return false;
 }
 __device__ __forceinline__ bool wait_bar(const Wait& w, uint32_t bar, uint32_t parity) {
   if (ptx::mbar_try_wait(bar, parity)) return true;
-  return wait_slow(w.abort, w.flags, bar, parity);
+  return wait_slow(w, bar, parity);
 }
 // The same by a whole warp, with one answer for all its lanes.
 __device__ __forceinline__ bool wait_warp(const Wait& w, uint32_t bar, uint32_t parity) {

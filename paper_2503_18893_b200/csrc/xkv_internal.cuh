@@ -216,6 +216,9 @@ int clf_factorize(const xkv_clf_config* c, const void* X, const void* omega, voi
 cudaError_t clf_gemm(const void* a, const void* b, int M, int N, int K, float* C, unsigned int* flags, int device,
                      cudaStream_t s);
 
+// xkv_cache.cu
+unsigned int cache_fault_injection();
+
 // xkv_tree.cu
 size_t tree_part_floats(const xkv_cache_config* c, int n_draft);
 cudaError_t launch_tree_attend(const xkv_cache_config* c, int l0, int l1, const __nv_bfloat16* q, int n_draft, const uint32_t* mask,

@@ -57,6 +57,7 @@ struct TreeArgs {
   __nv_bfloat16* out;
   float* lse;
   unsigned int* flags;
+  unsigned int inject;                         // XKV_INJECT_CACHE_* bits; 0 in normal use
 };
 
 // m / n_rep for rows of Q: m < 4096, n_rep <= 16 and rep_inv = ceil(2^16 / n_rep), so the product's excess stays below one.
@@ -272,13 +273,13 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_s;
-  const Wait wt{&abort_s, a.flags};
+  const Wait wt{&abort_s, a.flags, wait_limit(a.inject)};
   int left = range_s[1] - range_s[0];
   Place p = place_s;
   uint32_t n_loaded = 0;                       // producer: tiles (K and V each) asked for
 
   if (left > 0 && warp == kProducer) {
-    if (lane == 0) {                           // (the others of the warp wait at its end)
+    if (lane == 0 && !(a.inject & XKV_INJECT_CACHE_NO_LOAD)) { // (the others of the warp wait at its end)
       bool ok = true;
       while (left > 0 && ok) {
         const int t1 = min(p.nt, p.t + left);
@@ -511,7 +512,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(b_p + 16 * qt + 8 * buf);
+        if (lane == 0 && !(a.inject & XKV_INJECT_CACHE_NO_HANDOVER)) mbar_arrive(b_p + 16 * qt + 8 * buf);
       }
       if (!ok) break;
       // ---- the segment's result
@@ -736,6 +737,7 @@ cudaError_t launch_tree_attend(const xkv_cache_config* c, int l0, int l1, const 
   a.rep_inv = (65536u + a.n_rep - 1u) / a.n_rep;
   a.scale2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / sqrtf((float)c->d_h)) * kLog2e;
   a.q = q; a.mask = mask; a.draft_len = draft_len; a.V = V; a.len = len; a.out = out; a.lse = lse; a.flags = flags;
+  a.inject = cache_fault_injection();
   const int rows_q = n_draft * a.n_rep, qt = rows_q > kQRows ? 2 : 1;
   const int grid = sms < kPlanSms ? sms : kPlanSms;
   a.part = workspace;

@@ -41,6 +41,7 @@ struct WeighArgs {
   const int32_t* seen;
   float* weights;
   unsigned int* flags;
+  unsigned int inject;                         // XKV_INJECT_CACHE_* bits; 0 in normal use
 };
 
 __device__ __forceinline__ int clamp_to(int v, int most, bool* bad) {
@@ -196,7 +197,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_s;
-  const Wait wt{&abort_s, a.flags};
+  const Wait wt{&abort_s, a.flags, wait_limit(a.inject)};
   int left = range_s[1] - range_s[0];
   Spot p = spot_s;
   uint32_t n_loaded = 0;                       // producer: tiles asked for
@@ -208,7 +209,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
       const int row0 = (((a.l0 + p.l) * a.batch + p.b) * a.H_kv + p.g) * a.cap;
       const int cols = seen_tokens(a, p.b, p.len, nullptr, nullptr) * a.n_rep;
       left -= t1 - p.t;
-      if (lane == 0) {
+      if (lane == 0 && !(a.inject & XKV_INJECT_CACHE_NO_LOAD)) {
         for (int c0 = 0; c0 < max(cols, 1) && ok; c0 += kCols) {
           for (int t = p.t; t < t1; ++t) {
             const uint32_t slot = n_loaded % NS;
@@ -349,7 +350,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(b_free + 8 * wg);
+          if (lane == 0 && !(a.inject & XKV_INJECT_CACHE_NO_HANDOVER)) mbar_arrive(b_free + 8 * wg);
           if (j < p.len) w_head[j] = has_old ? fmaf(old, c0 ? 1.0f : a.decay, sum) : sum;
         }
       }
@@ -390,6 +391,7 @@ cudaError_t launch_cache_weigh(const xkv_cache_config* c, int l0, int l1, const 
   a.l0 = l0; a.layers = l1 - l0;
   a.scale2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / sqrtf((float)c->d_h)) * kLog2e;
   a.decay = decay; a.q = q; a.lse = lse; a.len = len; a.visible = visible; a.seen = seen; a.weights = weights; a.flags = flags;
+  a.inject = cache_fault_injection();
   if (c->d_h == 128) {
     e = ensure_dyn_smem<cache_weigh_kernel<128>>(WeighSmem<128>::kBytes, device);
     if (e == cudaSuccess) e = launch_pdl(cache_weigh_kernel<128>, dim3(sms), dim3(kWeighThreads), WeighSmem<128>::kBytes, s, k_map, a);

@@ -425,6 +425,18 @@ _lib.xkv_evict_compact.argtypes = [_CFG, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P]
 _lib.xkv_evict_compact.restype = ctypes.c_int
 
 
+XKV_INJECT_CACHE_NO_LOAD = 32
+XKV_INJECT_CACHE_NO_HANDOVER = 64
+_lib.xkv_debug_set_cache_fault_injection.argtypes = [ctypes.c_uint32]
+_lib.xkv_debug_set_cache_fault_injection.restype = ctypes.c_int
+
+
+def xkv_debug_set_cache_fault_injection(mask: int) -> None:
+    st = _lib.xkv_debug_set_cache_fault_injection(mask)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_debug_set_cache_fault_injection")
+
+
 def make_cache_config(*, G, batch, H_kv, H_q, d_h, cap, softmax_scale=0.0) -> xkv_cache_config:
     """Sizes of an uncompressed cache K, V bf16 [G][batch][H_kv][cap][d_h] (include/xkv.h)."""
     return xkv_cache_config(ctypes.sizeof(xkv_cache_config), G, batch, H_kv, H_q, d_h, cap, softmax_scale)
