@@ -277,7 +277,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
       float* w_head = a.weights + (((size_t)(a.l0 + p.l) * a.batch + p.b) * a.H_kv + p.g) * (size_t)a.cap;
       for (int c0 = 0; c0 < max(cols, 1) && ok; c0 += kCols, ++chunk) {
         const int nc = min(cols - c0, kCols), n16 = max(16, (nc + 15) & ~15);
-        // both warpgroups are done with the columns before (and with them the tensor core is with their queries)
+        // all warpgroups are done with the columns before (and with them the tensor core is with their queries)
         __syncwarp();
         if (lane == 0) mbar_arrive(b_done);
         if (!(ok = wait_warp(wt, b_done, chunk & 1u))) break;
