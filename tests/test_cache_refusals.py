@@ -107,3 +107,11 @@ def test_workspace_bytes(xkv):
     for n in (0, 257):
         with pytest.raises(xkv.XKVError):
             xkv.xkv_tree_workspace_bytes(cfg, n)
+
+
+def test_fault_injection_masks(xkv):
+    for mask in (1, 16, 128, xkv.XKV_INJECT_CACHE_NO_LOAD | 2):
+        with pytest.raises(xkv.XKVError):
+            xkv.xkv_debug_set_cache_fault_injection(mask)
+    xkv.xkv_debug_set_cache_fault_injection(xkv.XKV_INJECT_CACHE_NO_LOAD | xkv.XKV_INJECT_CACHE_NO_HANDOVER)
+    xkv.xkv_debug_set_cache_fault_injection(0)
