@@ -571,6 +571,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
           }
         }
+        __syncwarp();                          // the next problem's queries go where other lanes may still be reading
         if (live && whole && a.lse) a.lse[qh] = l == 0.0f ? -INFINITY : (m_used + log2f(l)) * 0.6931471805599453f;
         if (live && !whole) a.part_ml[pr] = make_float2(m_used, l);
       }
