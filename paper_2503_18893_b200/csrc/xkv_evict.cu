@@ -12,6 +12,8 @@ namespace cg = cooperative_groups;
 
 namespace {
 
+// Every array may come from the kernel before, which may still be writing it while these kernels start (they wait for it, but the
+// read-only path is for memory that does not change while a kernel lives): no input is loaded as read-only, nor named as unaliased.
 __device__ __forceinline__ void raise(unsigned int* flags, unsigned int bit) {
   if (flags) atomicOr(flags, bit);
 }
@@ -25,9 +27,9 @@ constexpr int kCommitRows = XKV_TREE_MAX_DRAFT / (kCommitThreads / 4);         /
 
 template <int DH>
 __global__ void __launch_bounds__(kCommitThreads)
-tree_commit_kernel(int batch, int H_kv, int cap, int l0, __nv_bfloat16* K, __nv_bfloat16* V, const int32_t* __restrict__ len,
-                   const int32_t* __restrict__ path, const int32_t* __restrict__ path_len, int n_path, int32_t* pos,
-                   const int32_t* __restrict__ first_pos, unsigned int* flags) {
+tree_commit_kernel(int batch, int H_kv, int cap, int l0, __nv_bfloat16* K, __nv_bfloat16* V, const int32_t* len,
+                   const int32_t* path, const int32_t* path_len, int n_path, int32_t* pos,
+                   const int32_t* first_pos, unsigned int* flags) {
   const int py = blockIdx.x, b = (py / H_kv) % batch;
   const size_t head = ((size_t)l0 * batch * H_kv + py) * (size_t)cap;
   const int tid = threadIdx.x;
@@ -73,7 +75,7 @@ constexpr int kCompactThreads = 256;
 
 template <int DH>
 __global__ void __launch_bounds__(kCompactThreads)
-evict_compact_kernel(int cap, size_t head0, __nv_bfloat16* K, __nv_bfloat16* V, const int32_t* __restrict__ src, int keep,
+evict_compact_kernel(int cap, size_t head0, __nv_bfloat16* K, __nv_bfloat16* V, const int32_t* src, int keep,
                      float* weights, int32_t* pos, unsigned int* flags) {
   __shared__ int to_s[kCompactThreads], from_s[kCompactThreads], count_s;
   const int tid = threadIdx.x;
@@ -217,8 +219,8 @@ __device__ __forceinline__ void find_bin(cg::cluster_group& cl, SelShared& s, in
 
 template <int ITEMS>
 __global__ void __launch_bounds__(kSelThreads, 1)
-evict_select_kernel(int batch, int H_kv, int cap, int l0, const float* __restrict__ weights, const int32_t* __restrict__ pos,
-                    const int32_t* __restrict__ since, const int32_t* __restrict__ len, int keep, int32_t* __restrict__ src,
+evict_select_kernel(int batch, int H_kv, int cap, int l0, const float* weights, const int32_t* pos,
+                    const int32_t* since, const int32_t* len, int keep, int32_t* src,
                     unsigned int* flags) {
   extern __shared__ int list_s[];                        // rows at or behind `keep` that stay, ascending
   __shared__ __align__(16) SelShared s;
@@ -255,7 +257,7 @@ evict_select_kernel(int batch, int H_kv, int cap, int l0, const float* __restric
     for (int k0 = 0; k0 < ITEMS; k0 += U) {
       float w[U];
 #pragma unroll
-      for (int k = 0; k < U; ++k) w[k] = k0 + k < held ? __ldg(wp + (k0 + k) * kSelThreads) : 0.0f;
+      for (int k = 0; k < U; ++k) w[k] = k0 + k < held ? __ldcg(wp + (k0 + k) * kSelThreads) : 0.0f;
 #pragma unroll
       for (int k = 0; k < U; ++k) key[k0 + k] = k0 + k < held ? weight_key(w[k]) : kOut;
     }
@@ -266,7 +268,7 @@ evict_select_kernel(int batch, int H_kv, int cap, int l0, const float* __restric
       for (int k0 = 0; k0 < ITEMS; k0 += U) {
         int at[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) at[k] = pp && k0 + k < held ? __ldg(pp + (k0 + k) * kSelThreads) : r0 + (k0 + k) * kSelThreads;
+        for (int k = 0; k < U; ++k) at[k] = pp && k0 + k < held ? __ldcg(pp + (k0 + k) * kSelThreads) : r0 + (k0 + k) * kSelThreads;
 #pragma unroll
         for (int k = 0; k < U; ++k)
           if (k0 + k < held && at[k] >= since_b) recent |= 1u << (k0 + k);
