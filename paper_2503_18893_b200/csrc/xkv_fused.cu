@@ -421,7 +421,7 @@ __host__ __device__ constexpr int value_slots() {
 template <int DH, int NR, int WB, bool PROF, int QUANT, bool MMA>
 __global__ void __launch_bounds__(fused_threads(QUANT), 1)
 sr_fused_kernel(const __grid_constant__ CUtensorMap bk_map, GroupDev dev, Sched sc, const __nv_bfloat16* __restrict__ q,
-                const int32_t* __restrict__ sel_idx, const int32_t* __restrict__ sel_cnt) {
+                const int32_t* sel_idx, const int32_t* sel_cnt) {
   extern __shared__ uint8_t smem_raw[];
   constexpr int HALF = DH / 2;
   constexpr int kThreads = fused_threads(QUANT), PW = prod_warps(QUANT), SPT = PW * 16;   // SPT: producer threads per stream
@@ -645,8 +645,8 @@ sr_fused_kernel(const __grid_constant__ CUtensorMap bk_map, GroupDev dev, Sched 
       auto fetch = [&](int ks, int i) {
         const uint32_t at = gw[i] + quant_group(ks, q4, r);
         // 4 bits: 16 bytes of codes and a separate scale/offset word; 3 bits: one 16-byte record {meta, w0, w1, w2}
-        cw[i] = __ldg(Cb + at);
-        if (QUANT == 4) mw[i] = __ldg(Mb + at);
+        cw[i] = Cb[at];
+        if (QUANT == 4) mw[i] = Mb[at];
       };
 #pragma unroll
       for (int i = 0; i < QP; ++i) fetch(0, i);

@@ -86,7 +86,8 @@ __device__ __forceinline__ float2 rope_entry(const float4* __restrict__ row, int
 }
 
 // Launch with programmatic stream serialization: the kernel may begin while the previous kernel of the stream
-// drains; it must execute griddepcontrol.wait before it reads anything an earlier kernel may have written.
+// drains; it must execute griddepcontrol.wait before it reads anything an earlier kernel may have written, and must not load that as
+// read-only memory (__ldg, const __restrict__), which is defined only for what does not change while a kernel lives.
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args&&... args) {
   cudaLaunchConfig_t cfg = {};

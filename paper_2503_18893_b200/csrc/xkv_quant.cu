@@ -199,7 +199,7 @@ quantize_rtn_kernel(const uint4* __restrict__ x, long long n_pieces, uint32_t* _
 // x_hat: bf16(code * scale + zero) with a single rounding (the packed bf16 fused multiply-add rounds the exact value
 // once; small integers are exact in bf16).  One thread per 8 scalars, so that the 16-byte stores of a warp are contiguous.
 __global__ void __launch_bounds__(kQuantThreads)
-dequantize_rtn4_kernel(const uint32_t* __restrict__ codes, const uint32_t* __restrict__ meta, long long n_pieces,
+dequantize_rtn4_kernel(const uint32_t* codes, const uint32_t* meta, long long n_pieces,
                        uint4* __restrict__ x) {
   const long long first = (long long)blockIdx.x * (kQuantThreads * kQuantPieces) + threadIdx.x;
   ptx::grid_dependency_wait();
@@ -208,8 +208,8 @@ dequantize_rtn4_kernel(const uint32_t* __restrict__ codes, const uint32_t* __res
 #pragma unroll
   for (int u = 0; u < kQuantPieces; ++u) {
     const long long i = first + u * kQuantThreads;
-    w[u] = i < n_pieces ? __ldg(codes + i) : 0u;
-    m[u] = i < n_pieces ? __ldg(meta + (i >> 2)) : 0u;
+    w[u] = i < n_pieces ? codes[i] : 0u;
+    m[u] = i < n_pieces ? meta[i >> 2] : 0u;
   }
 #pragma unroll
   for (int u = 0; u < kQuantPieces; ++u) {
@@ -223,7 +223,7 @@ dequantize_rtn4_kernel(const uint32_t* __restrict__ codes, const uint32_t* __res
 // The 3-bit variant, one thread per 16-byte record; the 64 bytes of a group go through shared memory so that the
 // stores of a warp are contiguous (unit u of group g sits at g * 4 + (u ^ (g / 2 % 4)): no bank conflicts either way).
 __global__ void __launch_bounds__(kQuantThreads)
-dequantize_rtn3_kernel(const uint4* __restrict__ rec, long long n_groups, uint4* __restrict__ x) {
+dequantize_rtn3_kernel(const uint4* rec, long long n_groups, uint4* __restrict__ x) {
   __shared__ uint4 stage[kQuantThreads * 4];
   const int tid = threadIdx.x;
   const long long g0 = (long long)blockIdx.x * kQuantThreads;

@@ -462,7 +462,7 @@ tail_tc_kernel(GroupDev dev, int l0, const __nv_bfloat16* __restrict__ q, const 
 constexpr int kDenseMergeThreads = 1024;
 template <int DH>
 __global__ void __launch_bounds__(kDenseMergeThreads)
-dense_merge_kernel(GroupDev dev, int l0, const float* __restrict__ part, int n_split, __nv_bfloat16* __restrict__ out,
+dense_merge_kernel(GroupDev dev, int l0, const float* part, int n_split, __nv_bfloat16* __restrict__ out,
                    float* __restrict__ lse) {
   __shared__ float twgt_s[kTailMaxSplit];
   __shared__ float ML_s[2];
