@@ -72,22 +72,18 @@ __device__ __forceinline__ void next_spot(const WeighArgs& a, Spot& p) {
   } while (p.nt == 0 && p.l < a.layers);
 }
 
-// Tokens of sequence b that saw a row, by a whole warp: their number, their list (may be nullptr), the least that one saw.
-__device__ __forceinline__ int seen_tokens(const WeighArgs& a, int b, int len, uint8_t* list, int* least) {
+// Tokens of sequence b that saw a row, by a whole warp: their number, their list (may be nullptr).
+__device__ __forceinline__ int seen_tokens(const WeighArgs& a, int b, int len, uint8_t* list) {
   const int lane = threadIdx.x & 31;
-  int n = 0, lo = INT32_MAX;
+  int n = 0;
   for (int i0 = 0; i0 < a.n_tok; i0 += 32) {
     const int i = i0 + lane;
     bool bad = false;
     const int v = i < a.n_tok ? (a.visible ? clamp_to(a.visible[(size_t)b * a.n_tok + i], len, &bad) : len) : 0;
     const unsigned on = __ballot_sync(0xffffffffu, v > 0);
-    if (v > 0) {
-      lo = min(lo, v);
-      if (list) list[n + __popc(on & ((1u << lane) - 1u))] = (uint8_t)i;
-    }
+    if (v > 0 && list) list[n + __popc(on & ((1u << lane) - 1u))] = (uint8_t)i;
     n += __popc(on);
   }
-  if (least) *least = __reduce_min_sync(0xffffffffu, lo);
   return n;
 }
 
@@ -114,7 +110,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
   __shared__ int abort_s, range_s[2];
   __shared__ Spot spot_s;
   __shared__ __align__(16) float bias_s[kCols];               // -lse log2(e) of a column; -inf: it adds nothing
-  __shared__ int vis_s[kCols];                 // rows that a column's token saw
+  __shared__ int vis_s[kCols];                 // rows that a column's token saw; none where its log-sum-exp is -inf
   __shared__ uint8_t list_s[4 * kGroups][kMaxTokens];    // every warp's own copy of the tokens that saw a row
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* q_gen = smem_raw + (base - smem_u32(smem_raw));
@@ -207,7 +203,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
     while (left > 0 && ok) {
       const int t1 = min(p.nt, p.t + left);
       const int row0 = (((a.l0 + p.l) * a.batch + p.b) * a.H_kv + p.g) * a.cap;
-      const int cols = seen_tokens(a, p.b, p.len, nullptr, nullptr) * a.n_rep;
+      const int cols = seen_tokens(a, p.b, p.len, nullptr) * a.n_rep;
       left -= t1 - p.t;
       if (lane == 0 && !(a.inject & XKV_INJECT_CACHE_NO_LOAD)) {
         for (int c0 = 0; c0 < max(cols, 1) && ok; c0 += kCols) {
@@ -234,7 +230,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
     while (left > 0 && ok) {
       const int t1 = min(p.nt, p.t + left), cnt = t1 - p.t;
       left -= cnt;
-      const int cols = seen_tokens(a, p.b, p.len, nullptr, nullptr) * a.n_rep;
+      const int cols = seen_tokens(a, p.b, p.len, nullptr) * a.n_rep;
       for (int c0 = 0; c0 < max(cols, 1) && ok; c0 += kCols, ++chunk) {
         const int n16 = max(16, (min(cols - c0, kCols) + 15) & ~15);
         const uint32_t idesc = idesc_bf16_f32(128, 0) | ((uint32_t)(n16 >> 3) << 17);
@@ -268,8 +264,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
       const int t0 = p.t, t1 = min(p.nt, p.t + left);
       left -= t1 - t0;
       __syncwarp();
-      int least;
-      const int tokens = seen_tokens(a, p.b, p.len, list, &least), cols = tokens * a.n_rep;
+      const int tokens = seen_tokens(a, p.b, p.len, list), cols = tokens * a.n_rep;
       __syncwarp();
       bool bad = false;
       const int old_rows = a.decay == 0.0f ? 0 : a.seen ? clamp_to(a.seen[p.b], p.len, &bad) : p.len;
@@ -296,8 +291,11 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
           if (tid < nc) {
             const int at = (c0 + tid) / a.n_rep, h = c0 + tid - at * a.n_rep, tok = list[at];
             const float l = a.lse[(tok0 + tok) * a.H_q + (size_t)p.g * a.n_rep + h];
-            bias = l == -INFINITY ? -INFINITY : -l * kLog2e;
-            vis = a.visible ? clamp_to(a.visible[(size_t)p.b * a.n_tok + tok], p.len, &bad) : p.len;
+            // (a bias of -inf alone would not do: it makes a NaN of a logit that is not finite)
+            if (l != -INFINITY) {
+              bias = -l * kLog2e;
+              vis = a.visible ? clamp_to(a.visible[(size_t)p.b * a.n_tok + tok], p.len, &bad) : p.len;
+            }
           }
           bias_s[tid] = bias;
           vis_s[tid] = vis;
@@ -306,6 +304,9 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
         __syncwarp();
         if (lane == 0) mbar_arrive(b_q);
         if (!(ok = wait_warp(wt, b_q, chunk & 1u))) break;
+        int least = INT32_MAX;                                 // rows that every column saw
+        for (int i = lane; i < nc; i += 32) least = min(least, vis_s[i]);
+        least = __reduce_min_sync(0xffffffffu, least);
         for (int t = t0; t < t1; ++t, ++it) {
           if ((int)(it % kGroups) != wg) continue;
           const int j = t * kTile + row;
@@ -314,8 +315,8 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
           const float old = has_old ? w_head[j] : 0.0f;        // (asked for before the wait)
           if (!(ok = wait_warp(wt, b_s + 8 * wg, (it / kGroups) & 1u))) break;
           tc_fence_after();
-          const bool all_see = (t + 1) * kTile <= least;       // every column's token saw every row of the tile
-          // 32 columns at a time that every token saw
+          const bool all_see = (t + 1) * kTile <= least;       // every column saw every row of the tile
+          // 32 columns at a time
           const int full = all_see ? nc >> 5 : 0;
           if (full > 0) {
             const u64 scale_2 = pack2(a.scale2, a.scale2);
