@@ -264,7 +264,7 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     tmem_relinquish();
   }
   grid_dependency_wait();                      // everything below may come from the kernel before
-  grid_dependency_launch();
+  grid_dependency_launch();                    // (before this CTA is sure to hold tensor memory: the merge, which comes next, takes none)
   if (warp == kProducer) {
     const Place p = find_piece<QT>(a, blockIdx.x, gridDim.x, range_s, blockIdx.x == 0);
     if (lane == 0) place_s = p;

@@ -135,7 +135,6 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
     tmem_relinquish();
   }
   grid_dependency_wait();                      // everything below may come from the kernel before
-  grid_dependency_launch();
   if (warp == kProducer) {
     // the list: tiles of a head over the batch, and the place of this CTA's first
     int head = 0;
@@ -192,6 +191,9 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // Only now that this CTA holds its tensor memory: a kernel started earlier could take some on this SM while the allocation above
+  // still waits for another stream's, and then wait for this kernel, which waits for it.
+  grid_dependency_launch();
   const uint32_t tmem = tmem_s;
   const Wait wt{&abort_s, a.flags, wait_limit(a.inject)};
   int left = range_s[1] - range_s[0];
