@@ -283,7 +283,8 @@ XKV_API int xkv_dense_attend(xkv_group* grp, int layer_begin, int layer_end, con
  * No handle and no allocation: a call gets the cache's sizes in a host struct and everything else as device pointers.  What is
  * behind the last row of a sequence is neither read into a result nor written, whatever it holds.
  * flags  one device word or NULL: bits XKV_FLAG_INDEX_RANGE (a length or row index was out of range: lengths are clamped, rows
- *        skipped) and XKV_FLAG_TIMEOUT (a bounded wait ran out, outputs unspecified) are OR-ed in; the caller clears it.
+ *        skipped) and XKV_FLAG_TIMEOUT (a bounded wait ran out: outputs that were being worked on are NaN) are OR-ed in; the caller
+ *        clears it.  Without a flag word lengths are clamped and rows skipped in silence, and only the NaNs tell of a timeout.
  * Limits: d_h 64 or 128, H_q a multiple of H_kv with H_q/H_kv <= 16, 1 <= cap <= XKV_CACHE_MAX_ROWS,
  * G*batch*H_kv <= 65535, G*batch*H_kv*cap < 2^31 (else UNSUPPORTED).  Data pointers are 16-byte aligned, int32 and fp32 arrays 4-byte.
  * Layers layer_begin <= l < layer_end are worked on; arrays span all G layers.  Calls may run at the same time as long as they
@@ -488,7 +489,7 @@ XKV_API int xkv_debug_set_fault_injection(xkv_group* grp, uint32_t mask);
 XKV_API int xkv_debug_set_clf_fault_injection(uint32_t mask);
 /*
  * The same for xkv_tree_attend and xkv_cache_weigh, for every later call of the process until the mask is set back to 0; waits
- * are shortened to two milliseconds, the call's flag word gets XKV_FLAG_TIMEOUT and its outputs are unspecified.
+ * are shortened to two milliseconds, the call's flag word gets XKV_FLAG_TIMEOUT and outputs that were being worked on are NaN.
  *   XKV_INJECT_CACHE_NO_LOAD      no tile is asked for.
  *   XKV_INJECT_CACHE_NO_HANDOVER  tiles are loaded and multiplied, but no warp hands its results on: the kernel gives up while
  *                                 copies of its own are outstanding.

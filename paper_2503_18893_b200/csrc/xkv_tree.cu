@@ -221,6 +221,28 @@ struct TreeSmem {
 template <int QT>
 constexpr int tree_threads() { return QT * 128 + 32 + QT * 32; }
 
+// By a warp of a CTA that has given up: the results of its n tiles from place x on say so, also to a caller without a flag word.
+template <int DH, int QT>
+__device__ __forceinline__ void results_are_nan(const TreeArgs& a, Place x, int n) {
+  const float nan = __int_as_float(0x7fffffff);
+  for (uint32_t seg = 0; n > 0; ++seg) {
+    const int t1 = min(x.nt, x.t + n);
+    for (int row = threadIdx.x & 31; row < QT * kQRows; row += 32) {
+      const int m = x.qp * (QT * kQRows) + row, token = token_of(a, m);
+      if (m >= x.drafts * a.n_rep) break;
+      if (x.t == 0 && t1 == x.nt) {
+        const size_t qh = (((size_t)(a.l0 + x.l) * a.batch + x.b) * a.n_draft + token) * a.H_q + (size_t)x.g * a.n_rep + (m - token * a.n_rep);
+        for (int c = 0; c < DH; c += 8) *reinterpret_cast<uint4*>(a.out + qh * DH + c) = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (a.lse) a.lse[qh] = nan;
+      } else {                                 // (the merge makes it the whole problem's)
+        a.part_ml[((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * (QT * kQRows) + row] = make_float2(nan, nan);
+      }
+    }
+    n -= t1 - x.t;
+    if (n > 0) next_problem<QT>(a, x);
+  }
+}
+
 template <int DH, int QT>
 __global__ void __launch_bounds__(tree_threads<QT>(), 1)
 tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const TreeArgs a) {
@@ -596,10 +618,13 @@ tree_attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
-  if (abort_s && warp == kProducer && lane == 0) {
+  if (abort_s && warp == kProducer) {
     // given up: tiles may still be on their way into this CTA's shared memory; stay (with a limit) for them
-    for (uint32_t n = n_loaded > NS ? n_loaded - NS : 0u; n < n_loaded; ++n)
-      for (uint32_t i = 0; i < (1u << 16); ++i) if (mbar_try_wait(b_full + 8 * (n % NS), (n / NS) & 1u)) break;
+    if (lane == 0) {
+      for (uint32_t n = n_loaded > NS ? n_loaded - NS : 0u; n < n_loaded; ++n)
+        for (uint32_t i = 0; i < (1u << 16); ++i) if (mbar_try_wait(b_full + 8 * (n % NS), (n / NS) & 1u)) break;
+    }
+    results_are_nan<DH, QT>(a, place_s, range_s[1] - range_s[0]);
   }
 }
 

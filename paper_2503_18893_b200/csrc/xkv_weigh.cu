@@ -372,6 +372,16 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
     }
     tmem_dealloc(tmem, 512);
   }
+  if (abort_s) {                               // given up: this CTA's rows say so, also to a caller without a flag word
+    Spot x = spot_s;
+    for (int n = range_s[1] - range_s[0]; n > 0; ) {
+      const int t1 = min(x.nt, x.t + n);
+      float* w = a.weights + (((size_t)(a.l0 + x.l) * a.batch + x.b) * a.H_kv + x.g) * (size_t)a.cap;
+      for (int j = x.t * kTile + tid; j < min(t1 * kTile, x.len); j += kWeighThreads) w[j] = __int_as_float(0x7fffffff);
+      n -= t1 - x.t;
+      if (n > 0) next_spot(a, x);
+    }
+  }
   if (abort_s && warp == kProducer && lane == 0) {
     // given up: tiles may still be on their way into this CTA's shared memory; stay (with a limit) for them
     for (uint32_t n = n_loaded > NS ? n_loaded - NS : 0u; n < n_loaded; ++n)
