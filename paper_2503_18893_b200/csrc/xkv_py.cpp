@@ -10,6 +10,9 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
+#include <string>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Exceptions.h>
@@ -239,7 +242,7 @@ PyObject* dequantize_rtn(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// ---- operators over an uncompressed cache.  Their tensors are checked here for type, layout, size and device before any address
+// ---- operators over an uncompressed cache.  Their tensors are checked here for type, layout, shape and device before any address
 // reaches a kernel: the calls take many arrays whose shapes have to agree with one host struct.
 struct Checked : Args {
   const xkv_cache_config* cfg;
@@ -269,10 +272,30 @@ struct Checked : Args {
     }
     return t.get_device() == device;
   }
-  int64_t heads() const { return (int64_t)cfg->G * cfg->batch * cfg->H_kv; }
-  int64_t tokens(int64_t n) const { return (int64_t)cfg->G * cfg->batch * n * cfg->H_q; }
-  // at_least: the tensor may be larger (a workspace)
-  void* tensor(const char* name, at::ScalarType type, int64_t numel, bool optional = false, bool at_least = false) {
+  typedef std::initializer_list<int64_t> Dims;
+  static int64_t product(Dims dims) {
+    int64_t n = 1;
+    for (int64_t d : dims) n *= d;
+    return n;
+  }
+  // Do two shapes of as many elements name the same order of axes?  Axes of one may be joined or split in the other ([G * batch], or a
+  // KV head's query heads apart); where several axes of one are only together as long as several of the other, they are not the same.
+  static bool same_order(c10::IntArrayRef x, c10::IntArrayRef y) {
+    size_t i = x.size(), j = y.size();
+    while (i > 0 || j > 0) {
+      int64_t n = 1, m = 1;
+      int axes_x = 0, axes_y = 0;
+      do {
+        if (n <= m && i > 0) { axes_x += x[--i] != 1; n *= x[i]; }
+        else if (j > 0) { axes_y += y[--j] != 1; m *= y[j]; }
+        else return n == m;
+      } while (n != m);
+      if (axes_x > 1 && axes_y > 1) return false;
+    }
+    return true;
+  }
+  // at_least: the tensor may be larger, and of any shape (a workspace)
+  void* tensor(const char* name, at::ScalarType type, Dims dims, bool optional = false, bool at_least = false) {
     PyObject* o = next();
     if (!o) return nullptr;
     if (o == Py_None && optional) return nullptr;
@@ -282,14 +305,18 @@ struct Checked : Args {
       return nullptr;
     }
     const at::Tensor& t = THPVariable_Unpack(o);
+    const int64_t numel = product(dims);
     const char* what = nullptr;
     if (t.scalar_type() != type && !(type == at::kInt && t.scalar_type() == at::kUInt32)) what = "has another type";
-    else if (!on_device(t)) what = "is not on the current CUDA device";
     else if (!t.is_contiguous()) what = "is not contiguous";
     else if (at_least ? t.numel() < numel : t.numel() != numel) what = "has another number of elements";
+    else if (!at_least && numel > 0 && !same_order(t.sizes(), c10::IntArrayRef(dims))) what = "has its axes in another order";
+    else if (!on_device(t)) what = "is not on the current CUDA device";
     if (what) {
-      PyErr_Format(PyExc_ValueError, "%s: the tensor %s (of type %s, %lld elements%s expected)", name, what, c10::toString(type),
-                   (long long)numel, at_least ? " at least" : "");
+      std::string shape;
+      for (int64_t d : dims) shape += "[" + std::to_string(d) + "]";
+      PyErr_Format(PyExc_ValueError, "%s: the tensor %s (of type %s, %s%s expected)", name, what, c10::toString(type), shape.c_str(),
+                   at_least ? " elements at least" : "");
       bad = true;
       return nullptr;
     }
@@ -323,74 +350,69 @@ struct Checked : Args {
 
 XKV_CACHE_PY(tree_attend, 15)
   const int n = a.i32();
-  const int64_t rows = a.heads() * c->cap * c->d_h, queries = a.tokens(n);
-  void* q = a.tensor("q", at::kBFloat16, queries * c->d_h);
-  const uint32_t* mask = (const uint32_t*)a.tensor("mask", at::kInt, (int64_t)c->batch * n * (((int64_t)n + 31) / 32), true);
-  const int32_t* drafts = (const int32_t*)a.tensor("draft_len", at::kInt, c->batch, true);
-  void* K = a.tensor("K", at::kBFloat16, rows);
-  void* V = a.tensor("V", at::kBFloat16, rows);
-  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch, true);
+  void* q = a.tensor("q", at::kBFloat16, {c->G, c->batch, n, c->H_q, c->d_h});
+  const uint32_t* mask = (const uint32_t*)a.tensor("mask", at::kInt, {c->batch, n, ((int64_t)n + 31) / 32}, true);
+  const int32_t* drafts = (const int32_t*)a.tensor("draft_len", at::kInt, {c->batch}, true);
+  void* K = a.tensor("K", at::kBFloat16, {c->G, c->batch, c->H_kv, c->cap, c->d_h});
+  void* V = a.tensor("V", at::kBFloat16, {c->G, c->batch, c->H_kv, c->cap, c->d_h});
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, {c->batch}, true);
   if (a.bad) return nullptr;
   uint64_t need = 0;
   const int refused = xkv_tree_workspace_bytes(c, n, &need);
   if (refused != XKV_OK) return PyLong_FromLong(refused);
-  void* ws = a.tensor("workspace", at::kByte, (int64_t)need, false, true);
-  void* out = a.tensor("out", at::kBFloat16, queries * c->d_h);
-  float* lse = (float*)a.tensor("lse", at::kFloat, queries, true);
-  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  void* ws = a.tensor("workspace", at::kByte, {(int64_t)need}, false, true);
+  void* out = a.tensor("out", at::kBFloat16, {c->G, c->batch, n, c->H_q, c->d_h});
+  float* lse = (float*)a.tensor("lse", at::kFloat, {c->G, c->batch, n, c->H_q}, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
   void* s = a.stream();
 XKV_CACHE_PY_END(xkv_tree_attend(c, l0, l1, q, n, mask, drafts, K, V, len, ws, need, out, lse, flags, s))
 
 XKV_CACHE_PY(tree_commit, 13)
-  const int64_t rows = a.heads() * c->cap;
-  void* K = a.tensor("K", at::kBFloat16, rows * c->d_h);
-  void* V = a.tensor("V", at::kBFloat16, rows * c->d_h);
-  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch);
+  void* K = a.tensor("K", at::kBFloat16, {c->G, c->batch, c->H_kv, c->cap, c->d_h});
+  void* V = a.tensor("V", at::kBFloat16, {c->G, c->batch, c->H_kv, c->cap, c->d_h});
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, {c->batch});
   const int n = a.i32();
-  const int32_t* path = (const int32_t*)a.tensor("path", at::kInt, (int64_t)c->batch * n);
-  const int32_t* path_len = (const int32_t*)a.tensor("path_len", at::kInt, c->batch, true);
-  int32_t* pos = (int32_t*)a.tensor("pos", at::kInt, rows, true);
-  const int32_t* first = (const int32_t*)a.tensor("first_pos", at::kInt, c->batch, true);
-  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  const int32_t* path = (const int32_t*)a.tensor("path", at::kInt, {c->batch, n});
+  const int32_t* path_len = (const int32_t*)a.tensor("path_len", at::kInt, {c->batch}, true);
+  int32_t* pos = (int32_t*)a.tensor("pos", at::kInt, {c->G, c->batch, c->H_kv, c->cap}, true);
+  const int32_t* first = (const int32_t*)a.tensor("first_pos", at::kInt, {c->batch}, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
   void* s = a.stream();
 XKV_CACHE_PY_END(xkv_tree_commit(c, l0, l1, K, V, len, path, path_len, n, pos, first, flags, s))
 
 XKV_CACHE_PY(cache_weigh, 14)
   const int n = a.i32();
-  const int64_t rows = a.heads() * c->cap, queries = a.tokens(n);
-  void* q = a.tensor("q", at::kBFloat16, queries * c->d_h);
-  const float* lse = (const float*)a.tensor("lse", at::kFloat, queries);
-  void* K = a.tensor("K", at::kBFloat16, rows * c->d_h);
-  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch, true);
-  const int32_t* visible = (const int32_t*)a.tensor("visible", at::kInt, (int64_t)c->batch * n, true);
-  const int32_t* seen = (const int32_t*)a.tensor("seen", at::kInt, c->batch, true);
+  void* q = a.tensor("q", at::kBFloat16, {c->G, c->batch, n, c->H_q, c->d_h});
+  const float* lse = (const float*)a.tensor("lse", at::kFloat, {c->G, c->batch, n, c->H_q});
+  void* K = a.tensor("K", at::kBFloat16, {c->G, c->batch, c->H_kv, c->cap, c->d_h});
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, {c->batch}, true);
+  const int32_t* visible = (const int32_t*)a.tensor("visible", at::kInt, {c->batch, n}, true);
+  const int32_t* seen = (const int32_t*)a.tensor("seen", at::kInt, {c->batch}, true);
   const float decay = a.real();
-  float* weights = (float*)a.tensor("weights", at::kFloat, rows);
-  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  float* weights = (float*)a.tensor("weights", at::kFloat, {c->G, c->batch, c->H_kv, c->cap});
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
   void* s = a.stream();
 XKV_CACHE_PY_END(xkv_cache_weigh(c, l0, l1, q, n, lse, K, len, visible, seen, decay, weights, flags, s))
 
 XKV_CACHE_PY(evict_select, 11)
-  const int64_t rows = a.heads() * c->cap;
-  const float* weights = (const float*)a.tensor("weights", at::kFloat, rows);
-  const int32_t* pos = (const int32_t*)a.tensor("pos", at::kInt, rows, true);
-  const int32_t* since = (const int32_t*)a.tensor("since", at::kInt, c->batch, true);
-  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, c->batch, true);
+  const float* weights = (const float*)a.tensor("weights", at::kFloat, {c->G, c->batch, c->H_kv, c->cap});
+  const int32_t* pos = (const int32_t*)a.tensor("pos", at::kInt, {c->G, c->batch, c->H_kv, c->cap}, true);
+  const int32_t* since = (const int32_t*)a.tensor("since", at::kInt, {c->batch}, true);
+  const int32_t* len = (const int32_t*)a.tensor("length", at::kInt, {c->batch}, true);
   const int keep = a.i32();
-  int32_t* src = (int32_t*)a.tensor("src", at::kInt, a.heads() * keep);
-  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  int32_t* src = (int32_t*)a.tensor("src", at::kInt, {c->G, c->batch, c->H_kv, keep});
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
   void* s = a.stream();
 XKV_CACHE_PY_END(xkv_evict_select(c, l0, l1, weights, pos, since, len, keep, src, flags, s))
 
 XKV_CACHE_PY(evict_compact, 11)
-  const int64_t rows = a.heads() * c->cap;
-  void* K = a.tensor("K", at::kBFloat16, rows * c->d_h);
-  void* V = a.tensor("V", at::kBFloat16, rows * c->d_h);
+  void* K = a.tensor("K", at::kBFloat16, {c->G, c->batch, c->H_kv, c->cap, c->d_h});
+  void* V = a.tensor("V", at::kBFloat16, {c->G, c->batch, c->H_kv, c->cap, c->d_h});
   const int keep = a.i32();
-  const int32_t* src = (const int32_t*)a.tensor("src", at::kInt, a.heads() * keep);
-  float* weights = (float*)a.tensor("weights", at::kFloat, rows, true);
-  int32_t* pos = (int32_t*)a.tensor("pos", at::kInt, rows, true);
-  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, 1, true, true);
+  const int32_t* src = (const int32_t*)a.tensor("src", at::kInt, {c->G, c->batch, c->H_kv, keep});
+  float* weights = (float*)a.tensor("weights", at::kFloat, {c->G, c->batch, c->H_kv, c->cap}, true);
+  int32_t* pos = (int32_t*)a.tensor("pos", at::kInt, {c->G, c->batch, c->H_kv, c->cap}, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
   void* s = a.stream();
 XKV_CACHE_PY_END(xkv_evict_compact(c, l0, l1, K, V, src, keep, weights, pos, flags, s))
 

@@ -442,10 +442,10 @@ def make_cache_config(*, G, batch, H_kv, H_q, d_h, cap, softmax_scale=0.0) -> xk
     return xkv_cache_config(ctypes.sizeof(xkv_cache_config), G, batch, H_kv, H_q, d_h, cap, softmax_scale)
 
 
-# The calls below check their tensors (type, contiguity, number of elements, the current device) and raise ValueError or
-# TypeError for one that does not fit `cfg`, XKVError for sizes that the library refuses.  `flags`: None or an int32 device
-# tensor into which the kernels OR XKV_FLAG_* bits.  Without one lengths out of range are clamped in silence, and only NaNs in the
-# outputs tell of a wait that ran out.
+# The calls below check their tensors (type, contiguity, shape, the current device) and raise ValueError or TypeError for one that
+# does not fit `cfg` -- a shape is the documented one, also with axes joined or split, but not with axes in another order --, XKVError
+# for sizes that the library refuses.  `flags`: None or an int32 device tensor into which the kernels OR XKV_FLAG_* bits.  Without one
+# lengths out of range are clamped in silence, and only NaNs in the outputs tell of a wait that ran out.
 
 
 def xkv_tree_workspace_bytes(cfg: xkv_cache_config, n_draft: int) -> int:
