@@ -285,7 +285,7 @@ XKV_API int xkv_dense_attend(xkv_group* grp, int layer_begin, int layer_end, con
  * flags  one device word or NULL: bits XKV_FLAG_INDEX_RANGE (a length or row index was out of range: lengths are clamped, rows
  *        skipped) and XKV_FLAG_TIMEOUT (a bounded wait ran out: outputs that were being worked on are NaN) are OR-ed in; the caller
  *        clears it.  Without a flag word lengths are clamped and rows skipped in silence, and only the NaNs tell of a timeout.
- * Limits: d_h 64 or 128, H_q a multiple of H_kv with H_q/H_kv <= 16, 1 <= cap <= XKV_CACHE_MAX_ROWS,
+ * Limits: d_h 64 or 128, H_q a multiple of H_kv with H_q/H_kv <= 16, 1 <= cap <= XKV_CACHE_MAX_ROWS (else INVALID_ARG);
  * G*batch*H_kv <= 65535, G*batch*H_kv*cap < 2^31 (else UNSUPPORTED).  Data pointers are 16-byte aligned, int32 and fp32 arrays 4-byte.
  * Layers layer_begin <= l < layer_end are worked on; arrays span all G layers.  Calls may run at the same time as long as they
  * share no output and no workspace.

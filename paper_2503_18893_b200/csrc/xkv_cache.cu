@@ -18,7 +18,8 @@ int check_cache(const xkv_cache_config* c) {
   if (c->d_h != 64 && c->d_h != 128) return XKV_ERR_INVALID_ARG;
   if (c->cap < 1 || c->cap > XKV_CACHE_MAX_ROWS) return XKV_ERR_INVALID_ARG;
   if (!(c->softmax_scale >= 0.0f) || isinf(c->softmax_scale)) return XKV_ERR_INVALID_ARG;
-  // problems are a grid dimension, rows a 32-bit coordinate of the copy engine
+  // problems are a grid dimension, rows a 32-bit coordinate of the copy engine (and with at most 32 blocks of query rows for each of a
+  // head's tiles, lists of tiles are below 2^31 then, too)
   const double heads = (double)c->G * c->batch * c->H_kv;
   if (heads > 65535.0 || heads * c->cap >= 2147483648.0) return XKV_ERR_UNSUPPORTED;
   return XKV_OK;
@@ -33,12 +34,6 @@ int check_layers(const xkv_cache_config* c, int l0, int l1) {
 template <typename... P>
 bool aligned(unsigned to, const P*... p) {
   return ((... | (uintptr_t)p) & (to - 1u)) == 0;
-}
-
-// Lists of tiles are counted in 32 bits.
-int check_tiles(const xkv_cache_config* c, int n_tok) {
-  const double blocks = ceil((double)n_tok * (c->H_q / c->H_kv) / 128.0);
-  return (double)c->G * c->batch * c->H_kv * (c->cap / 128 + 1) * blocks >= 2147483648.0 ? XKV_ERR_UNSUPPORTED : XKV_OK;
 }
 
 int finish(cudaError_t e) {
@@ -74,7 +69,6 @@ int xkv_tree_attend(const xkv_cache_config* cfg, int layer_begin, int layer_end,
       !aligned(4, mask, draft_len, len, lse, flags))
     return XKV_ERR_INVALID_ARG;
   if (workspace_bytes < (uint64_t)tree_part_floats(cfg, n_draft) * sizeof(float)) return XKV_ERR_INVALID_ARG;
-  if ((st = check_tiles(cfg, n_draft)) != XKV_OK) return st;
   int device = 0;
   if ((st = current_sm100_device(&device)) != XKV_OK) return st;
   return finish(launch_tree_attend(cfg, layer_begin, layer_end, (const __nv_bfloat16*)q, n_draft, mask, draft_len, (const __nv_bfloat16*)K,
@@ -99,7 +93,6 @@ int xkv_cache_weigh(const xkv_cache_config* cfg, int layer_begin, int layer_end,
   if (st != XKV_OK) return st;
   if (!q || !lse || !K || !weights || n_tok < 1 || n_tok > XKV_TREE_MAX_DRAFT || !(decay >= 0.0f && decay <= 1.0f)) return XKV_ERR_INVALID_ARG;
   if (!aligned(16, (const char*)q, (const char*)K) || !aligned(4, lse, len, visible, seen, weights, flags)) return XKV_ERR_INVALID_ARG;
-  if ((st = check_tiles(cfg, 1)) != XKV_OK) return st;
   int device = 0;
   if ((st = current_sm100_device(&device)) != XKV_OK) return st;
   return finish(launch_cache_weigh(cfg, layer_begin, layer_end, (const __nv_bfloat16*)q, n_tok, lse, (const __nv_bfloat16*)K, len, visible,

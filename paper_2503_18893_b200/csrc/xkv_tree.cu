@@ -44,7 +44,7 @@ constexpr float kGrow = 8.0f;                  // log2 of the growth of a maximu
 constexpr int kMergeWarps = 8;
 
 struct TreeArgs {
-  int batch, H_kv, H_q, n_rep, cap, n_draft, words, l0, layers, min_tiles;
+  int batch, H_kv, H_q, n_rep, cap, n_draft, words, l0, layers;
   uint32_t rep_inv;                            // ceil(2^16 / n_rep)
   float scale2;                                // softmax scale times log2(e)
   const __nv_bfloat16* q;
@@ -99,11 +99,6 @@ __device__ __forceinline__ void next_problem(const TreeArgs& a, Place& p) {
   } while (p.nt == 0 && p.l < a.layers);
 }
 
-// CTAs that share `total` tiles.
-__device__ __forceinline__ int tree_ctas(const TreeArgs& a, int total, int grid) {
-  return max(1, min(grid, total / a.min_tiles));
-}
-
 // Inclusive prefix sum over a warp.
 __device__ __forceinline__ int warp_prefix(int v) {
 #pragma unroll
@@ -156,7 +151,7 @@ __device__ __forceinline__ Place find_piece(const TreeArgs& a, int c, int grid, 
     Place x;
     head += __reduce_add_sync(0xffffffffu, lane_tiles<QT>(a, b0, x, report));
   }
-  const int per_layer = head * a.H_kv, total = per_layer * a.layers, ctas = total > 0 ? tree_ctas(a, total, grid) : 0;
+  const int per_layer = head * a.H_kv, total = per_layer * a.layers, ctas = min(grid, total);
   int u0 = 0, u1 = 0;
   if (c < ctas) { u0 = piece_begin(total, ctas, c); u1 = piece_begin(total, ctas, c + 1); }
   if (lane == 0) { range[0] = u0; range[1] = u1; }
@@ -644,7 +639,7 @@ tree_merge_kernel(const TreeArgs a, int attend_grid) {
   load_sequence<QT>(a, p);
   int before;
   const int head = head_tiles<QT>(a, b, &before);
-  const int total = head * a.H_kv * a.layers, ctas = tree_ctas(a, total, attend_grid);
+  const int total = head * a.H_kv * a.layers, ctas = min(attend_grid, total);
   const int qp = m0 / (QT * kQRows), live = p.drafts * a.n_rep - m0;
   const int u0 = (l * head + before) * a.H_kv + (g * p.n_qp + qp) * p.nt, u1 = u0 + p.nt;
   const int c0 = live > 0 ? piece_of(total, ctas, u0) : 0, c1 = live > 0 ? piece_of(total, ctas, u1 - 1) : 0;  // (else there may be no tiles)
@@ -759,7 +754,7 @@ cudaError_t launch_tree_attend(const xkv_cache_config* c, int l0, int l1, const 
   if (e != cudaSuccess) return e;
   TreeArgs a;
   a.batch = c->batch; a.H_kv = c->H_kv; a.H_q = c->H_q; a.n_rep = c->H_q / c->H_kv; a.cap = c->cap; a.n_draft = n_draft;
-  a.words = (n_draft + 31) / 32; a.l0 = l0; a.layers = l1 - l0; a.min_tiles = 1;
+  a.words = (n_draft + 31) / 32; a.l0 = l0; a.layers = l1 - l0;
   a.rep_inv = (65536u + a.n_rep - 1u) / a.n_rep;
   a.scale2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / sqrtf((float)c->d_h)) * kLog2e;
   a.q = q; a.mask = mask; a.draft_len = draft_len; a.V = V; a.len = len; a.out = out; a.lse = lse; a.flags = flags;
