@@ -723,13 +723,15 @@ cudaError_t launch_tree_as(const CUtensorMap& k_map, const CUtensorMap& v_map, c
   cudaError_t e = ensure_dyn_smem<tree_attend_kernel<DH, QT>>(TreeSmem<DH, QT>::kBytes, device);
   if (e == cudaSuccess) e = launch_pdl(tree_attend_kernel<DH, QT>, dim3(grid), dim3(tree_threads<QT>()), TreeSmem<DH, QT>::kBytes, s, k_map, v_map, a);
   if (e != cudaSuccess) return e;
-  // Few rows are a matter of latency: a warp each.  Many are one of the CTAs that they take.
+  // Few rows are a matter of latency: a warp each.  Many are one of the CTAs that they take: four a warp.  Whole calls, one and four rows
+  // a warp: 2048 rows 33.3 and 38.3 us (64 drafts over one layer of 8192), 18.3 and 19.6; 2560 36.6 and 37.8, 25.7 and 25.6; 3584 42.5
+  // and 42.3, 29.0 and 27.5; 4096 46.4 and 45.9; 8192 69.7 and 62.2, 44.3 and 37.1; 24576 113 and 88.6.
   const int rows = a.n_draft * a.n_rep, problems = a.layers * a.batch * a.H_kv;
   auto merge = [&](auto kernel, int per_warp) {
     const int per_cta = kMergeWarps * per_warp;
     return launch_pdl(kernel, dim3(problems, (rows + per_cta - 1) / per_cta), dim3(kMergeWarps * 32), 0, s, a, grid);
   };
-  e = (long long)rows * problems <= 8192 ? merge(tree_merge_kernel<DH, QT, 1>, 1) : merge(tree_merge_kernel<DH, QT, 4>, 4);
+  e = (long long)rows * problems <= 3500 ? merge(tree_merge_kernel<DH, QT, 1>, 1) : merge(tree_merge_kernel<DH, QT, 4>, 4);
   count_launch(kFamTree, 2);
   return e;
 }
