@@ -21,7 +21,7 @@ __device__ __forceinline__ void raise(unsigned int* flags, unsigned int bit) {
 // ---------------------------------------------------------------------------------------------
 // Commit.  A path may read a row that it also writes, so every row is in registers before the first store: a CTA takes 64
 // bytes of every row of one head's K or V, four lanes to a row.  Bound by latency: four sequences, up to 8 of 64 drafts, four layers of
-// eight heads 3.2 us; eight sequences, up to 200 of 256 drafts (20.6 MB) 5.3 us.
+// eight heads 2.9 us; eight sequences, up to 200 of 256 drafts (20.6 MB) 5.1 us.
 constexpr int kCommitThreads = 256;
 constexpr int kCommitRows = XKV_TREE_MAX_DRAFT / (kCommitThreads / 4);         // rows per thread
 
@@ -70,7 +70,7 @@ tree_commit_kernel(int batch, int H_kv, int cap, int l0, __nv_bfloat16* K, __nv_
 // ---------------------------------------------------------------------------------------------
 // Compaction.  Sources are at or behind `keep`, destinations before it, so rows move independently.  A CTA looks at 256
 // entries of a head's map, lists those that move, and copies their rows in 16-byte pieces, several in flight per thread.  Bound by
-// HBM where many rows move: 65531 rows to 16384, four layers of eight heads (411 MB) 70 us, 5.9 TB/s; 4224 to 4096 2.4 us.
+// HBM where many rows move: 65531 rows to 16384, four layers of eight heads (411 MB) 70 us, 5.9 TB/s; 4224 to 4096 2.4 us in a graph of such calls, 3.3 to 3.6 called one by one.
 constexpr int kCompactThreads = 256;
 
 template <int DH>
@@ -136,8 +136,9 @@ evict_compact_kernel(int cap, size_t head0, __nv_bfloat16* K, __nv_bfloat16* V, 
 // far as there is room.  Ranks in row order -- of ties, of holes, of the rows that fill them -- are ballots and a prefix sum
 // over (round, warp), so the map does not depend on timing.
 // Bound by latency (11 barriers of the CTA or the cluster) and, where heads take several waves of CTAs, by instructions, about 130 a
-// row and lane: 32 heads of 4224 rows 9.9 us, 128 heads of 32768 to 65536 rows 85 us (9.6 for their bytes).  With keys in shared
-// memory, all 2048 bins read from every CTA and a thread's rows side by side it took 16.7 and 304.
+// row and lane: 32 heads of 4224 rows 9.8 us, 128 heads of 32768 to 65536 rows 85 us (9.6 for their bytes).  With keys in shared
+// memory, all 2048 bins read from every CTA and a thread's rows side by side it took 16.7 and 304.  (Not all keys stay in registers
+// through the first digit's loads: 32 rounds spill 132 bytes a thread, 16 rounds 8.)
 constexpr int kSelThreads = 1024;
 constexpr int kSelBins = 2048;
 constexpr int kSelMaxCluster = 8;
@@ -480,7 +481,8 @@ cudaError_t launch_evict_select(const xkv_cache_config* c, int l0, int l1, const
   // CTAs per head.  A CTA holds 1024 rows a round in its registers, up to 32 rounds, and is alone on its SM.  Measured: 7 us and
   // 0.55 us a round for one CTA; 9.3 us and 0.8 us a round in a cluster, whose barriers cross SMs; and so many clusters of n at
   // once.  32 heads of 65500 rows: 35 us in pairs, 23 in fours, 48 in eights; 128 of them: 77, 96, 152; 128 of up to 65539 rows, which
-  // two CTAs do not hold: 85 in threes, 104 in fours; 32 of 4200 rows: 9.0 us alone, 10.6 in pairs.
+  // two CTAs do not hold: 85 in threes, 104 in fours; 32 of 4200 rows: 9.0 us alone, 10.6 in pairs.  The rule goes by the cache's room,
+  // since lengths are on the device: 128 heads half to quite full take 63 with room for 65536 rows each and 85 with room for 65537.
   constexpr int kAtOnce[kSelMaxCluster] = {148, 74, 43, 32, 26, 21, 14, 14};
   const int heads = (l1 - l0) * c->batch * c->H_kv;
   int n_cta = 0, rounds = 0;

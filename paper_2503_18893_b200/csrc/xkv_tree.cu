@@ -4,24 +4,28 @@
 // token i attends to where bit j of its mask is set.  For one (layer, sequence, KV head) the queries of all tokens and of the
 // head's n_rep query heads are the rows of one matrix Q, row token * n_rep + head, and
 //   S = scale Q K^T,   p = exp2(S log2(e) - m),   O += p V,   l += sum p
-// runs over 128-row tiles of the cache with a running maximum m.  The cache is read once for up to 256 rows of Q: 256 rows
-// are 256 multiplications for every byte read, where B200's HBM and its tensor cores take about as long.
+// runs over 128-row tiles of the cache with a running maximum m.  The cache is read once for up to 256 rows of Q: with 256
+// an element of two bytes meets 256 multiply-adds, 256 flops a byte, where B200's tensor cores (1651 TFLOP/s) and its HBM (6548 GB/s,
+// 252 flops a byte) take about as long.
 //
 //   producer  TMA: K and V tiles through one ring of shared-memory slots, across the borders of problems
 //   issuer    tcgen05.mma, a warp for each 128 rows of Q: S (both operands in shared memory) two steps ahead, and O += P V with
 //             P in tensor memory, where it lies over S
 //   softmax   a warpgroup for each 128 rows of Q: thread = row = TMEM lane, so a row's maximum and sum need no shuffle.
 //             O stays in tensor memory; it is rescaled only when a row's maximum has grown by more than 2^8 (a weight is then
-//             at most 2^8, which fp32 sums and bf16's relative precision do not notice).
+//             at most 2^8, which fp32 sums and bf16's relative precision do not notice; a published technique for such kernels).
 // Weights are rounded to bf16 for the tensor core (by half a step, relative 2^-8 at most, as the output is); the denominator
 // sums them unrounded in fp32.
 //
-// Up to 128 query rows a step is a tile of 128 cache rows; a CTA with 256 has the tensor memory for two steps of 64.  Measured on a
-// B200: 131072 rows, 64 query rows a head, four layers of eight heads 332-352 us, 6.1-6.5 TB/s (bound by HBM; 410 after a thousand
-// such calls in a row, at the power limit); eight sequences of up to 16411 rows, 231 query rows a head 231 us, 3.7 TB/s and 0.68
-// PFLOP/s of products (tensor cores 44 % busy, special-function units 35 %: bound by the hand-overs between the two, see the steps
-// that did not help: one step of 128 rows 245, exponentials in turns 256, two warpgroups per 128 rows in turns 256, the next
-// step's logits loaded part by part 240); 300 rows, one small window 9.9 us, of which the merge is 4 (latencies of two kernels).
+// Up to 128 query rows a step is a tile of 128 cache rows; a CTA with 256 has the tensor memory for two steps of 64.  Measured on
+// B200s, the first 50 ms of calls (in brackets: after a second of them, at the power limit): 131072 rows, 64 query rows a head, four
+// layers of eight heads 320-344 us (375-410), 6.2-6.7 TB/s: HBM.  Eight sequences of up to 16411 rows, 231 query rows a head 227-234
+// (268-275), 3.7 TB/s and 0.69 PFLOP/s of products (tensor cores 46 % busy, special-function units 37 %: bound by the hand-overs between
+// the two, see the steps that did not help: one step of 128 rows 245, exponentials in turns 256, two warpgroups per 128 rows in turns
+// 256, the next step's logits loaded part by part 240).  One layer of 8192 rows, 256 query rows a head 33.5, by time stamps of a CTA:
+// start and place 2.2, queries 3.3, first logits 0.8, four tiles 9.7 (14 in the slowest CTA), last product and partial result 2.8, a
+// second problem in four CTAs 2-5, to the merge 1.4, merge 5.2.  300 rows, one small window 10-10.6: place 1.0, queries 1.6, logits 0.6,
+// weights 1.9, product 0.5, result 0.8, to the merge 1.1, merge 2.5: latencies of two kernels.
 //
 // The tiles of all problems form one list that is cut into as many even pieces as there are CTAs, whatever the lengths of the
 // sequences: a CTA that holds a whole problem writes its output, the others leave (O, m, l) for tree_merge_kernel.  Lengths are

@@ -1,23 +1,26 @@
 // Accumulated attention weights of the rows of an uncompressed cache (xkv_cache_weigh):
 //   w[j] = (j < seen ? decay w[j] : 0) + sum over queries c that saw row j of exp2(scale log2(e) k_j . q_c - lse_c log2(e)).
-// The log-sum-exp is known, so a weight needs no maximum and no second pass: the cache's keys are read once.
+// The log-sum-exp is known, so a weight needs no maximum: the cache's keys are read once for up to 128 queries of a KV head.
 //
 // Rows of the cache are the rows of the tensor core's product and queries its columns, S[row][query] = K Q^T (tcgen05.mma,
 // M = 128 rows, N up to 128 queries of one KV head, in tensor memory): a thread then owns a row, adds up its columns in
 // registers and writes one weight, without a shuffle and in the same order in every call.  Only queries of tokens that saw a
-// row at all become columns.  More than 128 are taken 128 at a time, with another pass over the keys (there the exponentials
-// bound the kernel, not the reads).
+// row at all become columns.  More than 128 are taken 128 at a time, each with another pass over the keys of a CTA's tiles, which
+// comes from HBM again where those of all CTAs do not fit L2: 131072 rows, four layers of eight heads, 128 queries 198 us, 132 337
+// (two reads of the keys are 330), 192 354, 256 390, 260 526.
 //
 //   producer  TMA: K tiles through a ring of shared-memory slots
 //   issuer    tcgen05.mma into four accumulators in turn
 //   4 warpgroups, one for each accumulator: the exponentials and their sums.  The special-function unit takes 8 cycles for a
 //             warp's exponentials, one warp alone spends 10 and as long again on its loads and waits: four to a scheduler
 //             keep it fed (two, with accumulators of 256 columns: 224 us at 131072 rows, 32 tokens, four layers of eight heads).
-// As in the attention of drafted tokens, the tiles of all problems are one list in even pieces, one per CTA.
+// As in the attention of drafted tokens, the tiles of all problems are one list in even pieces, one per CTA.  Exponentials are the
+// hardware's (relative error 2^-22): a weight is off by 0.8e-7 to 6e-7 of itself against 64 bits, with exp() by 0.4e-7 to 2.3e-7.
 //
-// Measured on a B200, four layers of eight heads: 131072 rows, one token 170 us, 16 tokens 174 (6.5 and 6.4 TB/s: HBM), 32 tokens
-// 200 (5.5 TB/s; 537 M exponentials a call, for which the special-function units need 120 at the clock that the call runs at);
-// one layer of 8192 rows, one token 7.8 us, of which 3 are its bytes.
+// Measured on a B200, four layers of eight heads, the first 50 ms of calls: 131072 rows, one token 170 us, 16 tokens 174 (6.5 and
+// 6.4 TB/s: HBM), 32 tokens 198-204 (5.5 TB/s; 537 M exponentials a call, for which the special-function units need 120 at the clock
+// that the call runs at; 227-239 after a second of such calls, at the power limit); one layer of 8192 rows, one token 7.8 us, of
+// which 3 are its bytes.
 #include <cuda.h>
 #include <math.h>
 
@@ -109,7 +112,7 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap k_map, const WeighArgs a)
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s, range_s[2];
   __shared__ Spot spot_s;
-  __shared__ __align__(16) float bias_s[kCols];               // -lse log2(e) of a column; -inf: it adds nothing
+  __shared__ __align__(16) float bias_s[kCols];               // -lse log2(e) of a column
   __shared__ int vis_s[kCols];                 // rows that a column's token saw; none where its log-sum-exp is -inf
   __shared__ uint8_t list_s[4 * kGroups][kMaxTokens];    // every warp's own copy of the tokens that saw a row
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
