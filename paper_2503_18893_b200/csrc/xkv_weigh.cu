@@ -15,7 +15,7 @@
 //             warp's exponentials, one warp alone spends 10 and as long again on its loads and waits: four to a scheduler
 //             keep it fed (two, with accumulators of 256 columns: 224 us at 131072 rows, 32 tokens, four layers of eight heads).
 // As in the attention of drafted tokens, the tiles of all problems are one list in even pieces, one per CTA.  Exponentials are the
-// hardware's (relative error 2^-22): a weight is off by 0.8e-7 to 6e-7 of itself against 64 bits, with exp() by 0.4e-7 to 2.3e-7.
+// hardware's (relative error 2^-22): a weight is off by 0.3e-7 to 6e-7 of itself against 64 bits, with exp() by 0.2e-7 to 2.3e-7.
 //
 // Measured on a B200, four layers of eight heads, the first 50 ms of calls: 131072 rows, one token 170 us, 16 tokens 174 (6.5 and
 // 6.4 TB/s: HBM), 32 tokens 198-204 (5.5 TB/s; 537 M exponentials a call, for which the special-function units need 120 at the clock
