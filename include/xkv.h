@@ -383,6 +383,180 @@ XKV_API int xkv_evict_compact(const xkv_cache_config* cfg, int layer_begin, int 
                               int32_t keep, float* weights, int32_t* pos, uint32_t* flags, void* stream);
 
 /*
+ * Rotary positions as an operator of its own: queries and keys of a step before they meet a cache, the queries that xkv_sr_select and
+ * the attention calls take rotated, keys of a rotated cache turned back before xkv_clf_factorize and xkv_build_landmarks (which want
+ * them as they were), and the gradient of a rotation.
+ * Pair i of the first `rot` elements of a head is (x_i, x_i+rot/2) in the half layout and (x_2i, x_2i+1) in the interleaved one; at
+ * position p it is turned by the angle p f_i and multiplied by `gain`.  Elements from rot on are copied.
+ *   f_i = base^(-2i/rot), then by `scaling`:
+ *     NONE    f_i
+ *     LINEAR  f_i / factor
+ *     NTK     base replaced by base * factor^(rot/(rot-2))
+ *     LLAMA3  f_i where its wave 2 pi / f_i is shorter than original/high, f_i / factor where it is longer than original/low, and
+ *             (1-s) f_i / factor + s f_i between, s = (original f_i / (2 pi) - low) / (high - low)
+ *     YARN    r_i f_i / factor + (1-r_i) f_i, r_i = (i - lo) / (hi - lo) cut to 0 .. 1 (hi - lo at least 0.001), lo and hi the pairs whose
+ *             waves make beta_fast and beta_slow turns in `original` positions, rot ln(original / (2 pi beta)) / (2 ln base), rounded down
+ *             and up and cut to 0 .. rot-1; gain 0.1 ln(factor) + 1
+ *   gain is 1 but for YARN; a config's gain > 0 takes its place.
+ * xkv_rope_plan_init (host only) makes the plan that calls take: turns per position as 64-bit fractions, so that an angle is exact to
+ * 2^-33 of a turn up to position 2^31.  A plan is plain host memory and is copied at the call.
+ */
+#define XKV_ROPE_MAX_ROT 256
+#define XKV_ROPE_HALF 0
+#define XKV_ROPE_INTERLEAVED 1
+#define XKV_ROPE_SCALE_NONE 0
+#define XKV_ROPE_SCALE_LINEAR 1
+#define XKV_ROPE_SCALE_NTK 2
+#define XKV_ROPE_SCALE_LLAMA3 3
+#define XKV_ROPE_SCALE_YARN 4
+typedef struct {
+  uint32_t struct_size;        /* sizeof(xkv_rope_config) */
+  int32_t d_h;                 /* elements of a head, even, 2 .. 1024 */
+  int32_t rot;                 /* how many of them are rotated, even, 2 .. min(d_h, XKV_ROPE_MAX_ROT) (4 at least with NTK) */
+  int32_t layout, scaling;
+  double base, factor;         /* base > 1 (YARN) or > 0; factor > 0 */
+  double original;             /* LLAMA3, YARN: positions of the context that the model was trained on, > 0 */
+  double low, high;            /* LLAMA3: high > low > 0 */
+  double beta_fast, beta_slow; /* YARN: > 0 */
+  double gain;                 /* 0: the scaling's own */
+} xkv_rope_config;
+typedef struct {
+  uint32_t struct_size;        /* sizeof(xkv_rope_plan) */
+  int32_t d_h, rot, layout;
+  float gain;
+  uint32_t reserved;
+  uint64_t turns[XKV_ROPE_MAX_ROT / 2];  /* 2^64 f_i / (2 pi), modulo 2^64 */
+} xkv_rope_plan;
+XKV_API int xkv_rope_plan_init(const xkv_rope_config* cfg, xkv_rope_plan* plan);
+
+/*
+ * Rotates the heads of one or two tensors (a step's queries and its keys) by the same positions.
+ * direction  FORWARD: by p f_i, times gain.  ADJOINT: by -p f_i, times gain: the gradient of FORWARD.  INVERSE: by -p f_i, divided by
+ *            gain: undoes FORWARD.
+ * type       of all tensors of the call; arithmetic is fp32, rounded once.
+ * tensors    n_tensors = 1 or 2 (host array): x and y device pointers [rows][heads][d_h], elements of a head side by side, the distances
+ *            of rows and of heads in elements (parts of a fused projection's output, say).  y may be x (in place); they must not
+ *            overlap in another way.  Pointers aligned to the type's size.  heads >= 0; a tensor without heads does nothing.
+ * rows       >= 0; row r has position pos[r % n_pos]: layers of a window that are rotated together share positions.
+ * pos        int32 [n_pos], device, any values; n_pos >= 1 divides rows.
+ * Errors: INVALID_ARG, UNSUPPORTED (rows * heads of a tensor 2^31 or more), ARCH, CUDA.
+ */
+#define XKV_ROPE_FORWARD 0
+#define XKV_ROPE_ADJOINT 1
+#define XKV_ROPE_INVERSE 2
+#define XKV_BF16 0
+#define XKV_FP16 1
+#define XKV_FP32 2
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t x_row, x_head, y_row, y_head;  /* distances in elements */
+  int32_t heads;
+} xkv_rope_tensor;
+XKV_API int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const xkv_rope_tensor* tensors, int n_tensors, int64_t rows,
+                     const int32_t* pos, int64_t n_pos, void* stream);
+
+/*
+ * A paged cache of 8-bit codes.  The rows of a sequence lie in pages of `page` rows, the same pages in all G layers: row j of sequence b
+ * is row j % page of page table[b][j / page].
+ *   K8, V8            e4m3 codes [G][n_pages][H_kv][page][d_h]; keys as the model stores them (rotated)
+ *   k_scale, v_scale  fp32 [G][n_pages][H_kv]: powers of two; a code c of the page and head stands for the value c * scale
+ *   table             int32 [batch][max_pages]
+ * A scale that is a power of two costs e4m3 nothing but range: codes are the values' own roundings to 4 significant bits (half a
+ * step, 2^-4 of the value, down to 2^-15 of the page's largest).
+ *   xkv_page_assign    lengths of sequences that grow and shrink -> pages, places of new tokens
+ *   xkv_cache8_append  new keys and values into their places
+ *   xkv_cache8_read    rows back as an uncompressed cache (for xkv_dense_attend, xkv_tree_attend, xkv_clf_factorize)
+ *   xkv_cache8_attend  attention of each sequence's last tokens over its rows
+ * New tokens of a step lie behind one another, sequence by sequence: those of sequence b from first[b] to first[b+1] - 1 of n_tok.
+ * No handle and no allocation.  flags as for the uncompressed cache: one device word or NULL.  A page number outside [0, n_pages), a
+ * length or a slot out of range is not followed: what it names is skipped, XKV_FLAG_INDEX_RANGE is raised.
+ * Limits: d_h 64 or 128, H_q a multiple of H_kv with H_q/H_kv <= 16, page 16, 32, 64 or 128, max_pages * page <= XKV_CACHE_MAX_ROWS
+ * (else INVALID_ARG); G*batch*H_kv <= 65535, G*n_pages*H_kv*page < 2^31, G*n_tok*H_q < 2^31 (else UNSUPPORTED).  K8, V8, q, k, v, K, V, out
+ * and workspaces are 16-byte aligned, int32 and fp32 arrays 4-byte.  Layers layer_begin <= l < layer_end are worked on; arrays span all
+ * G.  Calls may run at the same time as long as none writes what another reads or writes.
+ * Errors of all of them: INVALID_ARG, UNSUPPORTED, ARCH, CUDA.
+ */
+typedef struct {
+  uint32_t struct_size; /* sizeof(xkv_cache8_config) */
+  int32_t G, batch, H_kv, H_q, d_h;
+  int32_t page;         /* rows of a page */
+  int32_t n_pages;      /* pages of the cache */
+  int32_t max_pages;    /* entries of a sequence in the table */
+  float softmax_scale;  /* logit scale; 0 means 1/sqrt(d_h) */
+} xkv_cache8_config;
+
+/*
+ * Pages for sequences that go from held[b] to want[b] rows (0 <= both <= max_pages * page; others are clamped, flag).
+ * A sequence that grows takes the pages that it lacks, ceil(want/page) - ceil(held/page), from the front of the ring of free pages, in
+ * the order of sequences, all or none: one that lacks pages when the sequences up to it want more than there are gets none, and keeps
+ * held[b] rows.  One that shrinks gives back the pages behind ceil(want/page), which join the ring's end in the order of sequences and
+ * rows; they are handed out from the next call on.
+ * table      int32 [batch][max_pages], in and out: entries below ceil(held/page) are the sequence's pages; taken ones are added, those
+ *            given back become -1, others are left as they are.
+ * ring       int32 [n_pages], in and out, page numbers;  state  int32 [2], in and out: place of the first free page in the ring, free
+ *            pages.  At the start ring = 0 .. n_pages-1, state = (0, n_pages).  A state out of range counts as no free page (flag).
+ *            Pages given back that find no room in the ring (it would hold more than n_pages) are dropped (flag).
+ * length     out int32 [batch]: want[b], or held[b] of a sequence that got no pages.  May be held or want.
+ * first      out int32 [batch+1] or NULL: sums of max(want - held, 0): the places of new tokens, also of those that got no pages.
+ *            (int32: a sum of 2^31 or more is cut to 2^31 - 1, flag).
+ * pos, slot  out int32 [n_tok], both or neither NULL (NULL only with n_tok = 0; with them `first` is not NULL): a new token's position
+ *            and slot = table[b][pos/page] * page + pos % page, -1 where the sequence got no pages or its page number is out of range
+ *            (flag).  Entries behind the last token: position 0, slot -1.  Tokens at and behind n_tok are not written (flag).
+ * batch, page, n_pages and max_pages of cfg are used; the rest has to be valid.  Arrays must not overlap but as said.
+ */
+XKV_API int xkv_page_assign(const xkv_cache8_config* cfg, const int32_t* held, const int32_t* want, int32_t* table, int32_t* ring,
+                            int32_t* state, int32_t* first, int32_t* length, int32_t* pos, int32_t* slot, int32_t n_tok, uint32_t* flags,
+                            void* stream);
+
+/*
+ * Stores new rows as codes.  The rows that a call brings to a page form one run of ascending slots, side by side among the n_tok tokens
+ * (what xkv_page_assign gives; two runs into one page leave that page's codes and scales unspecified).  For each page and head:
+ *   e   = the smallest exponent with max |x| <= 448 * 2^e over the run's finite elements, at least -60;
+ *         if the run does not begin with the page's first row, the page holds the rows before it: then at least the old scale's exponent
+ *   new codes = x 2^-e rounded to e4m3 (to nearest even), codes of the rows before the run = c 2^(e_old - e) rounded likewise
+ *   scale = 2^e
+ * NaN becomes e4m3's NaN, infinities +-448 * 2^e.  Rows of a page behind the run are left as they were.
+ * k, v   bf16 [G][n_tok][H_kv][d_h];  slot  int32 [n_tok], -1: the token is skipped (so are others out of range, flag).
+ */
+XKV_API int xkv_cache8_append(const xkv_cache8_config* cfg, int layer_begin, int layer_end, const void* k, const void* v,
+                              const int32_t* slot, int32_t n_tok, void* K8, void* V8, float* k_scale, float* v_scale, uint32_t* flags,
+                              void* stream);
+
+/*
+ * K, V bf16 [G][batch][H_kv][cap][d_h]: row j < length[b] becomes what its codes stand for (exactly); rows at and behind length[b], and rows of pages out of range, are left as they were.
+ * length  int32 [batch], 0 <= length[b] <= min(cap, max_pages * page) (else clamped, flag).  1 <= cap <= XKV_CACHE_MAX_ROWS;
+ *         G*batch*H_kv*cap < 2^31 (else UNSUPPORTED).  K or V may be NULL: that one is not read back.
+ */
+XKV_API int xkv_cache8_read(const xkv_cache8_config* cfg, int layer_begin, int layer_end, const int32_t* table, const int32_t* length,
+                            const void* K8, const void* V8, const float* k_scale, const float* v_scale, int32_t cap, void* K, void* V,
+                            uint32_t* flags, void* stream);
+
+/*
+ * out_i = softmax(scale * q_i K^T) V over rows 0 .. length[b] - n_b + i of its sequence for token i of the n_b = first[b+1] - first[b]
+ * new tokens of sequence b, whose own rows are the last n_b of length[b] (append first, then attend): a decode step with one token
+ * each, a verification of drafted tokens in a chain, a chunk of a prompt, or all of them in one call.
+ * q          bf16 [G][n_tok][H_q][d_h], rotated.
+ * first      int32 [batch+1], ascending, within 0 .. n_tok (else clamped, flag), or NULL: one token for each sequence, n_tok = batch.
+ * max_new    1 <= max_new <= n_tok: no sequence has more new tokens (the tokens of one that has are left out from max_new on, flag).
+ * length     int32 [batch], rows with the new ones, 0 <= length[b] <= max_pages * page (else clamped, flag).
+ * workspace  device scratch of xkv_cache8_workspace_bytes(cfg, max_new) bytes, used during the call's kernels only: calls that may
+ *            overlap (two streams, two captured graphs that are replayed at once) need one each.
+ * out        bf16 [G][n_tok][H_q][d_h];  lse  optional fp32 [G][n_tok][H_q], natural logarithm of the sum of exp of scaled logits.
+ * Tokens that belong to no sequence (before first[0], behind first[batch]) are left as they were.  A token that attends to nothing
+ * (length[b] - n_b + i < 0, or all its rows' pages out of range), or whose logits are all minus infinity, gets 0 and lse -inf.
+ * A row that a token does not attend to has no influence on it, also where its codes are NaN.  A query with an element that is not
+ * finite gets NaN.  Scales are read as powers of two (their exponents); one of 0 marks a page that holds nothing: it is left out.
+ * Queries enter the product with the keys to 2^-18 of their largest element, weights the one with the values to 2^-11 of themselves or
+ * 2^-21 of the largest weight (times its value's scale); sums, maxima and the products' accumulation are fp32.
+ */
+XKV_API int xkv_cache8_workspace_bytes(const xkv_cache8_config* cfg, int32_t max_new, uint64_t* bytes);
+XKV_API int xkv_cache8_attend(const xkv_cache8_config* cfg, int layer_begin, int layer_end, const void* q, const int32_t* first,
+                              int32_t n_tok, int32_t max_new, const int32_t* table, const int32_t* length, const void* K8, const void* V8,
+                              const float* k_scale, const float* v_scale, void* workspace, uint64_t workspace_bytes, void* out,
+                              float* lse, uint32_t* flags, void* stream);
+
+/*
  * Algorithm 1 (App. B.1), the prefill side of the selector, for every sequence, layer and KV head g:
  *   landmark[j]  = mean over the rows x of chunk j of rope(K[x]),  chunk j = rows c*j .. min(c*j+c, T)-1   (lines 1-3)
  *   min_cos[j]   = min over those rows of cos(rope(K[x]), landmark[j])  (fp32, the unrounded mean; a zero vector
@@ -460,7 +634,11 @@ XKV_API uint64_t xkv_kernel_launch_count(void);
 #define XKV_KERNEL_TREE 12       /* attention of drafted tokens, its merge, the commit of a path */
 #define XKV_KERNEL_WEIGH 13      /* accumulated attention weights */
 #define XKV_KERNEL_EVICT 14      /* which rows of a cache stay, and their move */
-#define XKV_KERNEL_FAMILIES 15
+#define XKV_KERNEL_ROPE 15       /* rotary positions */
+#define XKV_KERNEL_PAGES 16      /* pages and slots of a paged cache */
+#define XKV_KERNEL_CODES 17      /* rows into 8-bit codes and back */
+#define XKV_KERNEL_ATTEND8 18    /* attention over a paged cache of codes, its merge */
+#define XKV_KERNEL_FAMILIES 19
 XKV_API int xkv_debug_launch_counts(uint64_t* counts);
 
 /*

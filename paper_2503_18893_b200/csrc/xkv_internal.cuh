@@ -108,6 +108,7 @@ enum KernelFamily {
   kFamTile = XKV_KERNEL_TILE, kFamTailTc = XKV_KERNEL_TAIL_TC, kFamTailCuda = XKV_KERNEL_TAIL_CUDA,
   kFamLandmarks = XKV_KERNEL_LANDMARKS, kFamPrep = XKV_KERNEL_PREP, kFamDense = XKV_KERNEL_DENSE, kFamClf = XKV_KERNEL_CLF, kFamMergeMulti = XKV_KERNEL_MERGE_MULTI,
   kFamTree = XKV_KERNEL_TREE, kFamWeigh = XKV_KERNEL_WEIGH, kFamEvict = XKV_KERNEL_EVICT,
+  kFamRope = XKV_KERNEL_ROPE, kFamPages = XKV_KERNEL_PAGES, kFamCodes = XKV_KERNEL_CODES, kFamAttend8 = XKV_KERNEL_ATTEND8,
   kFamCount = XKV_KERNEL_FAMILIES
 };
 void count_launch(KernelFamily family, int n = 1);
@@ -240,6 +241,31 @@ cudaError_t launch_evict_select(const xkv_cache_config* c, int l0, int l1, const
                                 cudaStream_t s);
 cudaError_t launch_evict_compact(const xkv_cache_config* c, int l0, int l1, __nv_bfloat16* K, __nv_bfloat16* V, const int32_t* src,
                                  int keep, float* weights, int32_t* pos, unsigned int* flags, cudaStream_t s);
+
+// xkv_rope.cu
+int rope_plan_init(const xkv_rope_config* c, xkv_rope_plan* plan);
+cudaError_t launch_rope(const xkv_rope_plan* plan, int direction, int type, const xkv_rope_tensor* tensors, int n_tensors, int64_t rows,
+                        const int32_t* pos, int64_t n_pos, cudaStream_t s);
+
+// xkv_pages.cu
+cudaError_t launch_page_assign(const xkv_cache8_config* c, const int32_t* held, const int32_t* want, int32_t* table, int32_t* ring,
+                               int32_t* state, int32_t* first, int32_t* length, int32_t* pos, int32_t* slot, int32_t n_tok,
+                               unsigned int* flags, cudaStream_t s);
+
+// xkv_codes.cu
+cudaError_t launch_cache8_append(const xkv_cache8_config* c, int l0, int l1, const __nv_bfloat16* k, const __nv_bfloat16* v,
+                                 const int32_t* slot, int n_tok, void* K8, void* V8, float* k_scale, float* v_scale, unsigned int* flags,
+                                 cudaStream_t s);
+cudaError_t launch_cache8_read(const xkv_cache8_config* c, int l0, int l1, const int32_t* table, const int32_t* length, const void* K8,
+                               const void* V8, const float* k_scale, const float* v_scale, int cap, __nv_bfloat16* K, __nv_bfloat16* V,
+                               unsigned int* flags, cudaStream_t s);
+
+// xkv_attend8.cu
+size_t cache8_workspace_bytes(const xkv_cache8_config* c, int max_new);
+cudaError_t launch_cache8_attend(const xkv_cache8_config* c, int l0, int l1, const __nv_bfloat16* q, const int32_t* first, int n_tok,
+                                 int max_new, const int32_t* table, const int32_t* length, const void* K8, const void* V8,
+                                 const float* k_scale, const float* v_scale, void* workspace, __nv_bfloat16* out, float* lse,
+                                 unsigned int* flags, int device, cudaStream_t s);
 
 // xkv_fused.cu
 int fused_slots(const xkv_group* grp);

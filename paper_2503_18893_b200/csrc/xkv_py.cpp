@@ -322,6 +322,12 @@ struct Checked : Args {
     }
     return const_cast<void*>(t.const_data_ptr());
   }
+  // Elements of the tensor that comes next (0 for anything else), which stays the next.
+  int64_t numel_of_next() {
+    if (bad) return 0;
+    PyObject* o = v[at];
+    return THPVariable_Check(o) ? THPVariable_Unpack(o).numel() : 0;
+  }
   float real() {
     PyObject* o = next();
     if (!o) return 0.0f;
@@ -416,6 +422,173 @@ XKV_CACHE_PY(evict_compact, 11)
   void* s = a.stream();
 XKV_CACHE_PY_END(xkv_evict_compact(c, l0, l1, K, V, src, keep, weights, pos, flags, s))
 
+// ---- rotary positions, and the paged cache of 8-bit codes
+#define XKV_CACHE8_PY(name, want) \
+  PyObject* name(PyObject*, PyObject* const* args, Py_ssize_t nargs) { \
+    HANDLE_TH_ERRORS \
+    Checked a(args, nargs, want); \
+    const xkv_cache8_config* c = (const xkv_cache8_config*)a.ptr(); \
+    if (a.bad) return nullptr; \
+    if (!c) { \
+      PyErr_SetString(PyExc_ValueError, "no cache configuration"); \
+      return nullptr; \
+    }
+
+XKV_CACHE8_PY(page_assign, 12)
+  const int32_t* held = (const int32_t*)a.tensor("held", at::kInt, {c->batch});
+  const int32_t* want = (const int32_t*)a.tensor("want", at::kInt, {c->batch});
+  int32_t* table = (int32_t*)a.tensor("table", at::kInt, {c->batch, c->max_pages});
+  int32_t* ring = (int32_t*)a.tensor("ring", at::kInt, {c->n_pages});
+  int32_t* state = (int32_t*)a.tensor("state", at::kInt, {2});
+  int32_t* first = (int32_t*)a.tensor("first", at::kInt, {(int64_t)c->batch + 1}, true);
+  int32_t* length = (int32_t*)a.tensor("length", at::kInt, {c->batch});
+  const int64_t n_tok = a.numel_of_next();
+  int32_t* pos = (int32_t*)a.tensor("pos", at::kInt, {n_tok}, true);
+  int32_t* slot = (int32_t*)a.tensor("slot", at::kInt, {n_tok}, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
+  void* s = a.stream();
+  if (!a.bad && n_tok > INT32_MAX) return PyLong_FromLong(XKV_ERR_UNSUPPORTED);
+XKV_CACHE_PY_END(xkv_page_assign(c, held, want, table, ring, state, first, length, pos, slot, (int32_t)n_tok, flags, s))
+
+XKV_CACHE8_PY(cache8_append, 13)
+  const int l0 = a.i32(), l1 = a.i32(), n = a.i32();
+  void* k = a.tensor("k", at::kBFloat16, {c->G, n, c->H_kv, c->d_h});
+  void* v = a.tensor("v", at::kBFloat16, {c->G, n, c->H_kv, c->d_h});
+  const int32_t* slot = (const int32_t*)a.tensor("slot", at::kInt, {n});
+  void* K8 = a.tensor("K8", at::kFloat8_e4m3fn, {c->G, c->n_pages, c->H_kv, c->page, c->d_h});
+  void* V8 = a.tensor("V8", at::kFloat8_e4m3fn, {c->G, c->n_pages, c->H_kv, c->page, c->d_h});
+  float* ks = (float*)a.tensor("k_scale", at::kFloat, {c->G, c->n_pages, c->H_kv});
+  float* vs = (float*)a.tensor("v_scale", at::kFloat, {c->G, c->n_pages, c->H_kv});
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
+  void* s = a.stream();
+  if (!a.bad && n == 0) return PyLong_FromLong(XKV_OK);        // (tensors without elements have no address)
+XKV_CACHE_PY_END(xkv_cache8_append(c, l0, l1, k, v, slot, n, K8, V8, ks, vs, flags, s))
+
+XKV_CACHE8_PY(cache8_read, 14)
+  const int l0 = a.i32(), l1 = a.i32(), cap = a.i32();
+  const int32_t* table = (const int32_t*)a.tensor("table", at::kInt, {c->batch, c->max_pages});
+  const int32_t* length = (const int32_t*)a.tensor("length", at::kInt, {c->batch});
+  void* K8 = a.tensor("K8", at::kFloat8_e4m3fn, {c->G, c->n_pages, c->H_kv, c->page, c->d_h});
+  void* V8 = a.tensor("V8", at::kFloat8_e4m3fn, {c->G, c->n_pages, c->H_kv, c->page, c->d_h});
+  const float* ks = (const float*)a.tensor("k_scale", at::kFloat, {c->G, c->n_pages, c->H_kv});
+  const float* vs = (const float*)a.tensor("v_scale", at::kFloat, {c->G, c->n_pages, c->H_kv});
+  void* K = a.tensor("K", at::kBFloat16, {c->G, c->batch, c->H_kv, cap, c->d_h}, true);
+  void* V = a.tensor("V", at::kBFloat16, {c->G, c->batch, c->H_kv, cap, c->d_h}, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
+  void* s = a.stream();
+XKV_CACHE_PY_END(xkv_cache8_read(c, l0, l1, table, length, K8, V8, ks, vs, cap, K, V, flags, s))
+
+XKV_CACHE8_PY(cache8_attend, 18)
+  const int l0 = a.i32(), l1 = a.i32(), n = a.i32();
+  void* q = a.tensor("q", at::kBFloat16, {c->G, n, c->H_q, c->d_h});
+  const int32_t* first = (const int32_t*)a.tensor("first", at::kInt, {(int64_t)c->batch + 1}, true);
+  const int max_new = a.i32();
+  const int32_t* table = (const int32_t*)a.tensor("table", at::kInt, {c->batch, c->max_pages});
+  const int32_t* length = (const int32_t*)a.tensor("length", at::kInt, {c->batch});
+  void* K8 = a.tensor("K8", at::kFloat8_e4m3fn, {c->G, c->n_pages, c->H_kv, c->page, c->d_h});
+  void* V8 = a.tensor("V8", at::kFloat8_e4m3fn, {c->G, c->n_pages, c->H_kv, c->page, c->d_h});
+  const float* ks = (const float*)a.tensor("k_scale", at::kFloat, {c->G, c->n_pages, c->H_kv});
+  const float* vs = (const float*)a.tensor("v_scale", at::kFloat, {c->G, c->n_pages, c->H_kv});
+  if (a.bad) return nullptr;
+  uint64_t need = 0;
+  const int refused = xkv_cache8_workspace_bytes(c, max_new, &need);
+  if (refused != XKV_OK) return PyLong_FromLong(refused);
+  void* ws = a.tensor("workspace", at::kByte, {(int64_t)need}, false, true);
+  void* out = a.tensor("out", at::kBFloat16, {c->G, n, c->H_q, c->d_h});
+  float* lse = (float*)a.tensor("lse", at::kFloat, {c->G, n, c->H_q}, true);
+  uint32_t* flags = (uint32_t*)a.tensor("flags", at::kInt, {1}, true, true);
+  void* s = a.stream();
+XKV_CACHE_PY_END(xkv_cache8_attend(c, l0, l1, q, first, n, max_new, table, length, K8, V8, ks, vs, ws, need, out, lse, flags, s))
+
+// A tensor of heads: [..., heads, d_h] with the elements of a head side by side, and leading axes that join to one axis of rows.
+bool heads_of(Checked& a, const char* name, const at::Tensor& t, int d_h, void** p, int64_t* rows, int64_t* row, int64_t* head, int32_t* heads) {
+  const char* what = nullptr;
+  const int64_t n = t.dim();
+  if (n < 3 || t.size(-1) != d_h) what = "is not [..., rows, heads, d_h]";
+  else if (t.stride(-1) != 1 && d_h > 1) what = "does not have the elements of a head side by side";
+  else if (t.size(-2) > INT32_MAX) what = "has too many heads";
+  else if (!a.on_device(t)) what = "is not on the current CUDA device";
+  int64_t r = 1;
+  for (int64_t i = n - 3; !what && i >= 0; --i) {
+    if (t.size(i) != 1 && r > 1 && t.stride(i) != r * *row) what = "has leading axes that do not join to one";
+    if (t.size(i) != 1 && r == 1) *row = t.stride(i);
+    r *= t.size(i);
+  }
+  if (what) {
+    PyErr_Format(PyExc_ValueError, "%s: the tensor %s", name, what);
+    return false;
+  }
+  *p = const_cast<void*>(t.const_data_ptr());
+  *rows = r;
+  *head = t.stride(-2);
+  *heads = (int32_t)t.size(-2);
+  return true;
+}
+
+// rope(plan, direction, pos, x, y or None, x2 or None, y2 or None, stream)
+PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  Checked a(args, nargs, 8);
+  const xkv_rope_plan* plan = (const xkv_rope_plan*)a.ptr();
+  if (a.bad) return nullptr;
+  if (!plan) {
+    PyErr_SetString(PyExc_ValueError, "no rotation plan");
+    return nullptr;
+  }
+  const int direction = a.i32();
+  const int64_t n_pos = a.numel_of_next();
+  const int32_t* pos = (const int32_t*)a.tensor("pos", at::kInt, {n_pos});
+  xkv_rope_tensor t[2] = {};
+  int n = 0, type = -1;
+  int64_t rows = 0;
+  for (int i = 0; i < 2 && !a.bad; ++i) {
+    PyObject* x = a.next();
+    PyObject* y = a.next();
+    if (i == 1 && x == Py_None && y == Py_None) break;
+    const char* names[2][2] = {{"x", "out"}, {"x2", "out2"}};
+    if (!THPVariable_Check(x) || (y != Py_None && !THPVariable_Check(y))) {
+      PyErr_Format(PyExc_TypeError, "%s, %s: expected tensors", names[i][0], names[i][1]);
+      return nullptr;
+    }
+    const at::Tensor& tx = THPVariable_Unpack(x);
+    const at::Tensor& ty = y == Py_None ? tx : THPVariable_Unpack(y);
+    const at::ScalarType st = tx.scalar_type();
+    const int ti = st == at::kBFloat16 ? XKV_BF16 : st == at::kHalf ? XKV_FP16 : st == at::kFloat ? XKV_FP32 : -1;
+    void *px, *py;
+    int64_t rx, ry;
+    int32_t hy;
+    t[i].x_row = t[i].y_row = 0;
+    if (!heads_of(a, names[i][0], tx, plan->d_h, &px, &rx, &t[i].x_row, &t[i].x_head, &t[i].heads) ||
+        !heads_of(a, names[i][1], ty, plan->d_h, &py, &ry, &t[i].y_row, &t[i].y_head, &hy))
+      return nullptr;
+    const char* what = nullptr;
+    if (ti < 0) what = "bfloat16, float16 or float32 expected";
+    else if (i == 1 && ti != type) what = "both tensors have to have the same type";
+    else if (ty.scalar_type() != st || ry != rx || hy != t[i].heads) what = "the output has another type or shape";
+    else if (i == 1 && rx != rows) what = "both tensors have to have as many rows";
+    else if (n_pos < 1 || rx % n_pos) what = "the number of positions does not divide the number of rows";
+    if (what) {
+      PyErr_Format(PyExc_ValueError, "%s: %s", names[i][0], what);
+      return nullptr;
+    }
+    t[i].x = px;
+    t[i].y = py;
+    rows = rx;
+    type = ti;
+    n = i + 1;
+  }
+  if (n == 1) a.at = 7;
+  void* s = a.stream();
+  if (a.bad) return nullptr;
+  int st;
+  {
+    const WithoutGil no_gil;
+    st = xkv_rope(plan, direction, type, t, n, rows, pos, n_pos, s);
+  }
+  return PyLong_FromLong(st);
+  END_HANDLE_TH_ERRORS
+}
+
 // torch_hooks(get_device, get_current_raw_stream): how "the current stream" is found.
 PyObject* torch_hooks(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (nargs != 2) { PyErr_SetString(PyExc_TypeError, "expected 2 arguments"); return nullptr; }
@@ -430,7 +603,8 @@ PyObject* torch_hooks(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 PyMethodDef methods[] = {XKV_DEF(sr_select), XKV_DEF(sr_select_static), XKV_DEF(sr_reconstruct_attend),
                          XKV_DEF(sr_reconstruct_attend_tail), XKV_DEF(dense_attend), XKV_DEF(quantize_rtn),
                          XKV_DEF(dequantize_rtn), XKV_DEF(tree_attend), XKV_DEF(tree_commit), XKV_DEF(cache_weigh),
-                         XKV_DEF(evict_select), XKV_DEF(evict_compact), XKV_DEF(torch_hooks), {nullptr, nullptr, 0, nullptr}};
+                         XKV_DEF(evict_select), XKV_DEF(evict_compact), XKV_DEF(rope), XKV_DEF(page_assign),
+                         XKV_DEF(cache8_append), XKV_DEF(cache8_read), XKV_DEF(cache8_attend), XKV_DEF(torch_hooks), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_xkv", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -126,7 +126,7 @@ _lib.xkv_debug_set_fault_injection.argtypes = [_P, ctypes.c_uint32]
 _lib.xkv_debug_set_fault_injection.restype = ctypes.c_int
 
 XKV_KERNEL_FAMILIES = ("scan", "topk", "fused", "merge", "tile", "tail_tc", "tail_cuda", "landmarks", "prep", "dense",
-                       "clf", "merge_multi", "tree", "weigh", "evict")
+                       "clf", "merge_multi", "tree", "weigh", "evict", "rope", "pages", "codes", "attend8")
 XKV_FLAG_CLF_BREAKDOWN = 4
 XKV_INJECT_SCAN_NO_LOAD = 1
 XKV_INJECT_FUSED_NO_B = 2
@@ -499,6 +499,144 @@ def xkv_evict_compact(cfg: xkv_cache_config, layer_begin: int, layer_end: int, K
     st = _xkv.evict_compact(ctypes.addressof(cfg), layer_begin, layer_end, K, V, keep, src, weights, pos, flags, stream)
     if st != XKV_OK:
         raise XKVError(st, "xkv_evict_compact")
+
+
+# ---- rotary positions
+
+
+class xkv_rope_config(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("d_h", ctypes.c_int32), ("rot", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double), ("original", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double),
+                ("gain", ctypes.c_double)]
+
+
+XKV_ROPE_MAX_ROT = 256
+
+
+class xkv_rope_plan(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("d_h", ctypes.c_int32), ("rot", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("gain", ctypes.c_float), ("reserved", ctypes.c_uint32), ("turns", ctypes.c_uint64 * (XKV_ROPE_MAX_ROT // 2))]
+
+
+class xkv_rope_tensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_row", ctypes.c_int64), ("x_head", ctypes.c_int64),
+                ("y_row", ctypes.c_int64), ("y_head", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
+XKV_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+XKV_ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "llama3": 3, "yarn": 4}
+XKV_ROPE_DIRECTIONS = {"forward": 0, "adjoint": 1, "inverse": 2}
+_lib.xkv_rope_plan_init.argtypes = [ctypes.POINTER(xkv_rope_config), ctypes.POINTER(xkv_rope_plan)]
+_lib.xkv_rope_plan_init.restype = ctypes.c_int
+_lib.xkv_rope.argtypes = [ctypes.POINTER(xkv_rope_plan), ctypes.c_int, ctypes.c_int, ctypes.POINTER(xkv_rope_tensor), ctypes.c_int,
+                          ctypes.c_int64, _P, ctypes.c_int64, _P]
+_lib.xkv_rope.restype = ctypes.c_int
+
+
+def make_rope(*, d_h, rot=None, layout="half", base=10000.0, scaling="none", factor=1.0, original=0.0, low=1.0, high=4.0,
+              beta_fast=32.0, beta_slow=1.0, gain=0.0) -> xkv_rope_plan:
+    """The frequencies of a rotation of the first `rot` (all) elements of a head; `layout` one of XKV_ROPE_LAYOUTS, `scaling` of
+    XKV_ROPE_SCALINGS (formulas in include/xkv.h).  Host only."""
+    for name, value, known in (("layout", layout, XKV_ROPE_LAYOUTS), ("scaling", scaling, XKV_ROPE_SCALINGS)):
+        if value not in known:
+            raise ValueError(f"{name}: {value!r} is none of {', '.join(known)}")
+    cfg = xkv_rope_config(ctypes.sizeof(xkv_rope_config), d_h, d_h if rot is None else rot, XKV_ROPE_LAYOUTS[layout],
+                          XKV_ROPE_SCALINGS[scaling], base, factor, original, low, high, beta_fast, beta_slow, gain)
+    plan = xkv_rope_plan()
+    st = _lib.xkv_rope_plan_init(ctypes.byref(cfg), ctypes.byref(plan))
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_rope_plan_init")
+    return plan
+
+
+def xkv_rope(plan: xkv_rope_plan, x, pos, out=None, x2=None, out2=None, *, direction="forward", stream=None) -> None:
+    """Rotates x [..., rows, heads, d_h] (and x2, with as many rows) by the positions `pos` int32, into `out` or in place.  Rows and
+    heads may lie at any distance, the elements of a head side by side; row r has position pos[r % len(pos)].
+    `direction`: "forward", "adjoint" (the gradient of forward) or "inverse" (undoes forward)."""
+    if direction not in XKV_ROPE_DIRECTIONS:
+        raise ValueError(f"direction: {direction!r} is none of {', '.join(XKV_ROPE_DIRECTIONS)}")
+    st = _xkv.rope(ctypes.addressof(plan), XKV_ROPE_DIRECTIONS[direction], pos, x, out, x2, out2, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_rope")
+
+
+# ---- a paged cache of 8-bit codes.  Tensors are checked as for the uncompressed cache above; codes are torch.float8_e4m3fn.
+
+
+class xkv_cache8_config(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("G", ctypes.c_int32), ("batch", ctypes.c_int32), ("H_kv", ctypes.c_int32),
+                ("H_q", ctypes.c_int32), ("d_h", ctypes.c_int32), ("page", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+_CFG8 = ctypes.POINTER(xkv_cache8_config)
+_lib.xkv_page_assign.argtypes = [_CFG8, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P]
+_lib.xkv_page_assign.restype = ctypes.c_int
+_lib.xkv_cache8_append.argtypes = [_CFG8, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P]
+_lib.xkv_cache8_append.restype = ctypes.c_int
+_lib.xkv_cache8_read.argtypes = [_CFG8, _I, _I, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P]
+_lib.xkv_cache8_read.restype = ctypes.c_int
+_lib.xkv_cache8_workspace_bytes.argtypes = [_CFG8, _I, ctypes.POINTER(ctypes.c_uint64)]
+_lib.xkv_cache8_workspace_bytes.restype = ctypes.c_int
+_lib.xkv_cache8_attend.argtypes = [_CFG8, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, ctypes.c_uint64, _P, _P, _P, _P]
+_lib.xkv_cache8_attend.restype = ctypes.c_int
+
+
+def make_cache8_config(*, G, batch, H_kv, H_q, d_h, page, n_pages, max_pages, softmax_scale=0.0) -> xkv_cache8_config:
+    """Sizes of a paged cache of codes K8, V8 [G][n_pages][H_kv][page][d_h] with scales fp32 [G][n_pages][H_kv] and a block table int32
+    [batch][max_pages] (include/xkv.h)."""
+    return xkv_cache8_config(ctypes.sizeof(xkv_cache8_config), G, batch, H_kv, H_q, d_h, page, n_pages, max_pages, softmax_scale)
+
+
+def xkv_page_assign(cfg: xkv_cache8_config, held, want, table, ring, state, first, length, pos=None, slot=None, flags=None,
+                    stream=None) -> None:
+    """Pages for sequences that go from `held` to `want` rows (int32 [batch]): `table`, the `ring` of free pages (int32 [n_pages]) and
+    its `state` (int32 [2]: first, number) are updated; `length` becomes the rows of each sequence, `first` (int32 [batch+1], or None)
+    the places of new tokens, `pos` and `slot` (int32 [n_tok], or None) their positions and slots."""
+    st = _xkv.page_assign(ctypes.addressof(cfg), held, want, table, ring, state, first, length, pos, slot, flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_page_assign")
+
+
+def xkv_cache8_append(cfg: xkv_cache8_config, layer_begin: int, layer_end: int, k, v, slot, K8, V8, k_scale, v_scale, flags=None,
+                      stream=None) -> None:
+    """Stores k, v bf16 [G][n_tok][H_kv][d_h] as codes at `slot` (int32 [n_tok])."""
+    st = _xkv.cache8_append(ctypes.addressof(cfg), layer_begin, layer_end, slot.numel(), k, v, slot, K8, V8, k_scale, v_scale, flags,
+                            stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_cache8_append")
+
+
+def xkv_cache8_read(cfg: xkv_cache8_config, layer_begin: int, layer_end: int, table, length, K8, V8, k_scale, v_scale, K, V, flags=None,
+                    stream=None) -> None:
+    """The first `length` rows of every sequence as K, V bf16 [G][batch][H_kv][cap][d_h] (either may be None)."""
+    some = K if K is not None else V
+    if some is None:
+        raise ValueError("neither K nor V is asked for")
+    st = _xkv.cache8_read(ctypes.addressof(cfg), layer_begin, layer_end, some.shape[-2], table, length, K8, V8, k_scale, v_scale, K, V,
+                          flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_cache8_read")
+
+
+def xkv_cache8_workspace_bytes(cfg: xkv_cache8_config, max_new: int) -> int:
+    b = ctypes.c_uint64()
+    st = _lib.xkv_cache8_workspace_bytes(ctypes.byref(cfg), max_new, ctypes.byref(b))
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_cache8_workspace_bytes")
+    return b.value
+
+
+def xkv_cache8_attend(cfg: xkv_cache8_config, layer_begin: int, layer_end: int, q, first, max_new: int, table, length, K8, V8, k_scale,
+                      v_scale, workspace, out, lse=None, flags=None, stream=None) -> None:
+    """Attention of the sequences' last tokens q [G][n_tok][H_q][d_h], those of sequence b from first[b] on (None: one each), over its
+    `length` rows up to the token's own.  `max_new`: the most new tokens of a sequence; `workspace`: a uint8 device tensor of at least
+    xkv_cache8_workspace_bytes(cfg, max_new) bytes."""
+    st = _xkv.cache8_attend(ctypes.addressof(cfg), layer_begin, layer_end, q.shape[-3], q, first, max_new, table, length, K8, V8, k_scale,
+                            v_scale, workspace, out, lse, flags, stream)
+    if st != XKV_OK:
+        raise XKVError(st, "xkv_cache8_attend")
 
 
 def xkv_group_status(grp: Group, stream=None):
