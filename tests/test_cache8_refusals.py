@@ -158,10 +158,8 @@ def test_the_binding_checks_tensors(xkv):
     with pytest.raises(ValueError, match="q: the tensor"):
         xkv.xkv_cache8_attend(cfg, 0, 2, torch.zeros((2, 3, 8, 128)), None, 1, i, i, t, t, t, t, t, t)
     plan = xkv.make_rope(d_h=64)
-    with pytest.raises(ValueError, match="rows, heads, d_h"):
-        xkv.xkv_rope(plan, torch.zeros((3, 64)), i)
-    with pytest.raises(TypeError):
-        xkv.xkv_rope(plan, None, i)
+    with pytest.raises(ValueError, match="pos: the tensor"):
+        xkv.xkv_rope(plan, torch.zeros((3, 1, 64)), torch.zeros(3))
     with pytest.raises(ValueError, match="current CUDA device"):
         xkv.xkv_rope(plan, torch.zeros((3, 1, 64)), i)
 

@@ -112,6 +112,24 @@ def test_inverse_undoes_forward_and_adjoint_is_the_gradient(xkv):
         assert bool((((col * w).double().sum(-1) - grad[..., e].double()).abs() <= 2.0 ** -18 * 1.5 * 2 * w.abs().amax(-1)).all())
 
 
+def test_tensors_that_are_refused(xkv):
+    plan = xkv.make_rope(d_h=64)
+    x, pos = torch.zeros((6, 2, 64), device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    for bad in (x[0], x[..., :32], x.transpose(1, 2), x.double(), x.cpu(), torch.zeros((2, 6, 2, 64), device="cuda")[:, :5], x[:5]):
+        with pytest.raises(ValueError):
+            xkv.xkv_rope(plan, bad, pos)
+    for out in (x[:3], x.half(), x[:, :1], x.cpu()):
+        with pytest.raises(ValueError):
+            xkv.xkv_rope(plan, x, pos, out)
+    for second in (x[:3], x.half()):
+        with pytest.raises(ValueError):
+            xkv.xkv_rope(plan, x, pos, None, second)
+    with pytest.raises(TypeError):
+        xkv.xkv_rope(plan, None, pos)
+    with pytest.raises(TypeError):
+        xkv.xkv_rope(plan, x, pos, 5)
+
+
 def test_nothing_to_do(xkv):
     plan = xkv.make_rope(d_h=64)
     pos = torch.zeros(1, dtype=torch.int32, device="cuda")
