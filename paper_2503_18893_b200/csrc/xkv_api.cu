@@ -105,6 +105,19 @@ bool encode_bf16_map(void* out, const void* base, uint64_t rows, uint64_t cols, 
   return r == CUDA_SUCCESS;
 }
 
+// 2-D tensor of bytes [rows][cols], cols 64 or 128, box = box_rows whole rows, a swizzle as wide as a row.
+bool encode_byte_map(void* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {cols};
+  cuuint32_t box[2] = {(cuuint32_t)cols, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return enc((CUtensorMap*)out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, cols == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool encode_landmark_map(void* out, const void* base, uint64_t rows, uint64_t cols) {
   return encode_rows64(out, base, rows, cols, kLandmarkBoxRows);
 }

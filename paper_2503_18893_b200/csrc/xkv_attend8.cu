@@ -1,7 +1,29 @@
 // Attention over a paged cache of 8-bit codes (xkv_cache8_attend): out_i = softmax(scale q_i K^T) V over the rows of token i's sequence
-// up to its own, K and V being codes times their pages' scales.
+// up to its own, K and V being e4m3 codes times their pages' scales, powers of two.
 //
-// One CTA per token, query head and layer; thread = row of a 128-row tile for the logits, thread = column for the weighted sum.
+// The codes go from memory into the tensor core as they are, and the products are turned around, so that the 128 rows of a tile of the
+// cache are the wide side and a block of query rows (tokens times the query heads of a KV head, 8 to 64) the narrow one:
+//   S^T = K8 Q8^T       M = 128 rows of the cache, N = query rows
+//   O^T += V8^T P8^T    M = d_h, N = query rows, K = 128 rows of the cache
+// Both operands of such a product have to be e4m3, which holds 4 significant bits; a query and a weight are split into several:
+//   q 2^-x = q_hi + q_lo   (x: its row's largest element lies in [128, 256)): a bf16 value's 8 bits are two codes, exactly for elements
+//                          above 2^-10 of the largest, to 2^-18 of it below.  Two products into the same S.
+//   w = w_0 + 2^-5 w_1 + 2^-10 w_2   of a weight in 16 bits (fp16): each code is the rounding of 2^5 times what the one before left.
+//                          Three groups of columns of O, joined at the end.  Weights lie below 2^8 and the largest of a column above
+//                          2^4, so a weight is exact to 2^-12 of itself or 2^-24 of the largest: a long even rest beside a row that
+//                          draws most of the weight keeps its own.
+// A key's scale multiplies the row's logits.  A value's scale 2^e joins the exponent: w_j = 2^(z_j + e_j - m), so that codes meet weights
+// that hold their scale, and m is the maximum of z_j + e_j; the denominator sums w_j 2^-e_j in fp32.
+//
+//   producer  a page is one box of the copy engine: lane i of the warp has the i-th page of a tile, its entry of the table and its scales
+//             (asynchronous copies of four bytes, which report to the same barrier as the codes)
+//   issuer    S of a tile two ahead, O of this one
+//   softmax   two warpgroups, tile by tile in turns, each with its own maxima, sums and O; thread = row of the cache, so that a token's
+//             view (rows up to its own) is a comparison of the column with one number per thread.  Maxima move only when a weight would
+//             pass 2^8: one vote per tile.
+// All tiles of all problems form one list that is cut into as many even pieces as there are CTAs; a piece that holds a whole problem
+// writes its output, the others leave (O, m, l) for the merge.  Lengths are read on the device only.
+#include <cuda.h>
 #include <math.h>
 
 #include <cuda_fp16.h>
@@ -12,133 +34,848 @@ namespace xkv {
 
 namespace {
 
-constexpr int kThreads8 = 128;
+constexpr int kThreads8 = 320;                 // two warpgroups, producer, issuer
+constexpr int kProducer8 = 8, kIssuer8 = 9;
+constexpr int kMergeWarps8 = 8;
+constexpr float kTop = 8.0f, kSet = 4.0f;      // log2: a weight's bound; where a column's largest weight is put
 
 struct Attend8Args {
-  int batch, H_kv, H_q, n_rep, n_pages, max_pages, page_shift, n_tok, max_new, l0;
+  int batch, H_kv, H_q, n_rep, n_pages, max_pages, page_shift, n_tok, max_new, l0, layers;
+  int block_tok;                               // tokens of a block of query rows
+  uint32_t rep_inv;                            // ceil(2^16 / n_rep)
   float scale2;                                // softmax scale times log2(e)
   const __nv_bfloat16* q;
   const int32_t* first;
   const int32_t* table;
   const int32_t* length;
-  const uint8_t* K8;
-  const uint8_t* V8;
+  const uint8_t* V8;                           // (codes that are NaN)
   const float* k_scale;
   const float* v_scale;
+  float* part;                                 // [CTA][2][rows of a block][d_h]
+  float2* part_ml;                             // [CTA][2][rows of a block] (m, l)
   __nv_bfloat16* out;
   float* lse;
   unsigned int* flags;
+  unsigned int inject;                         // XKV_INJECT_CACHE_* bits; 0 in normal use
 };
 
-__device__ __forceinline__ float code_value(uint8_t c) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
-  return __half2float(__ushort_as_half((unsigned short)h));
+// A sequence: its first token, how many of its tokens are looked after, its rows, and those before its first new one (below zero if
+// it has more new tokens than rows).
+struct Seq {
+  int f0, n, base, len;
+};
+__device__ __forceinline__ Seq load_seq(const Attend8Args& a, int b, bool* bad) {
+  const int w0 = a.first ? a.first[b] : b, w1 = a.first ? a.first[b + 1] : b + 1, wl = a.length[b];
+  const int f0 = min(max(w0, 0), a.n_tok), f1 = min(max(w1, f0), a.n_tok), len = min(max(wl, 0), a.max_pages << a.page_shift);
+  *bad = f0 != w0 || f1 != w1 || len != wl || f1 - f0 > a.max_new;
+  return Seq{f0, min(f1 - f0, a.max_new), len - (f1 - f0), len};
 }
-__device__ __forceinline__ float power_of_two(float scale) { return __int_as_float(__float_as_int(scale) & 0x7f800000); }
+__device__ __forceinline__ int blocks_of(const Attend8Args& a, const Seq& s) { return (s.n + a.block_tok - 1) / a.block_tok; }
+// Rows that the last token of block qp sees, and the tiles that they lie in (one for tokens that see nothing: it says so).
+__device__ __forceinline__ int rows_seen(const Attend8Args& a, const Seq& s, int qp) {
+  return min(max(s.base + min(s.n, (qp + 1) * a.block_tok), 0), s.len);
+}
+__device__ __forceinline__ int tiles_of(int rows) { return max(1, (rows + kTile - 1) / kTile); }
 
-template <int DH>
-__global__ void __launch_bounds__(kThreads8) attend8_plain_kernel(const Attend8Args a) {
-  __shared__ float q_s[DH], p_s[kThreads8], red_s[2][4];
-  const int t = blockIdx.x, hq = blockIdx.y, l = a.l0 + (int)blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  ptx::grid_dependency_wait();
-  ptx::grid_dependency_launch();
-  bool bad = false;
-  auto first_of = [&](int b) {
-    const int f = a.first ? a.first[b] : b, c = min(max(f, 0), a.n_tok);
-    bad |= f != c;
-    return c;
-  };
-  int lo = 0, hi = a.batch - 1;                // the sequence of token t
+// sum over i < n of floor((a i + b) / m), all of them non-negative: Euclid's algorithm on (a, m).
+__device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+  long long sum = 0;
+  while (n > 0) {
+    if (a >= m) { sum += n * (n - 1) / 2 * (a / m); a %= m; }
+    if (b >= m) { sum += n * (b / m); b %= m; }
+    const long long y = a * n + b;
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const long long t = m;
+    m = a;
+    a = t;
+  }
+  return sum;
+}
+// Tiles of one head in blocks 0 .. qp-1 of a sequence of n_qp blocks; those before the last are full: their rows grow by block_tok.
+__device__ long long tiles_before(const Attend8Args& a, const Seq& s, int qp, int n_qp) {
+  if (qp == 0) return 0;
+  if (qp == n_qp) return tiles_before(a, s, qp - 1, n_qp) + tiles_of(rows_seen(a, s, qp - 1));
+  const int most = kTile - s.base;             // blocks that see up to one tile count one
+  const int ones = most > 0 ? min(qp, most / a.block_tok) : 0;
+  return ones + floor_sum(qp - ones, kTile, a.block_tok, s.base + (long long)(ones + 1) * a.block_tok + kTile - 1);
+}
+__device__ __forceinline__ long long tiles_of_head(const Attend8Args& a, const Seq& s) {
+  if (s.n <= a.block_tok) return s.n > 0 ? tiles_of(rows_seen(a, s, 0)) : 0;
+  const int n_qp = blocks_of(a, s);
+  return tiles_before(a, s, n_qp, n_qp);
+}
+
+// A place in the list of tiles.  Order: layer, head, sequence, block, tile.
+struct Place {
+  int l, g, b, qp, t, nt, n_qp;
+  Seq s;
+};
+__device__ __forceinline__ void set_block(const Attend8Args& a, Place& p) { p.nt = tiles_of(rows_seen(a, p.s, p.qp)); }
+// Moves to the next problem (there is one: the caller counts).
+__device__ __forceinline__ void next_problem(const Attend8Args& a, Place& p) {
+  p.t = 0;
+  if (++p.qp >= p.n_qp) {
+    p.qp = 0;
+    do {
+      if (++p.b == a.batch) {
+        p.b = 0;
+        if (++p.g == a.H_kv) { p.g = 0; ++p.l; }
+      }
+      bool bad;
+      p.s = load_seq(a, p.b, &bad);
+      p.n_qp = blocks_of(a, p.s);
+    } while (p.n_qp == 0 && p.l < a.layers);
+  }
+  set_block(a, p);
+}
+
+__device__ __forceinline__ long long warp_sum(long long v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// Lane: tiles of one head in sequence b0 + lane.
+__device__ __forceinline__ long long lane_tiles(const Attend8Args& a, int b0, Seq* s, bool report) {
+  const int b = b0 + (int)(threadIdx.x & 31);
+  if (b >= a.batch) return 0;
+  bool bad;
+  *s = load_seq(a, b, &bad);
+  if (bad && report && a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+  return tiles_of_head(a, *s);
+}
+// By a whole warp: tiles of one head over the batch, and over the sequences before b.
+__device__ __forceinline__ long long head_tiles(const Attend8Args& a, int b, long long* before, bool report = false) {
+  long long all = 0, mine = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    Seq s;
+    const long long v = lane_tiles(a, b0, &s, report);
+    all += v;
+    if (b0 + (int)(threadIdx.x & 31) < b) mine += v;
+  }
+  *before = warp_sum(mine);
+  return warp_sum(all);
+}
+__device__ __forceinline__ long long piece_begin8(long long total, int ctas, int c) { return total * c / ctas; }
+__device__ __forceinline__ int piece_of8(long long total, int ctas, long long u) { return (int)(((u + 1) * ctas - 1) / total); }
+
+// By a whole warp: how many tiles CTA c has, and the place of the first.
+__device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int grid, long long* count, bool report) {
+  long long before;
+  const long long head = head_tiles(a, 0, &before, report), total = head * a.H_kv * a.layers;
+  const int ctas = (int)min((long long)grid, total);
+  Place p = {};
+  *count = 0;
+  if (c >= ctas) return p;
+  const long long u0 = piece_begin8(total, ctas, c);
+  *count = piece_begin8(total, ctas, c + 1) - u0;
+  const long long lg = u0 / head;
+  long long rest = u0 - lg * head;
+  p.l = (int)(lg / a.H_kv);
+  p.g = (int)(lg - (long long)p.l * a.H_kv);
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {   // (u0 is in the list: the search ends inside the batch)
+    Seq s = {};
+    const long long v = lane_tiles(a, b0, &s, false);
+    long long upto = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+      if ((int)(threadIdx.x & 31) >= o) upto += x;
+    }
+    const unsigned holds = __ballot_sync(0xffffffffu, rest < upto);
+    if (holds) {
+      const int at = __ffs(holds) - 1;
+      rest -= __shfl_sync(0xffffffffu, upto - v, at);
+      p.b = b0 + at;
+      p.s.f0 = __shfl_sync(0xffffffffu, s.f0, at);
+      p.s.n = __shfl_sync(0xffffffffu, s.n, at);
+      p.s.base = __shfl_sync(0xffffffffu, s.base, at);
+      p.s.len = __shfl_sync(0xffffffffu, s.len, at);
+      break;
+    }
+    rest -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  p.n_qp = blocks_of(a, p.s);
+  int lo = 0, hi = p.n_qp - 1;                 // the last block that begins at or before `rest`
   while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (first_of(mid + 1) > t) hi = mid; else lo = mid + 1;
+    const int mid = (lo + hi + 1) >> 1;
+    if (tiles_before(a, p.s, mid, p.n_qp) <= rest) lo = mid; else hi = mid - 1;
   }
-  const int f0 = first_of(lo), f1 = first_of(lo + 1), n = f1 - f0;
-  if (t < f0 || t >= f1 || t - f0 >= a.max_new) return;
-  const int want = a.length[lo], len = min(max(want, 0), a.max_pages << a.page_shift);
-  bad |= want != len || n > a.max_new;
-  const int rows = max(0, min(len, len - n + (t - f0) + 1));
-  const int g = hq / a.n_rep;
-  const size_t qh = ((size_t)l * a.n_tok + t) * a.H_q + hq;
-  if (tid < DH) q_s[tid] = __bfloat162float(a.q[qh * DH + tid]);
+  p.qp = lo;
+  p.t = (int)(rest - tiles_before(a, p.s, lo, p.n_qp));
+  set_block(a, p);
+  return p;
+}
+
+// ---- e4m3
+__device__ __forceinline__ uint32_t encode_f32x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t encode_f16x2(__half2 x) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&x)));
+  return r;
+}
+__device__ __forceinline__ __half2 decode_f16x2(uint32_t codes) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+  return *reinterpret_cast<__half2*>(&h);
+}
+// Does one of four codes say NaN?
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu); }
+
+template <int N>
+__device__ __forceinline__ void load_columns(uint32_t addr, float (&v)[N]) {
+  if constexpr (N <= 16) {
+    ptx::tmem_ld<N>(addr, v);
+  } else {
+#pragma unroll
+    for (int c = 0; c < N; c += 32) ptx::tmem_ld32_nb(addr + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
+#pragma unroll
+    for (int c = 0; c < N; c += 32) ptx::tc_wait_ld32_nb(*reinterpret_cast<uint32_t(*)[32]>(v + c));
+    return;
+  }
+  ptx::tc_wait_ld();
+}
+
+template <int DH, int RB>
+struct Shape8 {
+  static constexpr int kQ = RB < 16 ? 16 : RB;                 // columns of S (a product is 16 wide at least)
+  static constexpr int kP = (3 * RB + 15) / 16 * 16;           // columns of O: three groups of RB
+  static constexpr int kSlot = kTile * DH;
+  static constexpr int kSlots = DH == 64 ? 16 : RB == 64 ? 8 : 10;         // K and V tiles in turns
+  static constexpr int kQBytes = kQ * DH, kPBytes = kP * kTile;
+  static constexpr int kBytes = 1024 + kSlots * kSlot + 2 * kPBytes + 2 * kQBytes;
+  static constexpr int kTmem = RB == 64 ? 512 : RB == 32 ? 256 : 128;      // 2 (kQ + kP), rounded up
+};
+
+// Sums of N columns over the lanes of a warp: lane i gets those of columns i, i + 32, ...
+template <int N>
+__device__ __forceinline__ void sum_columns(float (&v)[N], float* dst) {
+  const int lane = threadIdx.x & 31;
+  constexpr int W = N < 32 ? N : 32;
+#pragma unroll
+  for (int c0 = 0; c0 < N; c0 += W) {
+    // halves change places: after each step a lane has half as many columns, summed over twice as many lanes
+#pragma unroll
+    for (int w = W / 2; w > 0; w >>= 1) {
+      const bool up = lane & w;
+#pragma unroll
+      for (int i = 0; i < w; ++i) {
+        const float give = up ? v[c0 + i] : v[c0 + i + w], keep = up ? v[c0 + i + w] : v[c0 + i];
+        v[c0 + i] = keep + __shfl_xor_sync(0xffffffffu, give, w);
+      }
+    }
+    float x = v[c0];
+#pragma unroll
+    for (int o = W; o < 32; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (lane < W) dst[c0 + lane] = x;
+  }
+}
+
+// By a warp of a CTA that has given up: the results of its n tiles from place x on say so, also to a caller without a flag word.
+template <int DH, int RB>
+__device__ __forceinline__ void results_are_nan(const Attend8Args& a, Place x, long long n) {
+  const float nan = __int_as_float(0x7fffffff);
+  for (uint32_t seg = 0; n > 0; ++seg) {
+    const int t1 = (int)min((long long)x.nt, x.t + n), tok0 = x.qp * a.block_tok;
+    const int rows = min(a.block_tok, x.s.n - tok0) * a.n_rep;
+    for (int r = threadIdx.x & 31; r < rows; r += 32) {
+      if (x.t == 0 && t1 == x.nt) {
+        const size_t qh = ((size_t)(a.l0 + x.l) * a.n_tok + x.s.f0 + tok0 + r / a.n_rep) * a.H_q + x.g * a.n_rep + r % a.n_rep;
+        for (int c = 0; c < DH; c += 8) *reinterpret_cast<uint4*>(a.out + qh * DH + c) = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (a.lse) a.lse[qh] = nan;
+      } else {                                 // (the merge makes it the whole problem's)
+        a.part_ml[((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * RB + r] = make_float2(nan, nan);
+      }
+    }
+    n -= t1 - x.t;
+    if (n > 0) next_problem(a, x);
+  }
+}
+
+template <int DH, int RB>
+__global__ void __launch_bounds__(kThreads8, 1)
+attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const Attend8Args a) {
+  using namespace ptx;
+  using L = Shape8<DH, RB>;
+  constexpr int NS = L::kSlots, NQ = L::kQ, NP = L::kP;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bars_s[3 * NS + 8];
+  __shared__ uint32_t tmem_s;
+  __shared__ int abort_s;
+  __shared__ Place place_s;
+  __shared__ long long count_s;
+  __shared__ float2 scale_s[NS][8];            // of a tile's pages: keys', values'
+  __shared__ float2 info_s[2][RB];             // of a column: factor of its query, bound that its z may not pass
+  __shared__ __align__(16) float sub_s[2][RB]; // what is taken off z (m)
+  __shared__ float fac_s[2][RB], top_s[2][4][RB], sum_s[2][4][RB];
+  __shared__ uint32_t bad_s[2];                // new rows of the block's tokens with value codes that are NaN
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  constexpr uint32_t kPAt = NS * L::kSlot, kQAt = kPAt + 2 * L::kPBytes;         // ring, weights, queries (high, low)
+  const uint32_t bars = smem_u32(bars_s);
+  const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_sc = b_empty + 8 * NS, b_s = b_sc + 8 * NS, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16, b_drain = b_q + 8;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(b_full + 8 * i, 1);
+      mbar_init(b_empty + 8 * i, 1);
+      mbar_init(b_sc + 8 * i, 32);             // (every lane of the producer reports its copies)
+    }
+    for (int i = 0; i < 2; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_p + 8 * i, 4); mbar_init(b_o + 8 * i, 1); }
+    mbar_init(b_q, 8);
+    mbar_init(b_drain, 1);
+    fence_mbar_init();
+    abort_s = 0;
+  }
+  for (int i = tid; i < 2 * L::kPBytes / 16; i += kThreads8) *reinterpret_cast<uint4*>(gen + kPAt + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+  if (warp == kIssuer8) {
+    tmem_alloc(smem_u32(&tmem_s), L::kTmem);
+    tmem_relinquish();
+  }
+  grid_dependency_wait();                      // everything below may come from the kernel before
+  grid_dependency_launch();                    // (before this CTA is sure to hold tensor memory: the merge, which comes next, takes none)
+  if (warp == kProducer8) {
+    long long count;
+    const Place p = find_piece(a, blockIdx.x, gridDim.x, &count, blockIdx.x == 0);
+    if (lane == 0) { place_s = p; count_s = count; }
+  }
+  tc_fence_before();
   __syncthreads();
-  float m = -INFINITY, sum = 0.0f, acc = 0.0f;
-  for (int j0 = 0; j0 < rows; j0 += kThreads8) {
-    const int j = j0 + tid;
-    float z = -INFINITY, vs = 0.0f;
-    size_t row = 0;
-    if (j < rows) {
-      const int p = a.table[(size_t)lo * a.max_pages + (j >> a.page_shift)];
-      if (p >= 0 && p < a.n_pages) {
-        const size_t head = ((size_t)l * a.n_pages + p) * a.H_kv + g;
-        row = (head << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-        const float ks = power_of_two(a.k_scale[head]);
-        vs = power_of_two(a.v_scale[head]);
-        if (ks > 0.0f && vs > 0.0f) {
-          z = 0.0f;
-          for (int d = 0; d < DH; ++d) z = fmaf(q_s[d], code_value(a.K8[row * DH + d]), z);
-          z *= ks * a.scale2;
-        } else {
-          vs = 0.0f;
+  tc_fence_after();
+  const uint32_t tmem = tmem_s;
+  const Wait wt{&abort_s, a.flags, wait_limit(a.inject)};
+  long long left = count_s;
+  Place p = place_s;
+  uint32_t n_loaded = 0;                       // producer: slots asked for
+
+  if (left > 0 && warp == kProducer8) {
+    const int ppt_shift = 7 - a.page_shift, ppt = 1 << ppt_shift, tpb = 32 >> ppt_shift;       // pages of a tile, tiles of a batch of entries
+    bool ok = !(a.inject & XKV_INJECT_CACHE_NO_LOAD);
+    uint32_t k_tile = 0;
+    while (left > 0 && ok) {
+      const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left);
+      left -= t1 - t0;
+      const int rows = rows_seen(a, p.s, p.qp), pages = min((rows + (1 << a.page_shift) - 1) >> a.page_shift, t1 << ppt_shift);
+      const int32_t* entries = a.table + (size_t)p.b * a.max_pages;
+      auto entry = [&](int t) {                // lane: an entry of the batch that begins with tile t
+        const int i = (t << ppt_shift) + lane;
+        if (i >= pages) return -1;
+        const int e = entries[i];
+        if (e >= 0 && e < a.n_pages) return e;
+        if (a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+        return -1;
+      };
+      int now = 0, next = entry(t0);
+      for (int t = t0; t < t1 && ok; ++t, ++k_tile) {
+        const int in = (t - t0) & (tpb - 1);
+        if (in == 0) { now = next; next = entry(t + tpb); }
+        const int mine = __shfl_sync(0xffffffffu, now, ((in << ppt_shift) + lane) & 31), id = lane < ppt ? mine : -1;
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, id >= 0)) * ((uint32_t)DH << a.page_shift);
+        const size_t head = ((size_t)(a.l0 + p.l) * a.n_pages + (id >= 0 ? id : 0)) * a.H_kv + p.g;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const uint32_t slot = n_loaded % NS, full = b_full + 8 * slot;
+          if (!(ok = wait_warp(wt, b_empty + 8 * slot, ((n_loaded / NS) & 1u) ^ 1u))) break;
+          if (lane == 0) mbar_expect_tx(full, bytes);
+          __syncwarp();
+          if (id >= 0)
+            tma_load_2d(base + slot * L::kSlot + (uint32_t)lane * ((uint32_t)DH << a.page_shift), kv ? &v_map : &k_map, 0, (int)(head << a.page_shift), full);
+          if (kv == 0) {
+            // a tile's scales are read until its values' slot is free, and its keys' slot may be filled again before: a ring of their own
+            if (lane < ppt) {
+              const uint32_t at = smem_u32(&scale_s[k_tile % NS][lane]), n = id >= 0 ? 4u : 0u;
+              cp_async4(at, a.k_scale + head, n);
+              cp_async4(at + 4, a.v_scale + head, n);
+            }
+            cp_async_arrive_noinc(b_sc + 8 * (k_tile % NS));
+          }
+          ++n_loaded;
         }
-      } else {
-        bad = true;
+      }
+      if (left > 0) next_problem(a, p);
+    }
+    __syncwarp();
+  } else if (left > 0 && warp == kIssuer8) {
+    constexpr uint32_t idesc_s = idesc_e4m3_f32(128, NQ), idesc_o = idesc_e4m3_f32(DH, NP) | (1u << 15);     // V is read along its rows
+    const uint64_t ring_desc = smem_desc_rows<DH>(base), q_desc = smem_desc_rows<DH>(base + kQAt), p_desc = smem_desc_rows<128>(base + kPAt);
+    uint32_t k0 = 0, seg = 0;                  // tiles and segments so far
+    bool ok = true;
+    auto full = [&](uint32_t n) { return wait_warp(wt, b_full + 8 * (n % NS), (n / NS) & 1u); };
+    auto logits = [&](uint32_t k) {            // S of tile k, by one thread
+      const uint32_t slot = (2 * k) % NS;
+      const uint64_t kd = ring_desc + (uint64_t)(slot * (uint32_t)(L::kSlot >> 4));
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i)
+          tc_mma_e4m3(tmem + (k & 1u) * NQ, kd + (uint64_t)(2 * i), q_desc + (uint64_t)(h * (L::kQBytes >> 4) + 2 * i), idesc_s, h | i ? 1u : 0u);
+      tc_commit(b_s + 8 * (k & 1u));
+      tc_commit(b_empty + 8 * slot);
+    };
+    while (left > 0 && ok) {
+      const int n = (int)min((long long)p.nt, p.t + left) - p.t;
+      left -= n;
+      ok = wait_warp(wt, b_q, seg & 1u);
+      for (int s = 0; s < min(2, n) && ok; ++s) {
+        if (!(ok = full(2 * (k0 + s)))) break;
+        tc_fence_after();
+        if (elect_one()) logits(k0 + s);
+        __syncwarp();
+      }
+      for (int s = 0; s < n && ok; ++s) {
+        const uint32_t k = k0 + s, w = k & 1u, nv = 2 * k + 1;
+        if (!(ok = wait_warp(wt, b_p + 8 * w, (k >> 1) & 1u))) break;
+        const bool more = s + 2 < n;
+        // S two ahead goes first where its keys are in: the warpgroup waits for it
+        const bool early = more && __all_sync(0xffffffffu, mbar_test(b_full + 8 * ((nv + 3) % NS), ((nv + 3) / NS) & 1u));
+        if (!early && !(ok = full(nv))) break;
+        tc_fence_after();
+        if (early) {
+          if (elect_one()) logits(k + 2);
+          __syncwarp();
+          if (!(ok = full(nv))) break;
+        }
+        if (elect_one()) {
+          const uint64_t vd = ring_desc + (uint64_t)((nv % NS) * (uint32_t)(L::kSlot >> 4)), pd = p_desc + (uint64_t)(w * (uint32_t)(L::kPBytes >> 4));
+#pragma unroll
+          for (int i = 0; i < kTile / 32; ++i)
+            tc_mma_e4m3(tmem + 2 * NQ + w * NP, vd + (uint64_t)(i * (32 * DH >> 4)), pd + (uint64_t)(2 * i), idesc_o, (s >= 2) | (i > 0) ? 1u : 0u);
+          tc_commit(b_o + 8 * w);
+          tc_commit(b_empty + 8 * (nv % NS));
+        }
+        __syncwarp();
+        if (more && !early) {
+          if (!(ok = full(nv + 3))) break;
+          tc_fence_after();
+          if (elect_one()) logits(k + 2);
+          __syncwarp();
+        }
+      }
+      k0 += n;
+      ++seg;
+      if (left > 0 && ok) next_problem(a, p);
+    }
+  } else if (left > 0) {
+    const int wg = warp >> 2, row = tid & 127;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lane_base + (uint32_t)wg * NQ, o_base = tmem + lane_base + 2 * NQ;
+    uint8_t* p_row = gen + kPAt + wg * L::kPBytes + (row & 15);
+    uint32_t k0 = 0, mine = 0, seg = 0;        // tiles so far, those of this warpgroup, segments
+    bool ok = true;
+    while (left > 0 && ok) {
+      const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left), n = t1 - t0;
+      left -= n;
+      const int tok0 = p.qp * a.block_tok, rows = min(a.block_tok, p.s.n - tok0) * a.n_rep;    // query rows
+      const int seen = rows_seen(a, p.s, p.qp), new0 = p.s.base + tok0;                        // row of the block's first token
+      const size_t qh0 = ((size_t)(a.l0 + p.l) * a.n_tok + p.s.f0 + tok0) * a.H_q + (size_t)p.g * a.n_rep;
+      auto row_of = [&](int r) {               // place of query row r in q, out, lse
+        const int tok = (int)(((uint32_t)r * a.rep_inv) >> 16);
+        return qh0 + (size_t)tok * a.H_q + (r - tok * a.n_rep);
+      };
+      // ---- queries: two codes an element; 16-byte units swizzled by the row
+      constexpr int C = DH / 8;                // lanes of a row, eight elements each
+#pragma unroll
+      for (int i0 = 0; i0 < NQ * C; i0 += 256) {
+        const int i = i0 + tid, r = i / C, c = i % C;
+        if (NQ * C < 256 && i >= NQ * C) break;
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows) x = *reinterpret_cast<const uint4*>(a.q + row_of(r) * DH + c * 8);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
+        top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+        for (int o = C / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int ex = max((int)(top >> 7) - 127 - 7, -100);
+        const float f = __int_as_float((127 - ex) << 23);
+        uint32_t hi[2], lo[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint32_t h[2], l[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float x0 = __uint_as_float(w[2 * e + u] << 16) * f, x1 = __uint_as_float(w[2 * e + u] & 0xffff0000u) * f;
+            h[u] = encode_f32x2(x0, x1);
+            const float2 b = __half22float2(decode_f16x2(h[u]));
+            l[u] = encode_f32x2(x0 - b.x, x1 - b.y);
+          }
+          hi[e] = h[0] | (h[1] << 16);
+          lo[e] = l[0] | (l[1] << 16);
+        }
+        if (top >= 0x7f80u) hi[0] = hi[1] = 0x7f7f7f7fu;       // an element is not finite: neither is a logit
+        const int unit = DH == 128 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
+        uint8_t* at = gen + kQAt + r * DH + unit * 16 + (c & 1) * 8;
+        *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
+        *reinterpret_cast<uint2*>(at + L::kQBytes) = make_uint2(lo[0], lo[1]);
+        if (c == 0 && r < RB) {
+          const float qs = __int_as_float((127 + ex) << 23) * a.scale2;
+          info_s[0][r] = info_s[1][r] = make_float2(qs, r < rows ? -INFINITY : INFINITY);      // (nobody's column: no bound)
+          sub_s[0][r] = sub_s[1][r] = 0.0f;
+        }
+      }
+      if (tid < 2) bad_s[tid] = 0u;
+      fence_proxy_async();
+      named_bar_sync(3, 256);
+      if (lane == 0) mbar_arrive(b_q);
+      float l[RB];
+#pragma unroll
+      for (int r = 0; r < RB; ++r) l[r] = 0.0f;
+      bool any = false;                        // this warpgroup has tiles of the segment behind it
+
+      for (int s = (int)((k0 ^ (uint32_t)wg) & 1u); s < n; s += 2) {
+        const uint32_t k = k0 + s;
+        ok = ok && wait_warp(wt, b_s + 8 * wg, mine & 1u) && wait_warp(wt, b_sc + 8 * (k % NS), (k / NS) & 1u);
+        tc_fence_after();
+        float z[RB];
+        load_columns<RB>(s_addr, z);
+        const float2 sc = scale_s[k % NS][row >> a.page_shift];
+        const float ks = __int_as_float(__float_as_int(sc.x) & 0x7f800000);
+        const int ve = (__float_as_int(sc.y) >> 23) & 255;
+        const int j = (t0 + s) * kTile + row;
+        // columns from `from` on see the row
+        const bool dead = j >= seen || !(ks > 0.0f) || ve == 0;
+        const int from = dead ? RB : max(0, min(j - new0, 64) * a.n_rep);
+        const float e = (float)(ve - 127), e_inv = __int_as_float((254 - ve) << 23);
+        bool grow = !ok;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          if (r % 4 == 0 && r >= rows) break;
+          const float2 col = info_s[wg][r];
+          z[r] = fmaf(z[r], ks * col.x, e);
+          z[r] = r >= from ? z[r] : -INFINITY;
+          grow |= z[r] > col.y;
+        }
+        bool waited = false;
+        if (named_bar_any(1 + wg, 128, grow)) {
+          // ---- a weight would pass its bound (or a wait has run out): maxima move
+          if (ok && mine > 0) ok = wait_warp(wt, b_o + 8 * wg, (mine - 1) & 1u);
+          waited = true;
+          if (named_bar_any(1 + wg, 128, !ok)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int r = 0; r < RB; ++r) {
+            if (r % 4 == 0 && r >= rows) break;
+            const int b = __float_as_int(fmaxf(z[r], -INFINITY));              // (NaN counts as minus infinity); as an ordered integer
+            const int m = __reduce_max_sync(0xffffffffu, b ^ ((b >> 31) & 0x7fffffff));
+            if (lane == 0) top_s[wg][warp & 3][r] = __int_as_float(m ^ ((m >> 31) & 0x7fffffff));
+          }
+          named_bar_sync(1 + wg, 128);
+          if (row < RB) {
+            const float m = fmaxf(fmaxf(top_s[wg][0][row], top_s[wg][1][row]), fmaxf(top_s[wg][2][row], top_s[wg][3][row]));
+            float f = 1.0f;
+            if (row < rows && m > info_s[wg][row].y) {
+              const float old = info_s[wg][row].y;
+              f = old == -INFINITY ? 0.0f : exp2f(sub_s[wg][row] - (m - kSet));
+              sub_s[wg][row] = m - kSet;
+              info_s[wg][row].y = m - kSet + kTop;
+            }
+            fac_s[wg][row] = f;
+          }
+          named_bar_sync(1 + wg, 128);
+#pragma unroll
+          for (int r = 0; r < RB; ++r) {
+            if (r % 4 == 0 && r >= rows) break;
+            l[r] *= fac_s[wg][r];
+          }
+          if (any) {
+#pragma unroll 1
+            for (int g = 0; g < 3; ++g) {
+#pragma unroll 1
+              for (int c = 0; c < RB; c += 8) {
+                if (c >= rows) break;
+                const uint32_t at = o_base + (uint32_t)(wg * NP + g * RB + c);
+                float o[8];
+                tmem_ld<8>(at, o);
+                tc_wait_ld();
+                uint32_t x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = __float_as_uint(o[i] * fac_s[wg][c + i]);
+                tmem_st8(at, x);
+              }
+            }
+            tc_wait_st();
+          }
+        }
+        // ---- weights, as three codes each; the product before has to have read the last ones
+        if (ok && !waited && mine > 0) ok = wait_warp(wt, b_o + 8 * wg, (mine - 1) & 1u);
+#pragma unroll
+        for (int r = 0; r < RB; r += 2) {
+          if (r % 4 == 0 && r >= rows) break;
+          const float w0 = ex2_approx(z[r] - sub_s[wg][r]), w1 = ex2_approx(z[r + 1] - sub_s[wg][r + 1]);
+          l[r] = fmaf(w0, e_inv, l[r]);
+          l[r + 1] = fmaf(w1, e_inv, l[r + 1]);
+          const __half2 step = __float2half2_rn(32.0f);
+          __half2 h = __floats2half2_rn(w0, w1);
+#pragma unroll
+          for (int g = 0; g < 3; ++g) {
+            const uint32_t c = encode_f16x2(h);
+            const int n0 = g * RB + r, n1 = n0 + 1;
+            p_row[n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4)] = (uint8_t)c;
+            p_row[n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4)] = (uint8_t)(c >> 8);
+            if (g < 2) h = __hmul2(__hsub2(h, decode_f16x2(c)), step);
+          }
+        }
+        if (__any_sync(0xffffffffu, dead || from > 0)) {
+          // thread = value row: what no column sees is zeroed, NaN is taken out of what only some see, and listed
+          const uint32_t nv = 2 * k + 1;
+          ok = ok && wait_warp(wt, b_full + 8 * (nv % NS), (nv / NS) & 1u);
+          if (ok && (dead || from > 0)) {
+            uint4* v = reinterpret_cast<uint4*>(gen + (nv % NS) * L::kSlot + row * DH);      // (the order of its units does not matter)
+            uint32_t hit = 0;
+#pragma unroll
+            for (int c = 0; c < DH / 16; ++c) {
+              uint4 x = dead || from >= rows ? make_uint4(0u, 0u, 0u, 0u) : v[c];
+              const uint4 m = make_uint4(nan_codes(x.x), nan_codes(x.y), nan_codes(x.z), nan_codes(x.w));
+              hit |= m.x | m.y | m.z | m.w;
+              v[c] = make_uint4(x.x & ~m.x, x.y & ~m.y, x.z & ~m.z, x.w & ~m.w);
+            }
+            if (hit) atomicOr(&bad_s[(j - new0) >> 5], 1u << ((j - new0) & 31));
+          }
+        }
+        fence_proxy_async();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0 && ok && !(a.inject & XKV_INJECT_CACHE_NO_HANDOVER)) mbar_arrive(b_p + 8 * wg);
+        ++mine;
+        any = true;
+      }
+      // ---- the segment's result: both warpgroups meet (a warp whose wait has run out comes here, too)
+      if (ok && any) ok = wait_warp(wt, b_o + 8 * wg, (mine - 1) & 1u);
+      tc_fence_after();
+      sum_columns<RB>(l, sum_s[wg][warp & 3]);
+      if (named_bar_any(3, 256, !ok)) { ok = false; break; }
+      const bool whole = t0 == 0 && t1 == p.nt;
+      const bool has0 = n > (int)(k0 & 1u), has1 = n > (int)((k0 ^ 1u) & 1u);    // does a warpgroup have tiles of this segment?
+      const int d = DH == 128 ? row : (warp & 3) * 16 + lane;
+      const bool owns = DH == 128 || lane < 16;
+      const size_t pr = ((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * RB;
+      constexpr int HALF = RB / 2;
+#pragma unroll 1
+      for (int c0 = wg * HALF; c0 < (wg + 1) * HALF; c0 += 4) {
+        if (c0 >= rows) break;
+        float o[2][3][4];
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int g = 0; g < 3; ++g) tmem_ld<4>(o_base + (uint32_t)(w * NP + g * RB + c0), o[w][g]);
+        tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = c0 + i;
+          if (r >= rows) break;
+          // a warpgroup's maxima; what it has not seen counts nothing
+          const float m0 = info_s[0][r].y == -INFINITY ? -INFINITY : sub_s[0][r], m1 = info_s[1][r].y == -INFINITY ? -INFINITY : sub_s[1][r];
+          const float M = fmaxf(m0, m1);
+          const float f0 = !has0 ? 0.0f : m0 == M ? 1.0f : exp2f(m0 - M), f1 = !has1 ? 0.0f : m1 == M ? 1.0f : exp2f(m1 - M);
+          float x = 0.0f, sum = 0.0f;
+          if (has0) {
+            x = f0 * (o[0][0][i] + 0x1p-5f * (o[0][1][i] + 0x1p-5f * o[0][2][i]));
+            sum = f0 * (sum_s[0][0][r] + sum_s[0][1][r] + sum_s[0][2][r] + sum_s[0][3][r]);
+          }
+          if (has1) {
+            x += f1 * (o[1][0][i] + 0x1p-5f * (o[1][1][i] + 0x1p-5f * o[1][2][i]));
+            sum += f1 * (sum_s[1][0][r] + sum_s[1][1][r] + sum_s[1][2][r] + sum_s[1][3][r]);
+          }
+          uint32_t bad0 = bad_s[0], bad1 = bad_s[1];
+          while (owns && (bad0 | bad1)) {      // rows that were taken out, given back to the columns that see them
+            const int tok = bad0 ? __ffs(bad0) - 1 : 31 + __ffs(bad1);
+            if (bad0) bad0 &= bad0 - 1u; else bad1 &= bad1 - 1u;
+            if (tok * a.n_rep > r) continue;
+            const int jj = new0 + tok, page = a.table[(size_t)p.b * a.max_pages + (jj >> a.page_shift)];
+            const size_t head = ((size_t)(a.l0 + p.l) * a.n_pages + page) * a.H_kv + p.g;
+            if ((a.V8[((head << a.page_shift) + (jj & ((1 << a.page_shift) - 1))) * DH + d] & 0x7f) == 0x7f) x = __int_as_float(0x7fffffff);
+          }
+          if (whole) {
+            const size_t qh = row_of(r);
+            if (owns) a.out[qh * DH + d] = __float2bfloat16_rn(sum == 0.0f ? 0.0f : x / sum);
+            if (row == 0 && a.lse) a.lse[qh] = sum == 0.0f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
+          } else {
+            if (owns) a.part[(pr + r) * DH + d] = x;
+            if (row == 0) a.part_ml[pr + r] = make_float2(M, sum);
+          }
+        }
+      }
+      tc_fence_before();
+      k0 += n;
+      ++seg;
+      if (left > 0) {
+        next_problem(a, p);
+        named_bar_sync(3, 256);                // the next problem's columns go where the other warpgroup may still be reading
       }
     }
-    float top = z;
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (lane == 0) red_s[0][warp] = top;
-    __syncthreads();
-    const float m_new = fmaxf(m, fmaxf(fmaxf(red_s[0][0], red_s[0][1]), fmaxf(red_s[0][2], red_s[0][3])));
-    const float shift = m_new == -INFINITY ? 0.0f : m_new;
-    const float p = vs > 0.0f ? exp2f(z - shift) : 0.0f;
-    p_s[tid] = p;
-    float part = p;
-    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
-    if (lane == 0) red_s[1][warp] = part;
-    __syncthreads();
-    const float f = m == -INFINITY ? 0.0f : exp2f(m - shift);
-    sum = sum * f + (red_s[1][0] + red_s[1][1] + red_s[1][2] + red_s[1][3]);
-    acc *= f;
-    m = m_new;
-    if (tid < DH) {
-      for (int i = 0; i < min(kThreads8, rows - j0); ++i) {
-        const int p2 = a.table[(size_t)lo * a.max_pages + ((j0 + i) >> a.page_shift)];
-        if (p2 < 0 || p2 >= a.n_pages) continue;
-        const size_t head = ((size_t)l * a.n_pages + p2) * a.H_kv + g;
-        const float v2 = power_of_two(a.v_scale[head]);
-        if (!(v2 > 0.0f) || !(power_of_two(a.k_scale[head]) > 0.0f)) continue;
-        acc = fmaf(p_s[i], code_value(a.V8[((head << a.page_shift) + ((j0 + i) & ((1 << a.page_shift) - 1))) * DH + tid]) * v2, acc);
-      }
+  }
+
+  // wind down: nothing of this CTA may still touch shared or tensor memory
+  tc_fence_before();
+  __syncthreads();
+  if (abort_s) {                               // given up: nothing may still write tensor memory when it is freed
+    if (warp == kIssuer8) {
+      if (elect_one()) tc_commit(b_drain);
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(b_drain, 0))) break;
     }
     __syncthreads();
   }
-  if (tid < DH) a.out[qh * DH + tid] = __float2bfloat16_rn(sum == 0.0f ? 0.0f : acc / sum);
-  if (tid == 0 && a.lse) a.lse[qh] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
-  if (bad && a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+  if (warp == kIssuer8) {
+    tc_fence_after();
+    tmem_dealloc(tmem, L::kTmem);
+  }
+  if (abort_s && warp == kProducer8) {
+    // given up: tiles may still be on their way into this CTA's shared memory; stay (with a limit) for them
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (uint32_t n = n_loaded > NS ? n_loaded - NS : 0u; n < n_loaded; ++n)
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(b_full + 8 * (n % NS), (n / NS) & 1u))) break;
+    results_are_nan<DH, RB>(a, place_s, count_s);
+  }
+}
+
+// Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A warp has one query row, lane = d_h / 32 columns.
+template <int DH, int RB>
+__global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const Attend8Args a, int attend_grid) {
+  constexpr int V = DH / 32, AT_ONCE = 16;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int i0 = blockIdx.x * kMergeWarps8 + warp, t = i0 / a.H_q, hq = i0 - t * a.H_q, l = blockIdx.y;
+  const int g = hq / a.n_rep;
+  // Lengths come from before the kernel that this one waits for, which had waited for them before it let this one start: they are read
+  // while that kernel runs.
+  bool live = t < a.n_tok, bad;
+  int b = live ? t : 0;
+  if (a.first && live) {                       // the sequence of token t
+    int lo = 0, hi = a.batch - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (a.first[mid + 1] > t) hi = mid; else lo = mid + 1;
+    }
+    b = lo;
+  }
+  const Seq s = load_seq(a, b, &bad);
+  const int tok = t - s.f0;
+  live = live && tok >= 0 && tok < s.n;
+  long long before;
+  const long long head = head_tiles(a, b, &before), total = head * a.H_kv * a.layers;
+  const int ctas = (int)min((long long)attend_grid, total);
+  int c0 = 0, c1 = 0, r = 0;
+  long long u0 = 0;
+  if (live) {
+    const int qp = tok / a.block_tok;
+    r = (tok - qp * a.block_tok) * a.n_rep + (hq - g * a.n_rep);
+    u0 = ((long long)l * a.H_kv + g) * head + before + tiles_before(a, s, qp, blocks_of(a, s));
+    c0 = piece_of8(total, ctas, u0);
+    c1 = piece_of8(total, ctas, u0 + tiles_of(rows_seen(a, s, qp)) - 1);
+  }
+  ptx::grid_dependency_wait();                 // the pieces come from the kernel before; every CTA waits, so that who waits for this
+  ptx::grid_dependency_launch();               // kernel has waited for that one
+  if (c0 == c1) return;                        // one piece: written where it was computed
+  // a problem that begins inside a piece is that piece's last one, and in the others the first
+  const size_t first = (size_t)c0 * 2 + (piece_begin8(total, ctas, c0) == u0 ? 0 : 1);
+  auto slot = [&](int c) { return (c == c0 ? first : (size_t)c * 2) * RB + r; };
+  float M = -INFINITY, sum = 0.0f, acc[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+  for (int cb = c0; cb <= c1; cb += 32) {      // lane: the weight of one piece of 32
+    const int n = min(32, c1 - cb + 1);
+    float x[AT_ONCE][V];
+    auto load = [&](int j0) {
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const float* src = a.part + slot(cb + min(j0 + j, n - 1)) * DH + lane * V;
+        if constexpr (V == 4) *reinterpret_cast<float4*>(x[j]) = *reinterpret_cast<const float4*>(src);
+        else *reinterpret_cast<float2*>(x[j]) = *reinterpret_cast<const float2*>(src);
+      }
+    };
+    const float2 ml = lane < n ? a.part_ml[slot(cb + lane)] : make_float2(-INFINITY, 0.0f);
+    load(0);                                   // (asked for before the weights are known)
+    float top = ml.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float M_new = fmaxf(M, top), old = M == -INFINITY ? 1.0f : exp2f(M - M_new);
+    const float f = ml.x == -INFINITY ? (ml.y == 0.0f ? 0.0f : 1.0f) : exp2f(ml.x - M_new);    // (a piece of NaNs stays one)
+    M = M_new;
+    float part = f * ml.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+    sum = fmaf(sum, old, part);
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] *= old;
+    for (int j0 = 0; j0 < n; j0 += AT_ONCE) {
+      if (j0 > 0) load(j0);
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const float w = __shfl_sync(0xffffffffu, f, (j0 + j) & 31);
+        if (j0 + j < n && w != 0.0f) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) acc[i] = fmaf(w, x[j][i], acc[i]);
+        }
+      }
+    }
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const size_t qh = ((size_t)(a.l0 + l) * a.n_tok + t) * a.H_q + hq;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + qh * DH + lane * V);
+#pragma unroll
+  for (int i = 0; i < V; i += 2) dst[i / 2] = ptx::pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+  if (a.lse && lane == 0) a.lse[qh] = sum == 0.0f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
+}
+
+template <int DH, int RB>
+cudaError_t launch_as(const CUtensorMap& k_map, const CUtensorMap& v_map, const Attend8Args& a, int grid, int device, cudaStream_t s) {
+  cudaError_t e = ensure_dyn_smem<attend8_kernel<DH, RB>>(Shape8<DH, RB>::kBytes, device);
+  if (e == cudaSuccess) e = launch_pdl(attend8_kernel<DH, RB>, dim3(grid), dim3(kThreads8), Shape8<DH, RB>::kBytes, s, k_map, v_map, a);
+  if (e != cudaSuccess) return e;
+  const long long rows = (long long)a.n_tok * a.H_q;
+  e = launch_pdl(attend8_merge_kernel<DH, RB>, dim3((unsigned)((rows + kMergeWarps8 - 1) / kMergeWarps8), a.layers), dim3(kMergeWarps8 * 32), 0, s, a, grid);
+  count_launch(kFamAttend8, 2);
+  return e;
+}
+
+// Query rows of a block: as few as hold the tokens of the longest sequence.
+int block_rows(int max_new, int n_rep) {
+  const long long rows = (long long)max_new * n_rep;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
 }  // namespace
 
-size_t cache8_workspace_bytes(const xkv_cache8_config* c, int max_new) { return 16; }
+// A piece leaves at most two results: its first and its last problem.
+size_t cache8_workspace_bytes(const xkv_cache8_config* c, int max_new) {
+  return (size_t)kPlanSms * 2 * block_rows(max_new, c->H_q / c->H_kv) * (c->d_h + 2) * sizeof(float);
+}
 
 cudaError_t launch_cache8_attend(const xkv_cache8_config* c, int l0, int l1, const __nv_bfloat16* q, const int32_t* first, int n_tok,
                                  int max_new, const int32_t* table, const int32_t* length, const void* K8, const void* V8,
                                  const float* k_scale, const float* v_scale, void* workspace, __nv_bfloat16* out, float* lse,
                                  unsigned int* flags, int device, cudaStream_t s) {
+  CUtensorMap k_map, v_map;
+  const uint64_t rows = (uint64_t)c->G * c->n_pages * c->H_kv * c->page;
+  if (!encode_byte_map(&k_map, K8, rows, c->d_h, c->page) || !encode_byte_map(&v_map, V8, rows, c->d_h, c->page)) return cudaErrorInvalidValue;
+  int sms = 0;
+  const cudaError_t e = device_sms(device, &sms);
+  if (e != cudaSuccess) return e;
   Attend8Args a;
   a.batch = c->batch; a.H_kv = c->H_kv; a.H_q = c->H_q; a.n_rep = c->H_q / c->H_kv; a.n_pages = c->n_pages; a.max_pages = c->max_pages;
   a.page_shift = __builtin_ctz((unsigned)c->page);
-  a.n_tok = n_tok; a.max_new = max_new; a.l0 = l0;
+  a.n_tok = n_tok; a.max_new = max_new; a.l0 = l0; a.layers = l1 - l0;
+  const int rb = block_rows(max_new, a.n_rep);
+  a.block_tok = rb / a.n_rep;
+  a.rep_inv = (65536u + a.n_rep - 1u) / a.n_rep;
   a.scale2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / sqrtf((float)c->d_h)) * kLog2e;
-  a.q = q; a.first = first; a.table = table; a.length = length; a.K8 = (const uint8_t*)K8; a.V8 = (const uint8_t*)V8;
+  a.q = q; a.first = first; a.table = table; a.length = length; a.V8 = (const uint8_t*)V8;
   a.k_scale = k_scale; a.v_scale = v_scale; a.out = out; a.lse = lse; a.flags = flags;
-  const dim3 grid(n_tok, c->H_q, l1 - l0);
-  const cudaError_t e = c->d_h == 128 ? launch_pdl(attend8_plain_kernel<128>, grid, dim3(kThreads8), 0, s, a)
-                                      : launch_pdl(attend8_plain_kernel<64>, grid, dim3(kThreads8), 0, s, a);
-  count_launch(kFamAttend8);
-  return e;
+  a.inject = cache_fault_injection();
+  const int grid = sms < kPlanSms ? sms : kPlanSms;
+  a.part = (float*)workspace;
+  a.part_ml = reinterpret_cast<float2*>(a.part + (size_t)kPlanSms * 2 * rb * c->d_h);
+  if (c->d_h == 128)
+    return rb == 8 ? launch_as<128, 8>(k_map, v_map, a, grid, device, s) : rb == 16 ? launch_as<128, 16>(k_map, v_map, a, grid, device, s)
+         : rb == 32 ? launch_as<128, 32>(k_map, v_map, a, grid, device, s) : launch_as<128, 64>(k_map, v_map, a, grid, device, s);
+  return rb == 8 ? launch_as<64, 8>(k_map, v_map, a, grid, device, s) : rb == 16 ? launch_as<64, 16>(k_map, v_map, a, grid, device, s)
+       : rb == 32 ? launch_as<64, 32>(k_map, v_map, a, grid, device, s) : launch_as<64, 64>(k_map, v_map, a, grid, device, s);
 }
 
 }  // namespace xkv

@@ -173,6 +173,9 @@ bool encode_landmark_map(void* out, const void* base, uint64_t rows, uint64_t co
 // the same for a general bf16 matrix [rows][cols] with a row pitch (elements) and box_rows-row boxes of 64 columns
 bool encode_bf16_map(void* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows);
 
+// a matrix of bytes [rows][cols], cols 64 or 128, in boxes of whole rows
+bool encode_byte_map(void* out, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+
 // xkv_attend.cu
 size_t attend_part_floats(const xkv_group* grp);
 cudaError_t launch_reconstruct_attend(const xkv_group* grp, int l0, int l1, const __nv_bfloat16* q,
