@@ -200,9 +200,14 @@ cudaError_t launch_cache8_append(const xkv_cache8_config* c, int l0, int l1, con
                                  cudaStream_t s) {
   CodesArgs a = codes_args(c, l0, l1, K8, V8, k_scale, v_scale, flags);
   a.x[0] = k; a.x[1] = v; a.slot = slot; a.n_tok = n_tok;
-  a.per_group = 1;
+  // A group looks after one token as long as that gives two waves of CTAs at most (decode: every token is a run of its own, and runs
+  // of a group come one after the other), then after up to 32: most of a prompt's tokens begin no run.
   const int groups = kAppendThreads / 32 / (c->page / kRunRows);
-  const dim3 grid((n_tok + groups * a.per_group - 1) / (groups * a.per_group), c->H_kv, 2 * a.layers);
+  const long long per_token = (long long)c->H_kv * 2 * a.layers;
+  auto ctas = [&](int per_group) { return (n_tok + groups * per_group - 1) / (groups * per_group); };
+  a.per_group = 1;
+  while (a.per_group < 32 && ctas(a.per_group) * per_token > kPlanSms * 16) a.per_group *= 2;
+  const dim3 grid(ctas(a.per_group), c->H_kv, 2 * a.layers);
   const cudaError_t e = c->d_h == 128 ? launch_pdl(append_kernel<2>, grid, dim3(kAppendThreads), 0, s, a)
                                       : launch_pdl(append_kernel<1>, grid, dim3(kAppendThreads), 0, s, a);
   count_launch(kFamCodes);
