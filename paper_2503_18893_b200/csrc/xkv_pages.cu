@@ -12,6 +12,7 @@ namespace xkv {
 namespace {
 
 constexpr int kSeqs = 1024;                    // threads, and sequences of a block
+constexpr int kRanks = 8;                      // CTAs of a cluster, where there are many tokens
 
 struct PageArgs {
   int batch, page_shift, n_pages, max_pages, n_tok;
@@ -61,90 +62,87 @@ __device__ __forceinline__ Sums prefix(Sums v, Sums* warps_s, Sums* total) {
   return v;
 }
 
+// The last of 1024 sequences that begins at or before i: upto_s[x] <= i < upto_s[x + 1].
+__device__ __forceinline__ int sequence_of(const int* upto_s, int i) {
+  int lo = 0, hi = kSeqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (upto_s[mid + 1] > i) hi = mid; else lo = mid + 1;
+  }
+  return lo;
+}
+
+// A cluster: every CTA forms the sums of a block for itself, then they deal out its pages and tokens among them.
 __global__ void __launch_bounds__(kSeqs) page_assign_kernel(const PageArgs a) {
   __shared__ Sums warps_s[32];
-  __shared__ int held_s[kSeqs], fresh_s[kSeqs + 1];            // rows before the call; new tokens of the sequences before, in the block
-  __shared__ uint8_t ok_s[kSeqs];
+  // of the block's sequences: rows before the call (-1 - rows: it got no pages); pages taken, given back, and new tokens of those before
+  __shared__ int held_s[kSeqs], want_s[kSeqs], take_s[kSeqs + 1], give_s[kSeqs + 1], fresh_s[kSeqs + 1];
   __shared__ int taken_s, bad_s;
-  const int tid = threadIdx.x, lane = tid & 31;
+  const int tid = threadIdx.x, rank = blockIdx.x, ranks = gridDim.x;
   const int page = 1 << a.page_shift, most = a.max_pages << a.page_shift;
-  if (tid == 0) { taken_s = 0; bad_s = 0; }
+  if (tid == 0) { taken_s = 0; bad_s = 0; take_s[0] = give_s[0] = fresh_s[0] = 0; }
   ptx::grid_dependency_wait();
   ptx::grid_dependency_launch();
   int head = a.state[0], count = a.state[1];
+  bool bad = false;
   if (head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages) {
     head = count = 0;
-    if (tid == 0) bad_s = 1;
+    bad = true;
   }
   const int room = a.n_pages - count;          // places of the ring that hold no free page
+  auto place = [&](long long i) { return (int)((head + i) % a.n_pages); };
   long long take0 = 0, give0 = 0, fresh0 = 0;  // of the blocks before
-  __syncthreads();
   for (int b0 = 0; b0 < a.batch; b0 += kSeqs) {
     const int b = b0 + tid;
     int held = 0, want = 0;
-    bool bad = false;
     if (b < a.batch) {
       const int h = a.held[b], w = a.want[b];
       held = min(max(h, 0), most);
       want = min(max(w, 0), most);
-      bad = h != held || w != want;
+      bad |= h != held || w != want;
     }
     const int have = (held + page - 1) >> a.page_shift, need = (want + page - 1) >> a.page_shift;
     const Sums mine = {max(need - have, 0), max(have - need, 0), (long long)max(want - held, 0)};
     Sums all;
     const Sums upto = prefix(mine, warps_s, &all);
     const bool ok = mine.take == 0 || take0 + upto.take <= count;
-    if (b < a.batch) {
+    if (mine.take > 0 && ok) atomicMax(&taken_s, (int)(take0 + upto.take));
+    held_s[tid] = ok ? held : -1 - held;
+    want_s[tid] = want;
+    take_s[tid + 1] = upto.take;
+    give_s[tid + 1] = upto.give;
+    fresh_s[tid + 1] = (int)min(upto.fresh, 0x7fffffffll);
+    // every CTA has read what is overwritten now (`length` may be `held` or `want`)
+    ptx::cluster_sync();
+    if (rank == 0 && b < a.batch) {
+      const long long f = fresh0 + upto.fresh - mine.fresh, e = fresh0 + upto.fresh;
       if (a.first) {
-        const long long f = fresh0 + upto.fresh - mine.fresh, e = fresh0 + upto.fresh;
         a.first[b] = (int)min(f, 0x7fffffffll);
         if (b == a.batch - 1) a.first[a.batch] = (int)min(e, 0x7fffffffll);
-        if (e > 0x7fffffffll) bad = true;
+        bad |= e > 0x7fffffffll;
       }
       a.length[b] = ok ? want : held;
     }
-    // pages, by whole warps: a sequence after the other
-    const int took = ok ? mine.take : 0;
-    const int from = (int)((head + take0 + upto.take - mine.take) % a.n_pages);
-    const long long back = give0 + upto.give - mine.give;      // of those before this sequence
-    const int to = (int)((head + count + back) % a.n_pages);
-    const long long left = room - back;
-    if (mine.take > 0 && ok) atomicMax(&taken_s, (int)(take0 + upto.take));
-    if (mine.give > 0 && left < mine.give) bad = true;
-    for (unsigned todo = __ballot_sync(0xffffffffu, took > 0 || mine.give > 0); todo; todo &= todo - 1u) {
-      const int src = __ffs(todo) - 1;
-      const int n_take = __shfl_sync(0xffffffffu, took, src), n_give = __shfl_sync(0xffffffffu, mine.give, src);
-      const int at = __shfl_sync(0xffffffffu, n_take > 0 ? from : to, src);
-      const int row = __shfl_sync(0xffffffffu, n_take > 0 ? have : need, src);
-      const long long free_places = __shfl_sync(0xffffffffu, left, src);
-      int32_t* entry = a.table + (size_t)(b - lane + src) * a.max_pages + row;
-      for (int i = lane; i < n_take + n_give; i += 32) {
-        const int p = (int)(((long long)at + i) % a.n_pages);
-        if (n_take > 0) {
-          entry[i] = a.ring[p];
-        } else {
-          if (i < free_places) a.ring[p] = entry[i];
-          entry[i] = -1;
-        }
-      }
+    for (int i = rank * kSeqs + tid; i < all.take; i += ranks * kSeqs) {       // pages taken
+      const int x = sequence_of(take_s, i), h = held_s[x];
+      if (h >= 0) a.table[(size_t)(b0 + x) * a.max_pages + ((h + page - 1) >> a.page_shift) + i - take_s[x]] = a.ring[place(take0 + i)];
     }
-    held_s[tid] = held;
-    fresh_s[tid + 1] = (int)min(upto.fresh, 0x7fffffffll);
-    if (tid == 0) fresh_s[0] = 0;
-    ok_s[tid] = ok;
-    __syncthreads();                           // (taken pages are in the table for the whole CTA, too)
+    for (int i = rank * kSeqs + tid; i < all.give; i += ranks * kSeqs) {       // pages given back
+      const int x = sequence_of(give_s, i);
+      int32_t* entry = a.table + (size_t)(b0 + x) * a.max_pages + ((want_s[x] + page - 1) >> a.page_shift) + i - give_s[x];
+      if (give0 + i < room) a.ring[place(count + give0 + i)] = *entry;
+      else bad = true;
+      *entry = -1;
+    }
     if (a.slot) {
       const int n = (int)max(0ll, min(all.fresh, (long long)a.n_tok - fresh0));
-      for (int t = tid; t < n; t += kSeqs) {
-        int lo = 0, hi = kSeqs - 1;            // the last sequence that begins at or before t: fresh_s[lo] <= t < fresh_s[lo + 1]
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (fresh_s[mid + 1] > t) hi = mid; else lo = mid + 1;
-        }
-        const int pos = held_s[lo] + t - fresh_s[lo];
+      for (int t = rank * kSeqs + tid; t < n; t += ranks * kSeqs) {
+        const int x = sequence_of(fresh_s, t), h = held_s[x], held_x = h >= 0 ? h : -1 - h, pos = held_x + t - fresh_s[x];
         int slot = -1;
-        if (ok_s[lo]) {
-          const int p = a.table[(size_t)(b0 + lo) * a.max_pages + (pos >> a.page_shift)];
+        if (h >= 0) {
+          // a page that was taken just now is still in the ring, in whatever order the table is written
+          const int i = pos >> a.page_shift, fresh = i - ((held_x + page - 1) >> a.page_shift);
+          const int p = fresh >= 0 ? a.ring[place(take0 + take_s[x] + fresh)] : a.table[(size_t)(b0 + x) * a.max_pages + i];
           if (p >= 0 && p < a.n_pages) slot = (p << a.page_shift) + (pos & (page - 1));
           else bad = true;
         }
@@ -152,21 +150,22 @@ __global__ void __launch_bounds__(kSeqs) page_assign_kernel(const PageArgs a) {
         a.slot[fresh0 + t] = slot;
       }
     }
-    if (bad) bad_s = 1;
     take0 += all.take;
     give0 += all.give;
     fresh0 += all.fresh;
     __syncthreads();
   }
   if (a.slot) {
-    for (long long t = fresh0 + tid; t < a.n_tok; t += kSeqs) { a.pos[t] = 0; a.slot[t] = -1; }
-    if (tid == 0 && fresh0 > a.n_tok) bad_s = 1;
+    for (long long t = fresh0 + rank * kSeqs + tid; t < a.n_tok; t += ranks * kSeqs) { a.pos[t] = 0; a.slot[t] = -1; }
+    bad |= fresh0 > a.n_tok;
   }
+  if (bad) bad_s = 1;
   __syncthreads();
   if (tid == 0) {
-    const long long joined = min(give0, (long long)room);
-    a.state[0] = (int)(((long long)head + taken_s) % a.n_pages);
-    a.state[1] = count - taken_s + (int)joined;
+    if (rank == 0) {
+      a.state[0] = place(taken_s);
+      a.state[1] = count - taken_s + (int)min(give0, (long long)room);
+    }
     if (bad_s && a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
   }
 }
@@ -181,7 +180,20 @@ cudaError_t launch_page_assign(const xkv_cache8_config* c, const int32_t* held, 
   a.page_shift = __builtin_ctz((unsigned)c->page);
   a.held = held; a.want = want; a.table = table; a.ring = ring; a.state = state; a.first = first; a.length = length;
   a.pos = pos; a.slot = slot; a.flags = flags;
-  const cudaError_t e = launch_pdl(page_assign_kernel, dim3(1), dim3(kSeqs), 0, s, a);
+  const int ranks = n_tok > 2 * kSeqs ? kRanks : 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ranks);
+  cfg.blockDim = dim3(kSeqs);
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = ranks;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, page_assign_kernel, a);
   count_launch(kFamPages);
   return e;
 }
