@@ -15,8 +15,7 @@
 // A key's scale multiplies the row's logits.  A value's scale 2^e joins the exponent: w_j = 2^(z_j + e_j - m), so that codes meet weights
 // that hold their scale, and m is the maximum of z_j + e_j; the denominator sums w_j 2^-e_j in fp32.
 //
-//   producer  a page is one box of the copy engine: lane i of the warp has the i-th page of a tile, its entry of the table and its scales
-//             (asynchronous copies of four bytes, which report to the same barrier as the codes)
+//   producer  pages by the copy engine, with their scales (Ring8)
 //   issuer    S of a tile two ahead, O of this one
 //   softmax   two warpgroups, tile by tile in turns, each with its own maxima, sums and O; thread = row of the cache, so that a token's
 //             view (rows up to its own) is a comparison of the column with one number per thread.  Maxima move only when a weight would
@@ -26,9 +25,7 @@
 #include <cuda.h>
 #include <math.h>
 
-#include <cuda_fp16.h>
-
-#include "xkv_cache.cuh"
+#include "xkv_attend8.cuh"
 
 namespace xkv {
 
@@ -38,194 +35,6 @@ constexpr int kThreads8 = 320;                 // two warpgroups, producer, issu
 constexpr int kProducer8 = 8, kIssuer8 = 9;
 constexpr int kMergeWarps8 = 8;
 constexpr float kTop = 8.0f, kSet = 4.0f;      // log2: a weight's bound; where a column's largest weight is put
-
-struct Attend8Args {
-  int batch, H_kv, H_q, n_rep, n_pages, max_pages, page_shift, n_tok, max_new, l0, layers;
-  int block_tok;                               // tokens of a block of query rows
-  uint32_t rep_inv;                            // ceil(2^16 / n_rep)
-  float scale2;                                // softmax scale times log2(e)
-  const __nv_bfloat16* q;
-  const int32_t* first;
-  const int32_t* table;
-  const int32_t* length;
-  const uint8_t* V8;                           // (codes that are NaN)
-  const float* k_scale;
-  const float* v_scale;
-  float* part;                                 // [CTA][2][rows of a block][d_h]
-  float2* part_ml;                             // [CTA][2][rows of a block] (m, l)
-  __nv_bfloat16* out;
-  float* lse;
-  unsigned int* flags;
-  unsigned int inject;                         // XKV_INJECT_CACHE_* bits; 0 in normal use
-};
-
-// A sequence: its first token, how many of its tokens are looked after, its rows, and those before its first new one (below zero if
-// it has more new tokens than rows).
-struct Seq {
-  int f0, n, base, len;
-};
-__device__ __forceinline__ Seq load_seq(const Attend8Args& a, int b, bool* bad) {
-  const int w0 = a.first ? a.first[b] : b, w1 = a.first ? a.first[b + 1] : b + 1, wl = a.length[b];
-  const int f0 = min(max(w0, 0), a.n_tok), f1 = min(max(w1, f0), a.n_tok), len = min(max(wl, 0), a.max_pages << a.page_shift);
-  *bad = f0 != w0 || f1 != w1 || len != wl || f1 - f0 > a.max_new;
-  return Seq{f0, min(f1 - f0, a.max_new), len - (f1 - f0), len};
-}
-__device__ __forceinline__ int blocks_of(const Attend8Args& a, const Seq& s) { return (s.n + a.block_tok - 1) / a.block_tok; }
-// Rows that the last token of block qp sees, and the tiles that they lie in (one for tokens that see nothing: it says so).
-__device__ __forceinline__ int rows_seen(const Attend8Args& a, const Seq& s, int qp) {
-  return min(max(s.base + min(s.n, (qp + 1) * a.block_tok), 0), s.len);
-}
-__device__ __forceinline__ int tiles_of(int rows) { return max(1, (rows + kTile - 1) / kTile); }
-
-// sum over i < n of floor((a i + b) / m), all of them non-negative: Euclid's algorithm on (a, m).
-__device__ long long floor_sum(long long n, long long m, long long a, long long b) {
-  long long sum = 0;
-  while (n > 0) {
-    if (a >= m) { sum += n * (n - 1) / 2 * (a / m); a %= m; }
-    if (b >= m) { sum += n * (b / m); b %= m; }
-    const long long y = a * n + b;
-    if (y < m) break;
-    n = y / m;
-    b = y % m;
-    const long long t = m;
-    m = a;
-    a = t;
-  }
-  return sum;
-}
-// Tiles of one head in blocks 0 .. qp-1 of a sequence of n_qp blocks; those before the last are full: their rows grow by block_tok.
-__device__ long long tiles_before(const Attend8Args& a, const Seq& s, int qp, int n_qp) {
-  if (qp == 0) return 0;
-  if (qp == n_qp) return tiles_before(a, s, qp - 1, n_qp) + tiles_of(rows_seen(a, s, qp - 1));
-  const int most = kTile - s.base;             // blocks that see up to one tile count one
-  const int ones = most > 0 ? min(qp, most / a.block_tok) : 0;
-  return ones + floor_sum(qp - ones, kTile, a.block_tok, s.base + (long long)(ones + 1) * a.block_tok + kTile - 1);
-}
-__device__ __forceinline__ long long tiles_of_head(const Attend8Args& a, const Seq& s) {
-  if (s.n <= a.block_tok) return s.n > 0 ? tiles_of(rows_seen(a, s, 0)) : 0;
-  const int n_qp = blocks_of(a, s);
-  return tiles_before(a, s, n_qp, n_qp);
-}
-
-// A place in the list of tiles.  Order: layer, head, sequence, block, tile.
-struct Place {
-  int l, g, b, qp, t, nt, n_qp;
-  Seq s;
-};
-__device__ __forceinline__ void set_block(const Attend8Args& a, Place& p) { p.nt = tiles_of(rows_seen(a, p.s, p.qp)); }
-// Moves to the next problem (there is one: the caller counts).
-__device__ __forceinline__ void next_problem(const Attend8Args& a, Place& p) {
-  p.t = 0;
-  if (++p.qp >= p.n_qp) {
-    p.qp = 0;
-    do {
-      if (++p.b == a.batch) {
-        p.b = 0;
-        if (++p.g == a.H_kv) { p.g = 0; ++p.l; }
-      }
-      bool bad;
-      p.s = load_seq(a, p.b, &bad);
-      p.n_qp = blocks_of(a, p.s);
-    } while (p.n_qp == 0 && p.l < a.layers);
-  }
-  set_block(a, p);
-}
-
-__device__ __forceinline__ long long warp_sum(long long v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-// Lane: tiles of one head in sequence b0 + lane.
-__device__ __forceinline__ long long lane_tiles(const Attend8Args& a, int b0, Seq* s, bool report) {
-  const int b = b0 + (int)(threadIdx.x & 31);
-  if (b >= a.batch) return 0;
-  bool bad;
-  *s = load_seq(a, b, &bad);
-  if (bad && report && a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
-  return tiles_of_head(a, *s);
-}
-// By a whole warp: tiles of one head over the batch, and over the sequences before b.
-__device__ __forceinline__ long long head_tiles(const Attend8Args& a, int b, long long* before, bool report = false) {
-  long long all = 0, mine = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 32) {
-    Seq s;
-    const long long v = lane_tiles(a, b0, &s, report);
-    all += v;
-    if (b0 + (int)(threadIdx.x & 31) < b) mine += v;
-  }
-  *before = warp_sum(mine);
-  return warp_sum(all);
-}
-__device__ __forceinline__ long long piece_begin8(long long total, int ctas, int c) { return total * c / ctas; }
-__device__ __forceinline__ int piece_of8(long long total, int ctas, long long u) { return (int)(((u + 1) * ctas - 1) / total); }
-
-// By a whole warp: how many tiles CTA c has, and the place of the first.
-__device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int grid, long long* count, bool report) {
-  long long before;
-  const long long head = head_tiles(a, 0, &before, report), total = head * a.H_kv * a.layers;
-  const int ctas = (int)min((long long)grid, total);
-  Place p = {};
-  *count = 0;
-  if (c >= ctas) return p;
-  const long long u0 = piece_begin8(total, ctas, c);
-  *count = piece_begin8(total, ctas, c + 1) - u0;
-  const long long lg = u0 / head;
-  long long rest = u0 - lg * head;
-  p.l = (int)(lg / a.H_kv);
-  p.g = (int)(lg - (long long)p.l * a.H_kv);
-  for (int b0 = 0; b0 < a.batch; b0 += 32) {   // (u0 is in the list: the search ends inside the batch)
-    Seq s = {};
-    const long long v = lane_tiles(a, b0, &s, false);
-    long long upto = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long x = __shfl_up_sync(0xffffffffu, upto, o);
-      if ((int)(threadIdx.x & 31) >= o) upto += x;
-    }
-    const unsigned holds = __ballot_sync(0xffffffffu, rest < upto);
-    if (holds) {
-      const int at = __ffs(holds) - 1;
-      rest -= __shfl_sync(0xffffffffu, upto - v, at);
-      p.b = b0 + at;
-      p.s.f0 = __shfl_sync(0xffffffffu, s.f0, at);
-      p.s.n = __shfl_sync(0xffffffffu, s.n, at);
-      p.s.base = __shfl_sync(0xffffffffu, s.base, at);
-      p.s.len = __shfl_sync(0xffffffffu, s.len, at);
-      break;
-    }
-    rest -= __shfl_sync(0xffffffffu, upto, 31);
-  }
-  p.n_qp = blocks_of(a, p.s);
-  int lo = 0, hi = p.n_qp - 1;                 // the last block that begins at or before `rest`
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (tiles_before(a, p.s, mid, p.n_qp) <= rest) lo = mid; else hi = mid - 1;
-  }
-  p.qp = lo;
-  p.t = (int)(rest - tiles_before(a, p.s, lo, p.n_qp));
-  set_block(a, p);
-  return p;
-}
-
-// ---- e4m3
-__device__ __forceinline__ uint32_t encode_f32x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t encode_f16x2(__half2 x) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&x)));
-  return r;
-}
-__device__ __forceinline__ __half2 decode_f16x2(uint32_t codes) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
-  return *reinterpret_cast<__half2*>(&h);
-}
-// Does one of four codes say NaN?
-__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu); }
 
 template <int N>
 __device__ __forceinline__ void load_columns(uint32_t addr, float (&v)[N]) {
@@ -246,9 +55,9 @@ struct Shape8 {
   static constexpr int kQ = RB < 16 ? 16 : RB;                 // columns of S (a product is 16 wide at least)
   static constexpr int kP = (3 * RB + 15) / 16 * 16;           // columns of O: three groups of RB
   static constexpr int kSlot = kTile * DH;
-  static constexpr int kSlots = DH == 64 ? 16 : RB == 64 ? 8 : 10;         // K and V tiles in turns
+  static constexpr int kSlots = DH == 64 ? 8 : RB == 64 ? 4 : 5;           // tiles of keys, and as many of values
   static constexpr int kQBytes = kQ * DH, kPBytes = kP * kTile;
-  static constexpr int kBytes = 1024 + kSlots * kSlot + 2 * kPBytes + 2 * kQBytes;
+  static constexpr int kBytes = 1024 + 2 * kSlots * kSlot + 2 * kPBytes + 2 * kQBytes;
   static constexpr int kTmem = RB == 64 ? 512 : RB == 32 ? 256 : 128;      // 2 (kQ + kP), rounded up
 };
 
@@ -276,57 +85,34 @@ __device__ __forceinline__ void sum_columns(float (&v)[N], float* dst) {
   }
 }
 
-// By a warp of a CTA that has given up: the results of its n tiles from place x on say so, also to a caller without a flag word.
-template <int DH, int RB>
-__device__ __forceinline__ void results_are_nan(const Attend8Args& a, Place x, long long n) {
-  const float nan = __int_as_float(0x7fffffff);
-  for (uint32_t seg = 0; n > 0; ++seg) {
-    const int t1 = (int)min((long long)x.nt, x.t + n), tok0 = x.qp * a.block_tok;
-    const int rows = min(a.block_tok, x.s.n - tok0) * a.n_rep;
-    for (int r = threadIdx.x & 31; r < rows; r += 32) {
-      if (x.t == 0 && t1 == x.nt) {
-        const size_t qh = ((size_t)(a.l0 + x.l) * a.n_tok + x.s.f0 + tok0 + r / a.n_rep) * a.H_q + x.g * a.n_rep + r % a.n_rep;
-        for (int c = 0; c < DH; c += 8) *reinterpret_cast<uint4*>(a.out + qh * DH + c) = make_uint4(~0u, ~0u, ~0u, ~0u);
-        if (a.lse) a.lse[qh] = nan;
-      } else {                                 // (the merge makes it the whole problem's)
-        a.part_ml[((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * RB + r] = make_float2(nan, nan);
-      }
-    }
-    n -= t1 - x.t;
-    if (n > 0) next_problem(a, x);
-  }
-}
-
 template <int DH, int RB>
 __global__ void __launch_bounds__(kThreads8, 1)
 attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const Attend8Args a) {
   using namespace ptx;
   using L = Shape8<DH, RB>;
-  constexpr int NS = L::kSlots, NQ = L::kQ, NP = L::kP;
+  using Ring = Ring8<L::kSlots, L::kSlots, 2 * L::kSlots>;
+  constexpr int NQ = L::kQ, NP = L::kP, SR = 2 * L::kSlots;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars_s[3 * NS + 8];
+  __shared__ uint64_t bars_s[Ring::kBars + 8];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   __shared__ Place place_s;
   __shared__ long long count_s;
-  __shared__ float2 scale_s[NS][8];            // of a tile's pages: keys', values'
+  __shared__ float2 scale_s[SR][8];            // of a tile's pages: keys', values'
   __shared__ float2 info_s[2][RB];             // of a column: factor of its query, bound that its z may not pass
   __shared__ __align__(16) float sub_s[2][RB]; // what is taken off z (m)
   __shared__ float fac_s[2][RB], top_s[2][4][RB], sum_s[2][4][RB];
   __shared__ uint32_t bad_s[2];                // new rows of the block's tokens with value codes that are NaN
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
-  constexpr uint32_t kPAt = NS * L::kSlot, kQAt = kPAt + 2 * L::kPBytes;         // ring, weights, queries (high, low)
+  constexpr uint32_t kPAt = 2 * L::kSlots * L::kSlot, kQAt = kPAt + 2 * L::kPBytes;         // ring, weights, queries (high, low)
   const uint32_t bars = smem_u32(bars_s);
-  const uint32_t b_full = bars, b_empty = bars + 8 * NS, b_sc = b_empty + 8 * NS, b_s = b_sc + 8 * NS, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16, b_drain = b_q + 8;
+  const Ring ring{base, bars, scale_s};
+  const uint32_t b_s = bars + 8 * Ring::kBars, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16, b_drain = b_q + 8;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
-    for (int i = 0; i < NS; ++i) {
-      mbar_init(b_full + 8 * i, 1);
-      mbar_init(b_empty + 8 * i, 1);
-      mbar_init(b_sc + 8 * i, 32);             // (every lane of the producer reports its copies)
-    }
+    ring.init(1, 1);
     for (int i = 0; i < 2; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_p + 8 * i, 4); mbar_init(b_o + 8 * i, 1); }
     mbar_init(b_q, 8);
     mbar_init(b_drain, 1);
@@ -352,106 +138,60 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
   const Wait wt{&abort_s, a.flags, wait_limit(a.inject)};
   long long left = count_s;
   Place p = place_s;
-  uint32_t n_loaded = 0;                       // producer: slots asked for
+  uint32_t n_loaded = 0;                       // producer: tiles asked for
 
   if (left > 0 && warp == kProducer8) {
-    const int ppt_shift = 7 - a.page_shift, ppt = 1 << ppt_shift, tpb = 32 >> ppt_shift;       // pages of a tile, tiles of a batch of entries
-    bool ok = !(a.inject & XKV_INJECT_CACHE_NO_LOAD);
-    uint32_t k_tile = 0;
-    while (left > 0 && ok) {
-      const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left);
-      left -= t1 - t0;
-      const int rows = rows_seen(a, p.s, p.qp), pages = min((rows + (1 << a.page_shift) - 1) >> a.page_shift, t1 << ppt_shift);
-      const int32_t* entries = a.table + (size_t)p.b * a.max_pages;
-      auto entry = [&](int t) {                // lane: an entry of the batch that begins with tile t
-        const int i = (t << ppt_shift) + lane;
-        if (i >= pages) return -1;
-        const int e = entries[i];
-        if (e >= 0 && e < a.n_pages) return e;
-        if (a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
-        return -1;
-      };
-      int now = 0, next = entry(t0);
-      for (int t = t0; t < t1 && ok; ++t, ++k_tile) {
-        const int in = (t - t0) & (tpb - 1);
-        if (in == 0) { now = next; next = entry(t + tpb); }
-        const int mine = __shfl_sync(0xffffffffu, now, ((in << ppt_shift) + lane) & 31), id = lane < ppt ? mine : -1;
-        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, id >= 0)) * ((uint32_t)DH << a.page_shift);
-        const size_t head = ((size_t)(a.l0 + p.l) * a.n_pages + (id >= 0 ? id : 0)) * a.H_kv + p.g;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t slot = n_loaded % NS, full = b_full + 8 * slot;
-          if (!(ok = wait_warp(wt, b_empty + 8 * slot, ((n_loaded / NS) & 1u) ^ 1u))) break;
-          if (lane == 0) mbar_expect_tx(full, bytes);
-          __syncwarp();
-          if (id >= 0)
-            tma_load_2d(base + slot * L::kSlot + (uint32_t)lane * ((uint32_t)DH << a.page_shift), kv ? &v_map : &k_map, 0, (int)(head << a.page_shift), full);
-          if (kv == 0) {
-            // a tile's scales are read until its values' slot is free, and its keys' slot may be filled again before: a ring of their own
-            if (lane < ppt) {
-              const uint32_t at = smem_u32(&scale_s[k_tile % NS][lane]), n = id >= 0 ? 4u : 0u;
-              cp_async4(at, a.k_scale + head, n);
-              cp_async4(at + 4, a.v_scale + head, n);
-            }
-            cp_async_arrive_noinc(b_sc + 8 * (k_tile % NS));
-          }
-          ++n_loaded;
-        }
-      }
-      if (left > 0) next_problem(a, p);
-    }
-    __syncwarp();
+    n_loaded = ring.template produce<DH>(a, wt, &k_map, &v_map, p, left);
   } else if (left > 0 && warp == kIssuer8) {
     constexpr uint32_t idesc_s = idesc_e4m3_f32(128, NQ), idesc_o = idesc_e4m3_f32(DH, NP) | (1u << 15);     // V is read along its rows
     const uint64_t ring_desc = smem_desc_rows<DH>(base), q_desc = smem_desc_rows<DH>(base + kQAt), p_desc = smem_desc_rows<128>(base + kPAt);
     uint32_t k0 = 0, seg = 0;                  // tiles and segments so far
     bool ok = true;
-    auto full = [&](uint32_t n) { return wait_warp(wt, b_full + 8 * (n % NS), (n / NS) & 1u); };
+    auto keys = [&](uint32_t k) { return wait_warp(wt, ring.k_full(k), Ring::k_parity(k)); };
     auto logits = [&](uint32_t k) {            // S of tile k, by one thread
-      const uint32_t slot = (2 * k) % NS;
-      const uint64_t kd = ring_desc + (uint64_t)(slot * (uint32_t)(L::kSlot >> 4));
+      const uint64_t kd = ring_desc + (uint64_t)((k % L::kSlots) * (uint32_t)(L::kSlot >> 4));
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < DH / 32; ++i)
           tc_mma_e4m3(tmem + (k & 1u) * NQ, kd + (uint64_t)(2 * i), q_desc + (uint64_t)(h * (L::kQBytes >> 4) + 2 * i), idesc_s, h | i ? 1u : 0u);
       tc_commit(b_s + 8 * (k & 1u));
-      tc_commit(b_empty + 8 * slot);
+      tc_commit(ring.k_empty(k));
     };
     while (left > 0 && ok) {
       const int n = (int)min((long long)p.nt, p.t + left) - p.t;
       left -= n;
       ok = wait_warp(wt, b_q, seg & 1u);
       for (int s = 0; s < min(2, n) && ok; ++s) {
-        if (!(ok = full(2 * (k0 + s)))) break;
+        if (!(ok = keys(k0 + s))) break;
         tc_fence_after();
         if (elect_one()) logits(k0 + s);
         __syncwarp();
       }
       for (int s = 0; s < n && ok; ++s) {
-        const uint32_t k = k0 + s, w = k & 1u, nv = 2 * k + 1;
+        const uint32_t k = k0 + s, w = k & 1u;
         if (!(ok = wait_warp(wt, b_p + 8 * w, (k >> 1) & 1u))) break;
         const bool more = s + 2 < n;
         // S two ahead goes first where its keys are in: the warpgroup waits for it
-        const bool early = more && __all_sync(0xffffffffu, mbar_test(b_full + 8 * ((nv + 3) % NS), ((nv + 3) / NS) & 1u));
-        if (!early && !(ok = full(nv))) break;
+        const bool early = more && __all_sync(0xffffffffu, mbar_test(ring.k_full(k + 2), Ring::k_parity(k + 2)));
         tc_fence_after();
         if (early) {
           if (elect_one()) logits(k + 2);
           __syncwarp();
-          if (!(ok = full(nv))) break;
         }
+        if (!(ok = wait_warp(wt, ring.v_full(k), Ring::v_parity(k)))) break;
+        tc_fence_after();
         if (elect_one()) {
-          const uint64_t vd = ring_desc + (uint64_t)((nv % NS) * (uint32_t)(L::kSlot >> 4)), pd = p_desc + (uint64_t)(w * (uint32_t)(L::kPBytes >> 4));
+          const uint64_t vd = ring_desc + (uint64_t)((L::kSlots + k % L::kSlots) * (uint32_t)(L::kSlot >> 4)), pd = p_desc + (uint64_t)(w * (uint32_t)(L::kPBytes >> 4));
 #pragma unroll
           for (int i = 0; i < kTile / 32; ++i)
             tc_mma_e4m3(tmem + 2 * NQ + w * NP, vd + (uint64_t)(i * (32 * DH >> 4)), pd + (uint64_t)(2 * i), idesc_o, (s >= 2) | (i > 0) ? 1u : 0u);
           tc_commit(b_o + 8 * w);
-          tc_commit(b_empty + 8 * (nv % NS));
+          tc_commit(ring.v_empty(k));
         }
         __syncwarp();
         if (more && !early) {
-          if (!(ok = full(nv + 3))) break;
+          if (!(ok = keys(k + 2))) break;
           tc_fence_after();
           if (elect_one()) logits(k + 2);
           __syncwarp();
@@ -486,34 +226,12 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         if (NQ * C < 256 && i >= NQ * C) break;
         uint4 x = make_uint4(0u, 0u, 0u, 0u);
         if (r < rows) x = *reinterpret_cast<const uint4*>(a.q + row_of(r) * DH + c * 8);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
-        top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-        for (int o = C / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const int ex = max((int)(top >> 7) - 127 - 7, -100);
-        const float f = __int_as_float((127 - ex) << 23);
-        uint32_t hi[2], lo[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          uint32_t h[2], l[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float x0 = __uint_as_float(w[2 * e + u] << 16) * f, x1 = __uint_as_float(w[2 * e + u] & 0xffff0000u) * f;
-            h[u] = encode_f32x2(x0, x1);
-            const float2 b = __half22float2(decode_f16x2(h[u]));
-            l[u] = encode_f32x2(x0 - b.x, x1 - b.y);
-          }
-          hi[e] = h[0] | (h[1] << 16);
-          lo[e] = l[0] | (l[1] << 16);
-        }
-        if (top >= 0x7f80u) hi[0] = hi[1] = 0x7f7f7f7fu;       // an element is not finite: neither is a logit
-        const int unit = DH == 128 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
-        uint8_t* at = gen + kQAt + r * DH + unit * 16 + (c & 1) * 8;
-        *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
-        *reinterpret_cast<uint2*>(at + L::kQBytes) = make_uint2(lo[0], lo[1]);
+        uint2 hi, lo;
+        int ex;
+        encode_query<C>(x, &hi, &lo, &ex);
+        uint8_t* at = gen + kQAt + tile_place<DH>(r, c);
+        *reinterpret_cast<uint2*>(at) = hi;
+        *reinterpret_cast<uint2*>(at + L::kQBytes) = lo;
         if (c == 0 && r < RB) {
           const float qs = __int_as_float((127 + ex) << 23) * a.scale2;
           info_s[0][r] = info_s[1][r] = make_float2(qs, r < rows ? -INFINITY : INFINITY);      // (nobody's column: no bound)
@@ -531,11 +249,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
 
       for (int s = (int)((k0 ^ (uint32_t)wg) & 1u); s < n; s += 2) {
         const uint32_t k = k0 + s;
-        ok = ok && wait_warp(wt, b_s + 8 * wg, mine & 1u) && wait_warp(wt, b_sc + 8 * (k % NS), (k / NS) & 1u);
+        ok = ok && wait_warp(wt, b_s + 8 * wg, mine & 1u) && wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k));
         tc_fence_after();
         float z[RB];
         load_columns<RB>(s_addr, z);
-        const float2 sc = scale_s[k % NS][row >> a.page_shift];
+        const float2 sc = scale_s[k % SR][row >> a.page_shift];
         const float ks = __int_as_float(__float_as_int(sc.x) & 0x7f800000);
         const int ve = (__float_as_int(sc.y) >> 23) & 255;
         const int j = (t0 + s) * kTile + row;
@@ -624,10 +342,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         }
         if (__any_sync(0xffffffffu, dead || from > 0)) {
           // thread = value row: what no column sees is zeroed, NaN is taken out of what only some see, and listed
-          const uint32_t nv = 2 * k + 1;
-          ok = ok && wait_warp(wt, b_full + 8 * (nv % NS), (nv / NS) & 1u);
+          ok = ok && wait_warp(wt, ring.v_full(k), Ring::v_parity(k));
           if (ok && (dead || from > 0)) {
-            uint4* v = reinterpret_cast<uint4*>(gen + (nv % NS) * L::kSlot + row * DH);      // (the order of its units does not matter)
+            uint4* v = reinterpret_cast<uint4*>(gen + (L::kSlots + k % L::kSlots) * L::kSlot + row * DH);      // (the order of its units does not matter)
             uint32_t hit = 0;
 #pragma unroll
             for (int c = 0; c < DH / 16; ++c) {
@@ -727,16 +444,13 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     tmem_dealloc(tmem, L::kTmem);
   }
   if (abort_s && warp == kProducer8) {
-    // given up: tiles may still be on their way into this CTA's shared memory; stay (with a limit) for them
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    for (uint32_t n = n_loaded > NS ? n_loaded - NS : 0u; n < n_loaded; ++n)
-      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(b_full + 8 * (n % NS), (n / NS) & 1u))) break;
-    results_are_nan<DH, RB>(a, place_s, count_s);
+    ring.drain(n_loaded);
+    results_are_nan<DH>(a, place_s, count_s);
   }
 }
 
 // Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A warp has one query row, lane = d_h / 32 columns.
-template <int DH, int RB>
+template <int DH>
 __global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const Attend8Args a, int attend_grid) {
   constexpr int V = DH / 32, AT_ONCE = 16;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -774,7 +488,7 @@ __global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const 
   if (c0 == c1) return;                        // one piece: written where it was computed
   // a problem that begins inside a piece is that piece's last one, and in the others the first
   const size_t first = (size_t)c0 * 2 + (piece_begin8(total, ctas, c0) == u0 ? 0 : 1);
-  auto slot = [&](int c) { return (c == c0 ? first : (size_t)c * 2) * RB + r; };
+  auto slot = [&](int c) { return (c == c0 ? first : (size_t)c * 2) * a.block_rows + r; };
   float M = -INFINITY, sum = 0.0f, acc[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.0f;
@@ -825,11 +539,18 @@ __global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const 
 
 template <int DH, int RB>
 cudaError_t launch_as(const CUtensorMap& k_map, const CUtensorMap& v_map, const Attend8Args& a, int grid, int device, cudaStream_t s) {
-  cudaError_t e = ensure_dyn_smem<attend8_kernel<DH, RB>>(Shape8<DH, RB>::kBytes, device);
-  if (e == cudaSuccess) e = launch_pdl(attend8_kernel<DH, RB>, dim3(grid), dim3(kThreads8), Shape8<DH, RB>::kBytes, s, k_map, v_map, a);
+  const cudaError_t e = ensure_dyn_smem<attend8_kernel<DH, RB>>(Shape8<DH, RB>::kBytes, device);
+  return e != cudaSuccess ? e : launch_pdl(attend8_kernel<DH, RB>, dim3(grid), dim3(kThreads8), Shape8<DH, RB>::kBytes, s, k_map, v_map, a);
+}
+
+template <int DH>
+cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, const Attend8Args& a, int grid, int device, cudaStream_t s) {
+  cudaError_t e = a.block_rows == 8 ? launch_as<DH, 8>(k_map, v_map, a, grid, device, s) : a.block_rows == 16 ? launch_as<DH, 16>(k_map, v_map, a, grid, device, s)
+                : a.block_rows == 32 ? launch_as<DH, 32>(k_map, v_map, a, grid, device, s) : a.block_rows == 64 ? launch_as<DH, 64>(k_map, v_map, a, grid, device, s)
+                : launch_attend8_wide(k_map, v_map, DH, a, grid, device, s);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)a.n_tok * a.H_q;
-  e = launch_pdl(attend8_merge_kernel<DH, RB>, dim3((unsigned)((rows + kMergeWarps8 - 1) / kMergeWarps8), a.layers), dim3(kMergeWarps8 * 32), 0, s, a, grid);
+  e = launch_pdl(attend8_merge_kernel<DH>, dim3((unsigned)((rows + kMergeWarps8 - 1) / kMergeWarps8), a.layers), dim3(kMergeWarps8 * 32), 0, s, a, grid);
   count_launch(kFamAttend8, 2);
   return e;
 }
@@ -837,7 +558,7 @@ cudaError_t launch_as(const CUtensorMap& k_map, const CUtensorMap& v_map, const 
 // Query rows of a block: as few as hold the tokens of the longest sequence.
 int block_rows(int max_new, int n_rep) {
   const long long rows = (long long)max_new * n_rep;
-  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
 }
 
 }  // namespace
@@ -861,8 +582,8 @@ cudaError_t launch_cache8_attend(const xkv_cache8_config* c, int l0, int l1, con
   a.batch = c->batch; a.H_kv = c->H_kv; a.H_q = c->H_q; a.n_rep = c->H_q / c->H_kv; a.n_pages = c->n_pages; a.max_pages = c->max_pages;
   a.page_shift = __builtin_ctz((unsigned)c->page);
   a.n_tok = n_tok; a.max_new = max_new; a.l0 = l0; a.layers = l1 - l0;
-  const int rb = block_rows(max_new, a.n_rep);
-  a.block_tok = rb / a.n_rep;
+  a.block_rows = block_rows(max_new, a.n_rep);
+  a.block_tok = a.block_rows / a.n_rep;
   a.rep_inv = (65536u + a.n_rep - 1u) / a.n_rep;
   a.scale2 = (c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / sqrtf((float)c->d_h)) * kLog2e;
   a.q = q; a.first = first; a.table = table; a.length = length; a.V8 = (const uint8_t*)V8;
@@ -870,12 +591,8 @@ cudaError_t launch_cache8_attend(const xkv_cache8_config* c, int l0, int l1, con
   a.inject = cache_fault_injection();
   const int grid = sms < kPlanSms ? sms : kPlanSms;
   a.part = (float*)workspace;
-  a.part_ml = reinterpret_cast<float2*>(a.part + (size_t)kPlanSms * 2 * rb * c->d_h);
-  if (c->d_h == 128)
-    return rb == 8 ? launch_as<128, 8>(k_map, v_map, a, grid, device, s) : rb == 16 ? launch_as<128, 16>(k_map, v_map, a, grid, device, s)
-         : rb == 32 ? launch_as<128, 32>(k_map, v_map, a, grid, device, s) : launch_as<128, 64>(k_map, v_map, a, grid, device, s);
-  return rb == 8 ? launch_as<64, 8>(k_map, v_map, a, grid, device, s) : rb == 16 ? launch_as<64, 16>(k_map, v_map, a, grid, device, s)
-       : rb == 32 ? launch_as<64, 32>(k_map, v_map, a, grid, device, s) : launch_as<64, 64>(k_map, v_map, a, grid, device, s);
+  a.part_ml = reinterpret_cast<float2*>(a.part + (size_t)kPlanSms * 2 * a.block_rows * c->d_h);
+  return c->d_h == 128 ? launch_width<128>(k_map, v_map, a, grid, device, s) : launch_width<64>(k_map, v_map, a, grid, device, s);
 }
 
 }  // namespace xkv

@@ -1,0 +1,340 @@
+// Shared by the attention kernels over a paged cache of 8-bit codes (xkv_attend8.cu, xkv_attend8_wide.cu): what a call is given, the list
+// of tiles, e4m3.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include "xkv_cache.cuh"
+
+namespace xkv {
+
+struct Attend8Args {
+  int batch, H_kv, H_q, n_rep, n_pages, max_pages, page_shift, n_tok, max_new, l0, layers;
+  int block_tok;                               // tokens of a block of query rows
+  uint32_t rep_inv;                            // ceil(2^16 / n_rep)
+  float scale2;                                // softmax scale times log2(e)
+  const __nv_bfloat16* q;
+  const int32_t* first;
+  const int32_t* table;
+  const int32_t* length;
+  const uint8_t* V8;                           // (codes that are NaN)
+  const float* k_scale;
+  const float* v_scale;
+  int block_rows;                              // room for query rows in a piece's results
+  float* part;                                 // [CTA][2][block_rows][d_h]
+  float2* part_ml;                             // [CTA][2][block_rows] (m, l)
+  __nv_bfloat16* out;
+  float* lse;
+  unsigned int* flags;
+  unsigned int inject;                         // XKV_INJECT_CACHE_* bits; 0 in normal use
+};
+
+// A sequence: its first token, how many of its tokens are looked after, its rows, and those before its first new one (below zero if
+// it has more new tokens than rows).
+struct Seq {
+  int f0, n, base, len;
+};
+__device__ __forceinline__ Seq load_seq(const Attend8Args& a, int b, bool* bad) {
+  const int w0 = a.first ? a.first[b] : b, w1 = a.first ? a.first[b + 1] : b + 1, wl = a.length[b];
+  const int f0 = min(max(w0, 0), a.n_tok), f1 = min(max(w1, f0), a.n_tok), len = min(max(wl, 0), a.max_pages << a.page_shift);
+  *bad = f0 != w0 || f1 != w1 || len != wl || f1 - f0 > a.max_new;
+  return Seq{f0, min(f1 - f0, a.max_new), len - (f1 - f0), len};
+}
+__device__ __forceinline__ int blocks_of(const Attend8Args& a, const Seq& s) { return (s.n + a.block_tok - 1) / a.block_tok; }
+// Rows that the last token of block qp sees, and the tiles that they lie in (one for tokens that see nothing: it says so).
+__device__ __forceinline__ int rows_seen(const Attend8Args& a, const Seq& s, int qp) {
+  return min(max(s.base + min(s.n, (qp + 1) * a.block_tok), 0), s.len);
+}
+__device__ __forceinline__ int tiles_of(int rows) { return max(1, (rows + kTile - 1) / kTile); }
+
+// sum over i < n of floor((a i + b) / m), all of them non-negative: Euclid's algorithm on (a, m).
+static __device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+  long long sum = 0;
+  while (n > 0) {
+    if (a >= m) { sum += n * (n - 1) / 2 * (a / m); a %= m; }
+    if (b >= m) { sum += n * (b / m); b %= m; }
+    const long long y = a * n + b;
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const long long t = m;
+    m = a;
+    a = t;
+  }
+  return sum;
+}
+// Tiles of one head in blocks 0 .. qp-1 of a sequence of n_qp blocks; those before the last are full: their rows grow by block_tok.
+static __device__ long long tiles_before(const Attend8Args& a, const Seq& s, int qp, int n_qp) {
+  if (qp == 0) return 0;
+  if (qp == n_qp) return tiles_before(a, s, qp - 1, n_qp) + tiles_of(rows_seen(a, s, qp - 1));
+  const int most = kTile - s.base;             // blocks that see up to one tile count one
+  const int ones = most > 0 ? min(qp, most / a.block_tok) : 0;
+  return ones + floor_sum(qp - ones, kTile, a.block_tok, s.base + (long long)(ones + 1) * a.block_tok + kTile - 1);
+}
+__device__ __forceinline__ long long tiles_of_head(const Attend8Args& a, const Seq& s) {
+  if (s.n <= a.block_tok) return s.n > 0 ? tiles_of(rows_seen(a, s, 0)) : 0;
+  const int n_qp = blocks_of(a, s);
+  return tiles_before(a, s, n_qp, n_qp);
+}
+
+// A place in the list of tiles.  Order: layer, head, sequence, block, tile.
+struct Place {
+  int l, g, b, qp, t, nt, n_qp;
+  Seq s;
+};
+__device__ __forceinline__ void set_block(const Attend8Args& a, Place& p) { p.nt = tiles_of(rows_seen(a, p.s, p.qp)); }
+// Moves to the next problem (there is one: the caller counts).
+__device__ __forceinline__ void next_problem(const Attend8Args& a, Place& p) {
+  p.t = 0;
+  if (++p.qp >= p.n_qp) {
+    p.qp = 0;
+    do {
+      if (++p.b == a.batch) {
+        p.b = 0;
+        if (++p.g == a.H_kv) { p.g = 0; ++p.l; }
+      }
+      bool bad;
+      p.s = load_seq(a, p.b, &bad);
+      p.n_qp = blocks_of(a, p.s);
+    } while (p.n_qp == 0 && p.l < a.layers);
+  }
+  set_block(a, p);
+}
+
+__device__ __forceinline__ long long warp_sum(long long v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// Lane: tiles of one head in sequence b0 + lane.
+__device__ __forceinline__ long long lane_tiles(const Attend8Args& a, int b0, Seq* s, bool report) {
+  const int b = b0 + (int)(threadIdx.x & 31);
+  if (b >= a.batch) return 0;
+  bool bad;
+  *s = load_seq(a, b, &bad);
+  if (bad && report && a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+  return tiles_of_head(a, *s);
+}
+// By a whole warp: tiles of one head over the batch, and over the sequences before b.
+__device__ __forceinline__ long long head_tiles(const Attend8Args& a, int b, long long* before, bool report = false) {
+  long long all = 0, mine = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    Seq s;
+    const long long v = lane_tiles(a, b0, &s, report);
+    all += v;
+    if (b0 + (int)(threadIdx.x & 31) < b) mine += v;
+  }
+  *before = warp_sum(mine);
+  return warp_sum(all);
+}
+__device__ __forceinline__ long long piece_begin8(long long total, int ctas, int c) { return total * c / ctas; }
+__device__ __forceinline__ int piece_of8(long long total, int ctas, long long u) { return (int)(((u + 1) * ctas - 1) / total); }
+
+// By a whole warp: how many tiles CTA c has, and the place of the first.
+__device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int grid, long long* count, bool report) {
+  long long before;
+  const long long head = head_tiles(a, 0, &before, report), total = head * a.H_kv * a.layers;
+  const int ctas = (int)min((long long)grid, total);
+  Place p = {};
+  *count = 0;
+  if (c >= ctas) return p;
+  const long long u0 = piece_begin8(total, ctas, c);
+  *count = piece_begin8(total, ctas, c + 1) - u0;
+  const long long lg = u0 / head;
+  long long rest = u0 - lg * head;
+  p.l = (int)(lg / a.H_kv);
+  p.g = (int)(lg - (long long)p.l * a.H_kv);
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {   // (u0 is in the list: the search ends inside the batch)
+    Seq s = {};
+    const long long v = lane_tiles(a, b0, &s, false);
+    long long upto = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+      if ((int)(threadIdx.x & 31) >= o) upto += x;
+    }
+    const unsigned holds = __ballot_sync(0xffffffffu, rest < upto);
+    if (holds) {
+      const int at = __ffs(holds) - 1;
+      rest -= __shfl_sync(0xffffffffu, upto - v, at);
+      p.b = b0 + at;
+      p.s.f0 = __shfl_sync(0xffffffffu, s.f0, at);
+      p.s.n = __shfl_sync(0xffffffffu, s.n, at);
+      p.s.base = __shfl_sync(0xffffffffu, s.base, at);
+      p.s.len = __shfl_sync(0xffffffffu, s.len, at);
+      break;
+    }
+    rest -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  p.n_qp = blocks_of(a, p.s);
+  int lo = 0, hi = p.n_qp - 1;                 // the last block that begins at or before `rest`
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (tiles_before(a, p.s, mid, p.n_qp) <= rest) lo = mid; else hi = mid - 1;
+  }
+  p.qp = lo;
+  p.t = (int)(rest - tiles_before(a, p.s, lo, p.n_qp));
+  set_block(a, p);
+  return p;
+}
+
+// ---- e4m3
+__device__ __forceinline__ uint32_t encode_f32x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t encode_f16x2(__half2 x) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&x)));
+  return r;
+}
+__device__ __forceinline__ __half2 decode_f16x2(uint32_t codes) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+  return *reinterpret_cast<__half2*>(&h);
+}
+// Does one of four codes say NaN?
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu); }
+
+// By a warp of a CTA that has given up: the results of its n tiles from place x on say so, also to a caller without a flag word.
+template <int DH>
+__device__ __forceinline__ void results_are_nan(const Attend8Args& a, Place x, long long n) {
+  const float nan = __int_as_float(0x7fffffff);
+  for (uint32_t seg = 0; n > 0; ++seg) {
+    const int t1 = (int)min((long long)x.nt, x.t + n), tok0 = x.qp * a.block_tok;
+    const int rows = min(a.block_tok, x.s.n - tok0) * a.n_rep;
+    for (int r = threadIdx.x & 31; r < rows; r += 32) {
+      if (x.t == 0 && t1 == x.nt) {
+        const size_t qh = ((size_t)(a.l0 + x.l) * a.n_tok + x.s.f0 + tok0 + r / a.n_rep) * a.H_q + x.g * a.n_rep + r % a.n_rep;
+        for (int c = 0; c < DH; c += 8) *reinterpret_cast<uint4*>(a.out + qh * DH + c) = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (a.lse) a.lse[qh] = nan;
+      } else {                                 // (the merge makes it the whole problem's)
+        a.part_ml[((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * a.block_rows + r] = make_float2(nan, nan);
+      }
+    }
+    n -= t1 - x.t;
+    if (n > 0) next_problem(a, x);
+  }
+}
+
+// The copies of a CTA's tiles, by its producer's warp: a page is one box of the copy engine; lane i has the i-th page of a tile, its
+// entry of the table and its scales (asynchronous copies of four bytes, which report to a barrier of their own: a tile's scales are read
+// until its values have met their weights, and its keys' slot may be filled again before).  Keys go through a ring of KS slots, values
+// through one of VS behind it, scales through one of SR > VS + 2 tiles.  Barriers: keys full, keys empty, values full, values empty,
+// scales full.  Returns how many tiles were asked for.
+template <int KS, int VS, int SR>
+struct Ring8 {
+  static constexpr int kBars = 2 * KS + 2 * VS + SR;
+  uint32_t slots, bars;
+  float2 (*scales)[8];                         // keys', values'
+  __device__ __forceinline__ uint32_t k_full(uint32_t k) const { return bars + 8 * (k % KS); }
+  __device__ __forceinline__ uint32_t k_empty(uint32_t k) const { return bars + 8 * (KS + k % KS); }
+  __device__ __forceinline__ uint32_t v_full(uint32_t k) const { return bars + 8 * (2 * KS + k % VS); }
+  __device__ __forceinline__ uint32_t v_empty(uint32_t k) const { return bars + 8 * (2 * KS + VS + k % VS); }
+  __device__ __forceinline__ uint32_t scales_full(uint32_t k) const { return bars + 8 * (2 * KS + 2 * VS + k % SR); }
+  static __device__ __forceinline__ uint32_t k_parity(uint32_t k) { return (k / KS) & 1u; }
+  static __device__ __forceinline__ uint32_t v_parity(uint32_t k) { return (k / VS) & 1u; }
+  static __device__ __forceinline__ uint32_t scales_parity(uint32_t k) { return (k / SR) & 1u; }
+  // By one thread: how many arrivals empty a slot.
+  __device__ __forceinline__ void init(int k_done, int v_done) const {
+    for (int i = 0; i < KS; ++i) { ptx::mbar_init(k_full(i), 1); ptx::mbar_init(k_empty(i), k_done); }
+    for (int i = 0; i < VS; ++i) { ptx::mbar_init(v_full(i), 1); ptx::mbar_init(v_empty(i), v_done); }
+    for (int i = 0; i < SR; ++i) ptx::mbar_init(scales_full(i), 32);           // (every lane reports)
+  }
+  template <int DH>
+  __device__ __forceinline__ uint32_t produce(const Attend8Args& a, const Wait& wt, const CUtensorMap* k_map, const CUtensorMap* v_map, Place p, long long left) const {
+    const int lane = threadIdx.x & 31;
+    const int ppt_shift = 7 - a.page_shift, ppt = 1 << ppt_shift, tpb = 32 >> ppt_shift;       // pages of a tile, tiles of a batch of entries
+    const uint32_t page_bytes = (uint32_t)DH << a.page_shift;
+    bool ok = !(a.inject & XKV_INJECT_CACHE_NO_LOAD);
+    uint32_t k = 0;
+    while (left > 0 && ok) {
+      const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left);
+      left -= t1 - t0;
+      const int rows = rows_seen(a, p.s, p.qp), pages = min((rows + (1 << a.page_shift) - 1) >> a.page_shift, t1 << ppt_shift);
+      const int32_t* entries = a.table + (size_t)p.b * a.max_pages;
+      auto entry = [&](int t) {                // lane: an entry of the batch that begins with tile t
+        const int i = (t << ppt_shift) + lane;
+        if (i >= pages) return -1;
+        const int e = entries[i];
+        if (e >= 0 && e < a.n_pages) return e;
+        if (a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+        return -1;
+      };
+      int now = 0, next = entry(t0);
+      for (int t = t0; t < t1 && ok; ++t, ++k) {
+        const int in = (t - t0) & (tpb - 1);
+        if (in == 0) { now = next; next = entry(t + tpb); }
+        const int mine = __shfl_sync(0xffffffffu, now, ((in << ppt_shift) + lane) & 31), id = lane < ppt ? mine : -1;
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, id >= 0)) * page_bytes;
+        const size_t head = ((size_t)(a.l0 + p.l) * a.n_pages + (id >= 0 ? id : 0)) * a.H_kv + p.g;
+        const int y = (int)(head << a.page_shift);
+        if (!(ok = wait_warp(wt, k_empty(k), k_parity(k) ^ 1u))) break;
+        if (lane == 0) ptx::mbar_expect_tx(k_full(k), bytes);
+        __syncwarp();
+        if (id >= 0) ptx::tma_load_2d(slots + (k % KS) * (kTile * DH) + lane * page_bytes, k_map, 0, y, k_full(k));
+        if (lane < ppt) {
+          const uint32_t at = ptx::smem_u32(&scales[k % SR][lane]), n = id >= 0 ? 4u : 0u;    // (a page that is not there gets zeros)
+          ptx::cp_async4(at, a.k_scale + head, n);
+          ptx::cp_async4(at + 4, a.v_scale + head, n);
+        }
+        ptx::cp_async_arrive_noinc(scales_full(k));
+        if (!(ok = wait_warp(wt, v_empty(k), v_parity(k) ^ 1u))) { ++k; break; }
+        if (lane == 0) ptx::mbar_expect_tx(v_full(k), bytes);
+        __syncwarp();
+        if (id >= 0) ptx::tma_load_2d(slots + (KS + k % VS) * (kTile * DH) + lane * page_bytes, v_map, 0, y, v_full(k));
+      }
+      if (left > 0) next_problem(a, p);
+    }
+    __syncwarp();
+    return k;
+  }
+  // By the producer's warp of a CTA that has given up: tiles may still be on their way into its shared memory; stay (with a limit) for them.
+  __device__ __forceinline__ void drain(uint32_t loaded) const {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    for (uint32_t k = loaded > KS ? loaded - KS : 0u; k < loaded; ++k)
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, ptx::mbar_try_wait(k_full(k), k_parity(k)))) break;
+    for (uint32_t k = loaded > VS ? loaded - VS : 0u; k < loaded; ++k)
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, ptx::mbar_try_wait(v_full(k), v_parity(k)))) break;
+  }
+};
+
+// Eight elements of a query row as two codes each, by a lane of the C that hold the row side by side: the row's largest element lies in
+// [128, 256) times 2^ex.  A row with an element that is not finite becomes NaN.
+template <int C>
+__device__ __forceinline__ void encode_query(const uint4& x, uint2* hi, uint2* lo, int* ex) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
+  top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+  for (int o = C / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  *ex = max((int)(top >> 7) - 127 - 7, -60);                   // (with a scale's 2^-60 still a normal number)
+  const float f = __int_as_float((127 - *ex) << 23);
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
+    h[e] = encode_f32x2(x0, x1);
+    const float2 b = __half22float2(decode_f16x2(h[e]));
+    l[e] = encode_f32x2(x0 - b.x, x1 - b.y);
+  }
+  *hi = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+  *lo = make_uint2(l[0] | (l[1] << 16), l[2] | (l[3] << 16));
+  if (top >= 0x7f80u) *hi = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+}
+// Where eight bytes of a tile with rows of DH bytes and as wide a swizzle lie.
+template <int DH>
+__device__ __forceinline__ uint32_t tile_place(int r, int c) {
+  const int unit = DH == 128 ? (c >> 1) ^ (r & 7) : (c >> 1) ^ ((r >> 1) & 3);
+  return (uint32_t)(r * DH + unit * 16 + (c & 1) * 8);
+}
+
+// xkv_attend8_wide.cu: blocks of 128 or 256 query rows
+cudaError_t launch_attend8_wide(const CUtensorMap& k_map, const CUtensorMap& v_map, int d_h, const Attend8Args& a, int grid, int device,
+                                cudaStream_t s);
+
+}  // namespace xkv
