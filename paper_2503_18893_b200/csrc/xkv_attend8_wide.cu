@@ -259,8 +259,22 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       for (int s = 0; s < steps; ++s, ++st) {
         const int t = t0 + s / SPT, half = s % SPT;
         const uint32_t buf = st & 1u, k = k0 + (uint32_t)(s / SPT);
-        if (!(ok = wait_warp(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
         if (half == 0 && !(ok = wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k)))) break;
+        // sixteen columns lie in one page: factor of the logits, exponent of the values (a page that holds nothing: a bit)
+        constexpr int NP = KW / 16;
+        float f[NP], e[NP], e_inv[NP];
+        uint32_t dead = 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const float2 sc = scale_s[k % SR][(half * KW + 16 * i) >> a.page_shift];
+          const int kb = __float_as_int(sc.x) & 0x7f800000, ve = (__float_as_int(sc.y) >> 23) & 255;
+          const bool none = kb == 0 || ve == 0;
+          f[i] = none ? 1.0f : __int_as_float(kb) * qs;
+          e[i] = (float)(ve - 127);
+          e_inv[i] = __int_as_float((254 - ve) << 23);
+          dead |= none ? 1u << i : 0u;
+        }
+        if (!(ok = wait_warp(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
         tc_fence_after();
         const uint32_t s_addr = tmem + lane_base + (uint32_t)qt * 128u + buf * KW;
         const int j0 = t * kTile + half * KW;  // first row of the step
@@ -270,33 +284,24 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
           uint32_t z[NC][32];
 #pragma unroll
           for (int i = 0; i < NC; ++i) tmem_ld32_nb(s_addr + 32u * i, z[i]);
-          // sixteen columns lie in one page: factor of the logits, exponent of the values.  False for a page that holds nothing.
-          auto page_of = [&](int i, float* f, float* e, float* e_inv) {
-            const float2 sc = scale_s[k % SR][(half * KW + 16 * i) >> a.page_shift];
-            const int kb = __float_as_int(sc.x) & 0x7f800000, ve = (__float_as_int(sc.y) >> 23) & 255;
-            *f = __int_as_float(kb) * qs;
-            *e = (float)(ve - 127);
-            *e_inv = __int_as_float((254 - ve) << 23);
-            return kb != 0 && ve != 0;
-          };
+#pragma unroll
+          for (int i = 0; i < NC; ++i) tc_wait_ld32_nb(z[i]);
+          if (masked || dead) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+              const int n = dead >> i & 1u ? 0 : limit - (j0 + 16 * i);
+#pragma unroll
+              for (int x = 0; x < 16; ++x) z[i / 2][16 * (i & 1) + x] = x < n ? z[i / 2][16 * (i & 1) + x] : 0xff800000u;
+            }
+          }
           float top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < NC; ++i) {
-            tc_wait_ld32_nb(z[i]);
+          for (int i = 0; i < NP; ++i) {
+            float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (masked) {
-                const int n = limit - (j0 + 32 * i + 16 * h);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) z[i][16 * h + e] = e < n ? z[i][16 * h + e] : 0xff800000u;
-              }
-              float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-              for (int e = 0; e < 16; e += 2)
-                mx[(e >> 1) & 1] = fmaxf(fmaxf(mx[(e >> 1) & 1], __uint_as_float(z[i][16 * h + e])), __uint_as_float(z[i][16 * h + e + 1]));
-              float f, e, e_inv;
-              if (page_of(2 * i + h, &f, &e, &e_inv)) top = fmaxf(top, fmaf(fmaxf(mx[0], mx[1]), f, e));
-            }
+            for (int x = 0; x < 16; x += 2)
+              mx[(x >> 1) & 1] = fmaxf(fmaxf(mx[(x >> 1) & 1], __uint_as_float(z[i / 2][16 * (i & 1) + x])), __uint_as_float(z[i / 2][16 * (i & 1) + x + 1]));
+            top = fmaxf(top, fmaf(fmaxf(mx[0], mx[1]), f[i], e[i]));
           }
           const float m_new = fmaxf(m_used, top);
           if (s == 0) {
@@ -329,24 +334,19 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             uint32_t r[16];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              float f, e, e_inv;
-              if (page_of(2 * i + h, &f, &e, &e_inv)) {
-                const u64 f2 = pack2(f, f), b2 = pack2(e - shift, e - shift);
-                u64 sum = 0ull;
+              const int c = 2 * i + h;
+              const u64 f2 = pack2(f[c], f[c]), b2 = pack2(e[c] - shift, e[c] - shift);
+              u64 sum = 0ull;
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                  float2 w = unpack2(fma2(pack2u(z[i][16 * h + 2 * x], z[i][16 * h + 2 * x + 1]), f2, b2));
-                  w.x = ex2_approx(w.x);
-                  w.y = ex2_approx(w.y);
-                  sum = add2(sum, pack2(w.x, w.y));
-                  r[8 * h + x] = pack_f16(w.x, w.y);
-                }
-                const float2 two = unpack2(sum);
-                l = fmaf(two.x + two.y, e_inv, l);
-              } else {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) r[8 * h + x] = 0u;
+              for (int x = 0; x < 8; ++x) {
+                float2 w = unpack2(fma2(pack2u(z[i][16 * h + 2 * x], z[i][16 * h + 2 * x + 1]), f2, b2));
+                w.x = ex2_approx(w.x);
+                w.y = ex2_approx(w.y);
+                sum = add2(sum, pack2(w.x, w.y));
+                r[8 * h + x] = pack_f16(w.x, w.y);
               }
+              const float2 two = unpack2(sum);
+              l = fmaf(two.x + two.y, e_inv[c], l);
             }
             tmem_st16(s_addr + KW / 2 + 16u * i, r);
           }
