@@ -449,46 +449,24 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
   }
 }
 
-// Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A warp has one query row, lane = d_h / 32 columns.
+// Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A problem that lies in several pieces is joined where its second
+// piece begins (so there are at most as many as CTAs); a warp has one of its query rows, lane = d_h / 32 columns.
 template <int DH>
-__global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const Attend8Args a, int attend_grid) {
+__global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const Attend8Args a) {
   constexpr int V = DH / 32, AT_ONCE = 16;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int i0 = blockIdx.x * kMergeWarps8 + warp, t = i0 / a.H_q, hq = i0 - t * a.H_q, l = blockIdx.y;
-  const int g = hq / a.n_rep;
-  // Lengths come from before the kernel that this one waits for, which had waited for them before it let this one start: they are read
-  // while that kernel runs.
-  bool live = t < a.n_tok, bad;
-  int b = live ? t : 0;
-  if (a.first && live) {                       // the sequence of token t
-    int lo = 0, hi = a.batch - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (a.first[mid + 1] > t) hi = mid; else lo = mid + 1;
-    }
-    b = lo;
-  }
-  const Seq s = load_seq(a, b, &bad);
-  const int tok = t - s.f0;
-  live = live && tok >= 0 && tok < s.n;
-  long long before;
-  const long long head = head_tiles(a, b, &before), total = head * a.H_kv * a.layers;
-  const int ctas = (int)min((long long)attend_grid, total);
-  int c0 = 0, c1 = 0, r = 0;
-  long long u0 = 0;
-  if (live) {
-    const int qp = tok / a.block_tok;
-    r = (tok - qp * a.block_tok) * a.n_rep + (hq - g * a.n_rep);
-    u0 = ((long long)l * a.H_kv + g) * head + before + tiles_before(a, s, qp, blocks_of(a, s));
-    c0 = piece_of8(total, ctas, u0);
-    c1 = piece_of8(total, ctas, u0 + tiles_of(rows_seen(a, s, qp)) - 1);
-  }
-  ptx::grid_dependency_wait();                 // the pieces come from the kernel before; every CTA waits, so that who waits for this
-  ptx::grid_dependency_launch();               // kernel has waited for that one
-  if (c0 == c1) return;                        // one piece: written where it was computed
+  const int lane = threadIdx.x & 31, r = blockIdx.y * kMergeWarps8 + (threadIdx.x >> 5), c_second = blockIdx.x + 1;
+  ptx::grid_dependency_wait();                 // every CTA waits, so that who waits for this kernel has waited for the one before
+  ptx::grid_dependency_launch();
+  const Place p = a.pieces[c_second].at;
+  const long long second = a.pieces[c_second].count, first = a.pieces[c_second - 1].count;
+  if (second == 0 || p.t == 0 || p.t > first) return;          // nothing; a problem's first piece; not its second
+  const int tok0 = p.qp * a.block_tok;
+  if (r >= min(a.block_tok, p.s.n - tok0) * a.n_rep) return;
+  const int c0 = c_second - 1;
+  int c1 = c_second;
+  for (long long rest = p.nt - p.t - second; rest > 0; rest -= a.pieces[c1].count) ++c1;
   // a problem that begins inside a piece is that piece's last one, and in the others the first
-  const size_t first = (size_t)c0 * 2 + (piece_begin8(total, ctas, c0) == u0 ? 0 : 1);
-  auto slot = [&](int c) { return (c == c0 ? first : (size_t)c * 2) * a.block_rows + r; };
+  auto slot = [&](int c) { return ((size_t)c * 2 + (c == c0 && p.t < first ? 1 : 0)) * a.block_rows + r; };
   float M = -INFINITY, sum = 0.0f, acc[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.0f;
@@ -530,7 +508,7 @@ __global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const 
     }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const size_t qh = ((size_t)(a.l0 + l) * a.n_tok + t) * a.H_q + hq;
+  const size_t qh = ((size_t)(a.l0 + p.l) * a.n_tok + p.s.f0 + tok0 + r / a.n_rep) * a.H_q + p.g * a.n_rep + r % a.n_rep;
   uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + qh * DH + lane * V);
 #pragma unroll
   for (int i = 0; i < V; i += 2) dst[i / 2] = ptx::pack_bf16(acc[i] * inv, acc[i + 1] * inv);
@@ -549,8 +527,7 @@ cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, con
                 : a.block_rows == 32 ? launch_as<DH, 32>(k_map, v_map, a, grid, device, s) : a.block_rows == 64 ? launch_as<DH, 64>(k_map, v_map, a, grid, device, s)
                 : launch_attend8_wide(k_map, v_map, DH, a, grid, device, s);
   if (e != cudaSuccess) return e;
-  const long long rows = (long long)a.n_tok * a.H_q;
-  e = launch_pdl(attend8_merge_kernel<DH>, dim3((unsigned)((rows + kMergeWarps8 - 1) / kMergeWarps8), a.layers), dim3(kMergeWarps8 * 32), 0, s, a, grid);
+  if (grid > 1) e = launch_pdl(attend8_merge_kernel<DH>, dim3(grid - 1, a.block_rows / kMergeWarps8), dim3(kMergeWarps8 * 32), 0, s, a);
   count_launch(kFamAttend8, 2);
   return e;
 }
@@ -565,7 +542,7 @@ int block_rows(int max_new, int n_rep) {
 
 // A piece leaves at most two results: its first and its last problem.
 size_t cache8_workspace_bytes(const xkv_cache8_config* c, int max_new) {
-  return (size_t)kPlanSms * 2 * block_rows(max_new, c->H_q / c->H_kv) * (c->d_h + 2) * sizeof(float);
+  return (size_t)kPlanSms * (2 * block_rows(max_new, c->H_q / c->H_kv) * (c->d_h + 2) * sizeof(float) + sizeof(Piece8));
 }
 
 cudaError_t launch_cache8_attend(const xkv_cache8_config* c, int l0, int l1, const __nv_bfloat16* q, const int32_t* first, int n_tok,
@@ -592,6 +569,7 @@ cudaError_t launch_cache8_attend(const xkv_cache8_config* c, int l0, int l1, con
   const int grid = sms < kPlanSms ? sms : kPlanSms;
   a.part = (float*)workspace;
   a.part_ml = reinterpret_cast<float2*>(a.part + (size_t)kPlanSms * 2 * a.block_rows * c->d_h);
+  a.pieces = reinterpret_cast<Piece8*>(a.part_ml + (size_t)kPlanSms * 2 * a.block_rows);
   return c->d_h == 128 ? launch_width<128>(k_map, v_map, a, grid, device, s) : launch_width<64>(k_map, v_map, a, grid, device, s);
 }
 

@@ -22,6 +22,7 @@ struct Attend8Args {
   const float* k_scale;
   const float* v_scale;
   int block_rows;                              // room for query rows in a piece's results
+  struct Piece8* pieces;                       // [CTA]
   float* part;                                 // [CTA][2][block_rows][d_h]
   float2* part_ml;                             // [CTA][2][block_rows] (m, l)
   __nv_bfloat16* out;
@@ -48,17 +49,17 @@ __device__ __forceinline__ int rows_seen(const Attend8Args& a, const Seq& s, int
 }
 __device__ __forceinline__ int tiles_of(int rows) { return max(1, (rows + kTile - 1) / kTile); }
 
-// sum over i < n of floor((a i + b) / m), all of them non-negative: Euclid's algorithm on (a, m).
-static __device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+// sum over i < n of floor((a i + b) / m), all of them below 2^31: Euclid's algorithm on (a, m).
+static __device__ long long floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
   long long sum = 0;
   while (n > 0) {
-    if (a >= m) { sum += n * (n - 1) / 2 * (a / m); a %= m; }
-    if (b >= m) { sum += n * (b / m); b %= m; }
-    const long long y = a * n + b;
+    if (a >= m) { sum += (long long)n * (n - 1) / 2 * (a / m); a %= m; }
+    if (b >= m) { sum += (long long)n * (b / m); b %= m; }
+    const uint32_t y = a * n + b;
     if (y < m) break;
     n = y / m;
     b = y % m;
-    const long long t = m;
+    const uint32_t t = m;
     m = a;
     a = t;
   }
@@ -70,7 +71,7 @@ static __device__ long long tiles_before(const Attend8Args& a, const Seq& s, int
   if (qp == n_qp) return tiles_before(a, s, qp - 1, n_qp) + tiles_of(rows_seen(a, s, qp - 1));
   const int most = kTile - s.base;             // blocks that see up to one tile count one
   const int ones = most > 0 ? min(qp, most / a.block_tok) : 0;
-  return ones + floor_sum(qp - ones, kTile, a.block_tok, s.base + (long long)(ones + 1) * a.block_tok + kTile - 1);
+  return ones + floor_sum(qp - ones, kTile, a.block_tok, (uint32_t)(s.base + (ones + 1) * a.block_tok + kTile - 1));
 }
 __device__ __forceinline__ long long tiles_of_head(const Attend8Args& a, const Seq& s) {
   if (s.n <= a.block_tok) return s.n > 0 ? tiles_of(rows_seen(a, s, 0)) : 0;
@@ -116,38 +117,38 @@ __device__ __forceinline__ long long lane_tiles(const Attend8Args& a, int b0, Se
   if (bad && report && a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
   return tiles_of_head(a, *s);
 }
-// By a whole warp: tiles of one head over the batch, and over the sequences before b.
-__device__ __forceinline__ long long head_tiles(const Attend8Args& a, int b, long long* before, bool report = false) {
-  long long all = 0, mine = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 32) {
-    Seq s;
-    const long long v = lane_tiles(a, b0, &s, report);
-    all += v;
-    if (b0 + (int)(threadIdx.x & 31) < b) mine += v;
-  }
-  *before = warp_sum(mine);
-  return warp_sum(all);
-}
-__device__ __forceinline__ long long piece_begin8(long long total, int ctas, int c) { return total * c / ctas; }
-__device__ __forceinline__ int piece_of8(long long total, int ctas, long long u) { return (int)(((u + 1) * ctas - 1) / total); }
+// What a CTA has: `count` tiles from a place on.
+struct Piece8 {
+  Place at;
+  long long count;
+};
 
-// By a whole warp: how many tiles CTA c has, and the place of the first.
+// By a whole warp: the tiles of CTA c.  They are written down for the merge, too.
 __device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int grid, long long* count, bool report) {
-  long long before;
-  const long long head = head_tiles(a, 0, &before, report), total = head * a.H_kv * a.layers;
+  Seq s = {};
+  const long long mine = lane_tiles(a, 0, &s, report);         // (most batches have 32 sequences at most: they are looked at once)
+  long long head = mine;
+  for (int b0 = 32; b0 < a.batch; b0 += 32) {
+    Seq x;
+    head += lane_tiles(a, b0, &x, report);
+  }
+  head = warp_sum(head);
+  const long long total = head * a.H_kv * a.layers;
   const int ctas = (int)min((long long)grid, total);
   Place p = {};
   *count = 0;
-  if (c >= ctas) return p;
-  const long long u0 = piece_begin8(total, ctas, c);
-  *count = piece_begin8(total, ctas, c + 1) - u0;
+  if (c >= ctas) {
+    if ((threadIdx.x & 31) == 0) a.pieces[c] = Piece8{p, 0};
+    return p;
+  }
+  const long long u0 = total * c / ctas;
+  *count = total * (c + 1) / ctas - u0;
   const long long lg = u0 / head;
   long long rest = u0 - lg * head;
   p.l = (int)(lg / a.H_kv);
   p.g = (int)(lg - (long long)p.l * a.H_kv);
   for (int b0 = 0; b0 < a.batch; b0 += 32) {   // (u0 is in the list: the search ends inside the batch)
-    Seq s = {};
-    const long long v = lane_tiles(a, b0, &s, false);
+    const long long v = b0 == 0 ? mine : lane_tiles(a, b0, &s, false);
     long long upto = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -176,6 +177,7 @@ __device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int gri
   p.qp = lo;
   p.t = (int)(rest - tiles_before(a, p.s, lo, p.n_qp));
   set_block(a, p);
+  if ((threadIdx.x & 31) == 0) a.pieces[c] = Piece8{p, *count};
   return p;
 }
 
