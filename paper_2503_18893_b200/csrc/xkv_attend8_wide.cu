@@ -168,18 +168,22 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         const uint8_t* src = gen + (L::kKeys + k % L::kCodes) * L::kSlot;
         uint8_t* dst = gen + kVAt + (k & 1u) * L::kValues;
         const bool some = (t + 1) * kTile > new0 + 1;          // rows that not all tokens of the block see
+        // pages that hold nothing
+        const float2 sc = scale_s[k % SR][min(lane, 127 >> a.page_shift)];
+        const uint32_t dead = __ballot_sync(0xffffffffu, (__float_as_int(sc.x) & 0x7f800000) == 0 || (__float_as_int(sc.y) & 0x7f800000) == 0);
 #pragma unroll 4
         for (int r0 = 0; r0 < kTile; r0 += STEP) {
-          const int r = r0 + ct / C, j = t * kTile + r;
+          // (the upper units of a row go with the lower ones of its neighbour: then stores of eight lanes meet all banks)
+          const int r = r0 + ((ct / C) ^ (c >> 2)), j = t * kTile + r;
           uint4 x = *reinterpret_cast<const uint4*>(src + tile_place<DH>(r, 2 * c));
-          const float2 sc = scale_s[k % SR][r >> a.page_shift];
-          const bool dead = j >= seen || (__float_as_int(sc.x) & 0x7f800000) == 0 || (__float_as_int(sc.y) & 0x7f800000) == 0;
-          if (dead) x = make_uint4(0u, 0u, 0u, 0u);
-          if (some && j > new0) {
-            const uint4 m = make_uint4(nan_codes(x.x), nan_codes(x.y), nan_codes(x.z), nan_codes(x.w));
-            if (m.x | m.y | m.z | m.w) {
-              atomicOr(&bad_s[seg & 15u][(j - new0) >> 5], 1u << ((j - new0) & 31));
-              x = make_uint4(x.x & ~m.x, x.y & ~m.y, x.z & ~m.z, x.w & ~m.w);
+          if (dead || some) {
+            if (j >= seen || (dead >> (r >> a.page_shift) & 1u)) x = make_uint4(0u, 0u, 0u, 0u);
+            if (j > new0) {
+              const uint4 m = make_uint4(nan_codes(x.x), nan_codes(x.y), nan_codes(x.z), nan_codes(x.w));
+              if (m.x | m.y | m.z | m.w) {
+                atomicOr(&bad_s[seg & 15u][(j - new0) >> 5], 1u << ((j - new0) & 31));
+                x = make_uint4(x.x & ~m.x, x.y & ~m.y, x.z & ~m.z, x.w & ~m.w);
+              }
             }
           }
           const uint32_t w[4] = {x.x, x.y, x.z, x.w};
