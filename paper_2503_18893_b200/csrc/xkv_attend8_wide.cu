@@ -11,6 +11,7 @@
 //   issuers    a warp for each 128 rows of Q: S two steps ahead, O += P V with P in tensor memory, where it lies over S
 //   softmax    a warpgroup for each 128 rows of Q: thread = row, so that maxima and sums need no shuffle.  O is rescaled only when a
 //              maximum has grown by more than 2^8 (fp16 holds weights of 2^8, and of 2^-24).
+//   scales     a warp: what 16 columns of a page need, worked out once per page
 // A step is a tile of 128 rows of the cache for 128 rows of Q, and half a tile for 256 (tensor memory holds two steps of S and O).
 #include <math.h>
 
@@ -33,7 +34,12 @@ struct Wide8 {
   static constexpr int kBytes = 1024 + (kKeys + kCodes) * kSlot + 2 * kValues + QT * kQBytes;
 };
 template <int QT>
-constexpr int wide_threads() { return QT * 128 + 128 + 32 + QT * 32; }
+constexpr int wide_threads() { return QT * 128 + 256; }      // (whole warpgroups: registers move between them)
+// Registers a thread: a softmax warpgroup keeps 128 logits; the sum over warpgroups stays that of the launch (128 and 168 a thread).
+template <int QT>
+constexpr int kSoftmaxRegs = QT == 2 ? 168 : 232;
+template <int QT>
+constexpr int kOtherRegs = QT == 2 ? 88 : 128;
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
@@ -48,14 +54,16 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
   using L = Wide8<DH, QT>;
   constexpr int SR = 8;
   using Ring = Ring8<L::kKeys, L::kCodes, SR>;
-  constexpr int KW = QT == 2 ? 64 : 128, SPT = kTile / KW;
+  constexpr int KW = QT == 2 ? 64 : 128, SPT = kTile / KW;     // rows of the cache of a step, steps of a tile
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars_s[Ring::kBars + 20];
+  __shared__ uint64_t bars_s[Ring::kBars + 20 + SR];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   __shared__ Place place_s;
   __shared__ long long count_s;
   __shared__ float2 scale_s[SR][8];
+  __shared__ float4 page_s[SR][8];             // of a tile's pages: keys' scale, values' exponent, its power of two turned over
+  __shared__ uint32_t dead_s[SR];              // which of them hold nothing
   // New rows of a block with value codes that are NaN, by segment: converters are less than eight segments ahead of the slower warpgroup.
   __shared__ uint32_t bad_s[16][8];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -63,14 +71,15 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
   constexpr uint32_t kVAt = (L::kKeys + L::kCodes) * L::kSlot, kQAt = kVAt + 2 * L::kValues;
   const uint32_t bars = smem_u32(bars_s);
   const Ring ring{base, bars, scale_s};
-  const uint32_t b_s = bars + 8 * Ring::kBars, b_p = b_s + 32, b_o = b_p + 32, b_q = b_o + 32, b_vf = b_q + 16, b_ve = b_vf + 16, b_drain = b_ve + 16;
+  const uint32_t b_s = bars + 8 * Ring::kBars, b_p = b_s + 32, b_o = b_p + 32, b_q = b_o + 32, b_vf = b_q + 16, b_ve = b_vf + 16, b_drain = b_ve + 16, b_pg = b_drain + 16;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  constexpr int kConvert = QT * 4, kProducer = kConvert + 4, kIssuer = kProducer + 1;
+  constexpr int kConvert = QT * 4, kProducer = kConvert + 4, kScales = kProducer + 1, kIssuer = kScales + 1;
 
   if (tid == 0) {
     ring.init(QT, 4);
     for (int i = 0; i < 4; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_p + 8 * i, 4); mbar_init(b_o + 8 * i, 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(b_q + 8 * i, 4); mbar_init(b_vf + 8 * i, 4); mbar_init(b_ve + 8 * i, QT); mbar_init(b_drain + 8 * i, 1); }
+    for (int i = 0; i < SR; ++i) mbar_init(b_pg + 8 * i, 1);
     fence_mbar_init();
     abort_s = 0;
   }
@@ -95,121 +104,8 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
   Place p = place_s;
   uint32_t n_loaded = 0;                       // producer: tiles asked for
 
-  if (left > 0 && warp == kProducer) {
-    n_loaded = ring.template produce<DH>(a, wt, &k_map, &v_map, p, left);
-  } else if (left > 0 && warp >= kIssuer) {
-    // ---- branches outside the issue are taken on a vote and descriptors differ by constants, so that they stay in uniform registers
-    const int qt = warp - kIssuer;
-    constexpr uint32_t idesc_s = idesc_e4m3_f32(128, KW);
-    constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((128u >> 4) << 24);     // fp16; V is read along its rows
-    const uint64_t q_desc = smem_desc_rows<DH>(base + kQAt + qt * L::kQBytes), k_desc = smem_desc_rows<DH>(base);
-    const uint64_t v_desc = (smem_desc_sw128(base + kVAt, 0) & ~(0xFFFFull << 16)) | ((uint64_t)(L::kSlab >> 4) << 16);
-    const uint32_t s_tmem = tmem + (uint32_t)qt * 128u, o_tmem = tmem + 256u + (uint32_t)qt * 128u;
-    uint32_t k0 = 0, st = 0, n_o = 0, seg = 0; // tiles, steps, commits on b_o and segments so far
-    bool ok = true;
-    auto logits = [&](uint32_t buf, uint32_t k, int half) {
-      const uint64_t kd = k_desc + (uint64_t)((k % L::kKeys) * (uint32_t)(L::kSlot >> 4) + (uint32_t)half * (KW * DH >> 4));
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < DH / 32; ++i)
-          tc_mma_e4m3(s_tmem + buf * KW, q_desc + (uint64_t)(h * (L::kQPart >> 4) + 2 * i), kd + (uint64_t)(2 * i), idesc_s, h | i ? 1u : 0u);
-      tc_commit(b_s + 16 * qt + 8 * buf);
-      if (half == SPT - 1) tc_commit(ring.k_empty(k));
-    };
-    auto keys = [&](uint32_t k) { return wait_warp(wt, ring.k_full(k), Ring::k_parity(k)); };
-    while (left > 0 && ok) {
-      const int t1 = (int)min((long long)p.nt, p.t + left), steps = (t1 - p.t) * SPT;
-      left -= t1 - p.t;
-      ok = wait_warp(wt, b_q + 8 * qt, seg & 1u);
-      for (int s = 0; s < min(2, steps) && ok; ++s) {          // two steps of logits ahead
-        if (s % SPT == 0 && !(ok = keys(k0 + s / SPT))) break;
-        tc_fence_after();
-        if (elect_one()) logits((st + s) & 1u, k0 + s / SPT, s % SPT);
-        __syncwarp();
-      }
-      for (int s = 0; s < steps && ok; ++s) {
-        const uint32_t buf = (st + s) & 1u, k = k0 + s / SPT, kn = k0 + (s + 2) / SPT;
-        const bool more = s + 2 < steps;
-        if (s % SPT == 0 && !(ok = wait_warp(wt, b_vf + 8 * (k & 1u), (k >> 1) & 1u))) break;
-        if (more && s % SPT == 0 && !(ok = keys(kn))) break;
-        if (!(ok = wait_warp(wt, b_p + 16 * qt + 8 * buf, ((st + s) >> 1) & 1u))) break;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t vd = v_desc + (uint64_t)((k & 1u) * (uint32_t)(L::kValues >> 4) + (uint32_t)(s % SPT) * (KW * 8));
-#pragma unroll
-          for (int i = 0; i < KW / 16; ++i)
-            tc_mma_bf16_ts(o_tmem, s_tmem + buf * KW + KW / 2 + (uint32_t)i * 8u, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, (s | i) ? 1u : 0u);
-          if (s % SPT == SPT - 1) tc_commit(b_ve + 8 * (k & 1u));
-          // the logits after the next follow the product that reads P, which lies where they go; their commit tells of both
-          if (more) logits(buf, kn, (s + 2) % SPT); else tc_commit(b_o + 16 * qt + 8 * (n_o & 1u));
-        }
-        __syncwarp();
-        n_o += more ? 0u : 1u;
-      }
-      st += steps;
-      k0 += t1 - p.t;
-      ++seg;
-      if (left > 0 && ok) next_problem(a, p);
-    }
-  } else if (left > 0 && warp >= kConvert) {
-    constexpr int C = DH / 16, STEP = 128 / C; // 16-byte units of a row of codes; rows per round
-    const int ct = tid - kConvert * 32, c = ct % C;
-    uint32_t k = 0, seg = 0;
-    bool ok = true;
-    while (left > 0 && ok) {
-      const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left);
-      left -= t1 - t0;
-      const int seen = rows_seen(a, p.s, p.qp), new0 = p.s.base + p.qp * a.block_tok;
-      if (ct < 8) bad_s[(seg + 8) & 15u][ct] = 0u;
-      for (int t = t0; t < t1; ++t, ++k) {
-        if (!(ok = wait_warp(wt, ring.v_full(k), Ring::v_parity(k)) && wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k)) &&
-                   wait_warp(wt, b_ve + 8 * (k & 1u), ((k >> 1) & 1u) ^ 1u))) break;
-        const uint8_t* src = gen + (L::kKeys + k % L::kCodes) * L::kSlot;
-        uint8_t* dst = gen + kVAt + (k & 1u) * L::kValues;
-        const bool some = (t + 1) * kTile > new0 + 1;          // rows that not all tokens of the block see
-        // pages that hold nothing
-        const float2 sc = scale_s[k % SR][min(lane, 127 >> a.page_shift)];
-        const uint32_t dead = __ballot_sync(0xffffffffu, (__float_as_int(sc.x) & 0x7f800000) == 0 || (__float_as_int(sc.y) & 0x7f800000) == 0);
-#pragma unroll 4
-        for (int r0 = 0; r0 < kTile; r0 += STEP) {
-          // (the upper units of a row go with the lower ones of its neighbour: then stores of eight lanes meet all banks)
-          const int r = r0 + ((ct / C) ^ (c >> 2)), j = t * kTile + r;
-          uint4 x = *reinterpret_cast<const uint4*>(src + tile_place<DH>(r, 2 * c));
-          if (dead || some) {
-            if (j >= seen || (dead >> (r >> a.page_shift) & 1u)) x = make_uint4(0u, 0u, 0u, 0u);
-            if (j > new0) {
-              const uint4 m = make_uint4(nan_codes(x.x), nan_codes(x.y), nan_codes(x.z), nan_codes(x.w));
-              if (m.x | m.y | m.z | m.w) {
-                atomicOr(&bad_s[seg & 15u][(j - new0) >> 5], 1u << ((j - new0) & 31));
-                x = make_uint4(x.x & ~m.x, x.y & ~m.y, x.z & ~m.z, x.w & ~m.w);
-              }
-            }
-          }
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-          uint32_t h[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const __half2 lo = decode_f16x2(w[e]), hi = decode_f16x2(w[e] >> 16);
-            h[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
-            h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
-          }
-          uint8_t* row = dst + (c >> 2) * L::kSlab + r * 128;  // 64 columns: four units of codes, eight of values
-          const int u = 2 * (c & 3);
-          *reinterpret_cast<uint4*>(row + ((u ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(row + (((u + 1) ^ (r & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
-        }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(b_vf + 8 * (k & 1u));
-          mbar_arrive(ring.v_empty(k));
-        }
-      }
-      ++seg;
-      if (left > 0 && ok) next_problem(a, p);
-    }
-  } else if (left > 0) {
+  if (left > 0 && warp < kConvert) {
+    regs_more<kSoftmaxRegs<QT>>();
     const int qt = warp >> 2, row = tid & 127;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     uint8_t* q_gen = gen + kQAt + qt * L::kQBytes;
@@ -261,41 +157,34 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       float m_used = -INFINITY, l = 0.0f;
       const int steps = (t1 - t0) * SPT;
       for (int s = 0; s < steps; ++s, ++st) {
-        const int t = t0 + s / SPT, half = s % SPT;
+        const int half = s % SPT;
         const uint32_t buf = st & 1u, k = k0 + (uint32_t)(s / SPT);
-        if (half == 0 && !(ok = wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k)))) break;
-        // sixteen columns lie in one page: factor of the logits, exponent of the values (a page that holds nothing: a bit)
-        constexpr int NP = KW / 16;
-        float f[NP], e[NP], e_inv[NP];
-        uint32_t dead = 0;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const float2 sc = scale_s[k % SR][(half * KW + 16 * i) >> a.page_shift];
-          const int kb = __float_as_int(sc.x) & 0x7f800000, ve = (__float_as_int(sc.y) >> 23) & 255;
-          const bool none = kb == 0 || ve == 0;
-          f[i] = none ? 1.0f : __int_as_float(kb) * qs;
-          e[i] = (float)(ve - 127);
-          e_inv[i] = __int_as_float((254 - ve) << 23);
-          dead |= none ? 1u << i : 0u;
-        }
-        if (!(ok = wait_warp(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
+        if (!(ok = wait_warp(wt, b_pg + 8 * (k % SR), (k / SR) & 1u) && wait_warp(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
         tc_fence_after();
         const uint32_t s_addr = tmem + lane_base + (uint32_t)qt * 128u + buf * KW;
-        const int j0 = t * kTile + half * KW;  // first row of the step
+        const int j0 = (t0 + s / SPT) * kTile + half * KW;     // first row of the step
+        const uint32_t dead = dead_s[k % SR];
         if (warp_live) {
-          constexpr int NC = KW / 32;
-          const bool masked = j0 + KW > new0 + 1;
+          constexpr int NC = KW / 32, NP = KW / 16;
           uint32_t z[NC][32];
 #pragma unroll
           for (int i = 0; i < NC; ++i) tmem_ld32_nb(s_addr + 32u * i, z[i]);
+          float f[NP], e[NP], e_inv[NP];       // sixteen columns lie in one page
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            const float4 x = page_s[k % SR][(half * KW + 16 * i) >> a.page_shift];
+            f[i] = x.x * qs;
+            e[i] = x.y;
+            e_inv[i] = x.z;
+          }
 #pragma unroll
           for (int i = 0; i < NC; ++i) tc_wait_ld32_nb(z[i]);
-          if (masked || dead) {
+          if (j0 + KW > new0 + 1 || dead) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-              const int n = dead >> i & 1u ? 0 : limit - (j0 + 16 * i);
+              const int see = dead >> ((half * KW + 16 * i) >> a.page_shift) & 1u ? 0 : limit - (j0 + 16 * i);
 #pragma unroll
-              for (int x = 0; x < 16; ++x) z[i / 2][16 * (i & 1) + x] = x < n ? z[i / 2][16 * (i & 1) + x] : 0xff800000u;
+              for (int x = 0; x < 16; ++x) z[i / 2][16 * (i & 1) + x] = x < see ? z[i / 2][16 * (i & 1) + x] : 0xff800000u;
             }
           }
           float top = -INFINITY;
@@ -317,9 +206,9 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
               const bool next = s + 1 < steps;
               if (!(ok = wait_warp(wt, (next ? b_s + 8 * (buf ^ 1u) : b_o + 8 * (n_o & 1u)) + 16 * qt, ((next ? st + 1 : n_o) >> 1) & 1u))) break;
               tc_fence_after();
-              const float f = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
+              const float g = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
               if (grow) m_used = m_new;
-              l *= f;
+              l *= g;
 #pragma unroll 1
               for (int c = 0; c < DH; c += 16) {
                 float o[16];
@@ -327,7 +216,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
                 tmem_ld<16>(o_addr + (uint32_t)c, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(o[e] * f);
+                for (int x = 0; x < 16; ++x) r[x] = __float_as_uint(o[x] * g);
                 tmem_st16(o_addr + (uint32_t)c, r);
               }
             }
@@ -423,6 +312,133 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       tc_fence_before();
       ++seg;
       if (left > 0) next_problem(a, p);
+    }
+  } else if (left > 0 && warp < kProducer) {
+    regs_fewer<kOtherRegs<QT>>();
+    constexpr int C = DH / 16, STEP = 128 / C; // 16-byte units of a row of codes; rows per round
+    const int ct = tid - kConvert * 32, c = ct % C;
+    uint32_t k = 0, seg = 0;
+    bool ok = true;
+    while (left > 0 && ok) {
+      const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left);
+      left -= t1 - t0;
+      const int seen = rows_seen(a, p.s, p.qp), new0 = p.s.base + p.qp * a.block_tok;
+      if (ct < 8) bad_s[(seg + 8) & 15u][ct] = 0u;
+      for (int t = t0; t < t1; ++t, ++k) {
+        if (!(ok = wait_warp(wt, ring.v_full(k), Ring::v_parity(k)) && wait_warp(wt, b_pg + 8 * (k % SR), (k / SR) & 1u) &&
+                   wait_warp(wt, b_ve + 8 * (k & 1u), ((k >> 1) & 1u) ^ 1u))) break;
+        const uint8_t* src = gen + (L::kKeys + k % L::kCodes) * L::kSlot;
+        uint8_t* dst = gen + kVAt + (k & 1u) * L::kValues;
+        const bool some = (t + 1) * kTile > new0 + 1;          // rows that not all tokens of the block see
+        const uint32_t dead = dead_s[k % SR];
+#pragma unroll 2
+        for (int r0 = 0; r0 < kTile; r0 += STEP) {
+          // (the upper units of a row go with the lower ones of its neighbour: then stores of eight lanes meet all banks)
+          const int r = r0 + ((ct / C) ^ (c >> 2)), j = t * kTile + r;
+          uint4 x = *reinterpret_cast<const uint4*>(src + tile_place<DH>(r, 2 * c));
+          if (dead || some) {
+            if (j >= seen || (dead >> (r >> a.page_shift) & 1u)) x = make_uint4(0u, 0u, 0u, 0u);
+            if (j > new0) {
+              const uint4 m = make_uint4(nan_codes(x.x), nan_codes(x.y), nan_codes(x.z), nan_codes(x.w));
+              if (m.x | m.y | m.z | m.w) {
+                atomicOr(&bad_s[seg & 15u][(j - new0) >> 5], 1u << ((j - new0) & 31));
+                x = make_uint4(x.x & ~m.x, x.y & ~m.y, x.z & ~m.z, x.w & ~m.w);
+              }
+            }
+          }
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          uint32_t h[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const __half2 lo = decode_f16x2(w[e]), hi = decode_f16x2(w[e] >> 16);
+            h[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
+            h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
+          }
+          uint8_t* row = dst + (c >> 2) * L::kSlab + r * 128;  // 64 columns: four units of codes, eight of values
+          const int u = 2 * (c & 3);
+          *reinterpret_cast<uint4*>(row + ((u ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(row + (((u + 1) ^ (r & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(b_vf + 8 * (k & 1u));
+          mbar_arrive(ring.v_empty(k));
+        }
+      }
+      ++seg;
+      if (left > 0 && ok) next_problem(a, p);
+    }
+  } else if (left > 0) {
+    regs_fewer<kOtherRegs<QT>>();
+    if (warp == kProducer) {
+      n_loaded = ring.template produce<DH>(a, wt, &k_map, &v_map, p, left);
+    } else if (warp == kScales) {
+      for (uint32_t k = 0; k < (uint32_t)count_s; ++k) {
+        if (!wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k))) break;
+        const float2 sc = scale_s[k % SR][min(lane, 127 >> a.page_shift)];
+        const int kb = __float_as_int(sc.x) & 0x7f800000, ve = (__float_as_int(sc.y) >> 23) & 255;
+        const uint32_t dead = __ballot_sync(0xffffffffu, kb == 0 || ve == 0);
+        if (lane < 8) page_s[k % SR][lane] = make_float4(kb == 0 ? 1.0f : __int_as_float(kb), (float)(ve - 127), __int_as_float((254 - ve) << 23), 0.0f);
+        if (lane == 0) dead_s[k % SR] = dead;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_pg + 8 * (k % SR));
+      }
+    } else if (warp < kIssuer + QT) {
+      // ---- branches outside the issue are taken on a vote and descriptors differ by constants, so that they stay in uniform registers
+      const int qt = warp - kIssuer;
+      constexpr uint32_t idesc_s = idesc_e4m3_f32(128, KW);
+      constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((128u >> 4) << 24);   // fp16; V is read along its rows
+      const uint64_t q_desc = smem_desc_rows<DH>(base + kQAt + qt * L::kQBytes), k_desc = smem_desc_rows<DH>(base);
+      const uint64_t v_desc = (smem_desc_sw128(base + kVAt, 0) & ~(0xFFFFull << 16)) | ((uint64_t)(L::kSlab >> 4) << 16);
+      const uint32_t s_tmem = tmem + (uint32_t)qt * 128u, o_tmem = tmem + 256u + (uint32_t)qt * 128u;
+      uint32_t k0 = 0, st = 0, n_o = 0, seg = 0;               // tiles, steps, commits on b_o and segments so far
+      bool ok = true;
+      auto logits = [&](uint32_t buf, uint32_t k, int half) {
+        const uint64_t kd = k_desc + (uint64_t)((k % L::kKeys) * (uint32_t)(L::kSlot >> 4) + (uint32_t)half * (KW * DH >> 4));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < DH / 32; ++i)
+            tc_mma_e4m3(s_tmem + buf * KW, q_desc + (uint64_t)(h * (L::kQPart >> 4) + 2 * i), kd + (uint64_t)(2 * i), idesc_s, h | i ? 1u : 0u);
+        tc_commit(b_s + 16 * qt + 8 * buf);
+        if (half == SPT - 1) tc_commit(ring.k_empty(k));
+      };
+      auto keys = [&](uint32_t k) { return wait_warp(wt, ring.k_full(k), Ring::k_parity(k)); };
+      while (left > 0 && ok) {
+        const int n = (int)min((long long)p.nt, p.t + left) - p.t, steps = n * SPT;
+        left -= n;
+        ok = wait_warp(wt, b_q + 8 * qt, seg & 1u);
+        for (int s = 0; s < min(2, steps) && ok; ++s) {        // two steps of logits ahead
+          if (s % SPT == 0 && !(ok = keys(k0 + s / SPT))) break;
+          tc_fence_after();
+          if (elect_one()) logits((st + s) & 1u, k0 + s / SPT, s % SPT);
+          __syncwarp();
+        }
+        for (int s = 0; s < steps && ok; ++s) {
+          const uint32_t buf = (st + s) & 1u, k = k0 + s / SPT, kn = k0 + (s + 2) / SPT;
+          const bool more = s + 2 < steps;
+          if (s % SPT == 0 && !(ok = wait_warp(wt, b_vf + 8 * (k & 1u), (k >> 1) & 1u))) break;
+          if (more && s % SPT == 0 && !(ok = keys(kn))) break;
+          if (!(ok = wait_warp(wt, b_p + 16 * qt + 8 * buf, ((st + s) >> 1) & 1u))) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t vd = v_desc + (uint64_t)((k & 1u) * (uint32_t)(L::kValues >> 4) + (uint32_t)(s % SPT) * (KW * 8));
+#pragma unroll
+            for (int i = 0; i < KW / 16; ++i)
+              tc_mma_bf16_ts(o_tmem, s_tmem + buf * KW + KW / 2 + (uint32_t)i * 8u, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, (s | i) ? 1u : 0u);
+            if (s % SPT == SPT - 1) tc_commit(b_ve + 8 * (k & 1u));
+            // the logits after the next follow the product that reads P, which lies where they go; their commit tells of both
+            if (more) logits(buf, kn, (s + 2) % SPT); else tc_commit(b_o + 16 * qt + 8 * (n_o & 1u));
+          }
+          __syncwarp();
+          n_o += more ? 0u : 1u;
+        }
+        st += steps;
+        k0 += n;
+        ++seg;
+        if (left > 0 && ok) next_problem(a, p);
+      }
     }
   }
 
