@@ -31,34 +31,38 @@ namespace xkv {
 
 namespace {
 
-constexpr int kThreads8 = 320;                 // two warpgroups, producer, issuer
-constexpr int kProducer8 = 8, kIssuer8 = 9;
+constexpr int kThreads8 = 512;                 // two warpgroups of softmax, one of queries and results; producer, two issuers
+constexpr int kHelper8 = 8, kProducer8 = 12, kLogits8 = 13, kValues8 = 14;
 constexpr int kMergeWarps8 = 8;
 constexpr float kTop = 8.0f, kSet = 4.0f;      // log2: a weight's bound; where a column's largest weight is put
 
+// N columns, and the N behind them.
 template <int N>
-__device__ __forceinline__ void load_columns(uint32_t addr, float (&v)[N]) {
+__device__ __forceinline__ void load_columns(uint32_t addr, float (&u)[N], float (&v)[N]) {
   if constexpr (N <= 16) {
-    ptx::tmem_ld<N>(addr, v);
+    ptx::tmem_ld<N>(addr, u);
+    ptx::tmem_ld<N>(addr + N, v);
+    ptx::tc_wait_ld();
   } else {
-#pragma unroll
-    for (int c = 0; c < N; c += 32) ptx::tmem_ld32_nb(addr + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
-#pragma unroll
-    for (int c = 0; c < N; c += 32) ptx::tc_wait_ld32_nb(*reinterpret_cast<uint32_t(*)[32]>(v + c));
-    return;
+    auto& x = *reinterpret_cast<uint32_t(*)[32]>(u);
+    auto& y = *reinterpret_cast<uint32_t(*)[32]>(v);
+    ptx::tmem_ld32_nb(addr, x);
+    ptx::tmem_ld32_nb(addr + 32, y);
+    ptx::tc_wait_ld32_nb(x);
+    ptx::tc_wait_ld32_nb(y);
   }
-  ptx::tc_wait_ld();
 }
 
 template <int DH, int RB>
 struct Shape8 {
-  static constexpr int kQ = RB < 16 ? 16 : RB;                 // columns of S (a product is 16 wide at least)
-  static constexpr int kP = (3 * RB + 15) / 16 * 16;           // columns of O: three groups of RB
+  static constexpr int kQ = 2 * RB;                            // columns of S: two codes of a query
+  static constexpr int kP = (3 * RB + 15) / 16 * 16;           // columns of O: three codes of a weight
   static constexpr int kSlot = kTile * DH;
-  static constexpr int kSlots = DH == 64 ? 8 : RB == 64 ? 4 : 5;           // tiles of keys, and as many of values
+  static constexpr int kSlots = DH == 64 ? 8 : 5;              // tiles of keys, and as many of values
+  static constexpr int kAhead = RB == 32 ? 2 : 4;              // tiles of S in tensor memory
   static constexpr int kQBytes = kQ * DH, kPBytes = kP * kTile;
   static constexpr int kBytes = 1024 + 2 * kSlots * kSlot + 2 * kPBytes + 2 * kQBytes;
-  static constexpr int kTmem = RB == 64 ? 512 : RB == 32 ? 256 : 128;      // 2 (kQ + kP), rounded up
+  static constexpr int kTmem = RB == 8 ? 256 : 512;            // S of tiles ahead, O of two warpgroups for two problems; rounded up
 };
 
 // Sums of N columns over the lanes of a warp: lane i gets those of columns i, i + 32, ...
@@ -91,36 +95,39 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
   using namespace ptx;
   using L = Shape8<DH, RB>;
   using Ring = Ring8<L::kSlots, L::kSlots, 2 * L::kSlots>;
-  constexpr int NQ = L::kQ, NP = L::kP, SR = 2 * L::kSlots;
+  constexpr int NQ = L::kQ, NP = L::kP, SR = 2 * L::kSlots, NB = L::kAhead;
+  static_assert(L::kSlots >= NB, "S of a tile is read before its keys' slot is multiplied again");
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars_s[Ring::kBars + 8];
+  __shared__ uint64_t bars_s[Ring::kBars + 12];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s;
   __shared__ Place place_s;
   __shared__ long long count_s;
   __shared__ float2 scale_s[SR][8];            // of a tile's pages: keys', values'
-  __shared__ float2 info_s[2][RB];             // of a column: factor of its query, bound that its z may not pass
-  __shared__ __align__(16) float sub_s[2][RB]; // what is taken off z (m)
-  __shared__ float fac_s[2][RB], top_s[2][4][RB], sum_s[2][4][RB];
-  __shared__ uint32_t bad_s[2];                // new rows of the block's tokens with value codes that are NaN
+  // By segment (two in turns) and warpgroup, of a column: factor of its query, bound that its z may not pass; what is taken off z (m);
+  // sums of weights
+  __shared__ float2 info_s[2][2][RB];
+  __shared__ __align__(16) float sub_s[2][2][RB];
+  __shared__ float sum_s[2][2][4][RB];
+  __shared__ float fac_s[2][RB], top_s[2][4][RB];
+  __shared__ uint32_t bad_s[2];                // by segment: new rows of the block's tokens with value codes that are NaN
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
-  constexpr uint32_t kPAt = 2 * L::kSlots * L::kSlot, kQAt = kPAt + 2 * L::kPBytes;         // ring, weights, queries (high, low)
+  constexpr uint32_t kPAt = 2 * L::kSlots * L::kSlot, kQAt = kPAt + 2 * L::kPBytes;         // ring, weights, queries
   const uint32_t bars = smem_u32(bars_s);
+  // A slot is empty when its product is done, which is also what tells of S and O: k_empty of a tile "S is there", v_empty "O has it"
   const Ring ring{base, bars, scale_s};
-  const uint32_t b_s = bars + 8 * Ring::kBars, b_p = b_s + 16, b_o = b_p + 16, b_q = b_o + 16, b_drain = b_q + 8;
+  const uint32_t b_p = bars + 8 * Ring::kBars, b_q = b_p + 32, b_done = b_q + 16, b_free = b_done + 16, b_drain = b_free + 16;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
     ring.init(1, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(b_s + 8 * i, 1); mbar_init(b_p + 8 * i, 4); mbar_init(b_o + 8 * i, 1); }
-    mbar_init(b_q, 8);
-    mbar_init(b_drain, 1);
+    for (int i = 0; i < 4; ++i) mbar_init(b_p + 8 * i, 4);
+    for (int i = 0; i < 2; ++i) { mbar_init(b_q + 8 * i, 4); mbar_init(b_done + 8 * i, 9); mbar_init(b_free + 8 * i, 4); mbar_init(b_drain + 8 * i, 1); }
     fence_mbar_init();
     abort_s = 0;
   }
-  for (int i = tid; i < 2 * L::kPBytes / 16; i += kThreads8) *reinterpret_cast<uint4*>(gen + kPAt + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-  if (warp == kIssuer8) {
+  if (warp == kLogits8) {
     tmem_alloc(smem_u32(&tmem_s), L::kTmem);
     tmem_relinquish();
   }
@@ -139,109 +146,182 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
   long long left = count_s;
   Place p = place_s;
   uint32_t n_loaded = 0;                       // producer: tiles asked for
+  const uint64_t ring_desc = smem_desc_rows<DH>(base);
 
   if (left > 0 && warp == kProducer8) {
     n_loaded = ring.template produce<DH>(a, wt, &k_map, &v_map, p, left);
-  } else if (left > 0 && warp == kIssuer8) {
-    constexpr uint32_t idesc_s = idesc_e4m3_f32(128, NQ), idesc_o = idesc_e4m3_f32(DH, NP) | (1u << 15);     // V is read along its rows
-    const uint64_t ring_desc = smem_desc_rows<DH>(base), q_desc = smem_desc_rows<DH>(base + kQAt), p_desc = smem_desc_rows<128>(base + kPAt);
-    uint32_t k0 = 0, seg = 0;                  // tiles and segments so far
+  } else if (left > 0 && warp == kLogits8) {
+    // ---- S of tile k, as soon as its keys are in and the weights of the tile that had its place are formed
+    constexpr uint32_t idesc = idesc_e4m3_f32(128, NQ);
+    uint32_t k = 0, seg = 0;
     bool ok = true;
-    auto keys = [&](uint32_t k) { return wait_warp(wt, ring.k_full(k), Ring::k_parity(k)); };
-    auto logits = [&](uint32_t k) {            // S of tile k, by one thread
-      const uint64_t kd = ring_desc + (uint64_t)((k % L::kSlots) * (uint32_t)(L::kSlot >> 4));
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < DH / 32; ++i)
-          tc_mma_e4m3(tmem + (k & 1u) * NQ, kd + (uint64_t)(2 * i), q_desc + (uint64_t)(h * (L::kQBytes >> 4) + 2 * i), idesc_s, h | i ? 1u : 0u);
-      tc_commit(b_s + 8 * (k & 1u));
-      tc_commit(ring.k_empty(k));
-    };
     while (left > 0 && ok) {
       const int n = (int)min((long long)p.nt, p.t + left) - p.t;
       left -= n;
-      ok = wait_warp(wt, b_q, seg & 1u);
-      for (int s = 0; s < min(2, n) && ok; ++s) {
-        if (!(ok = keys(k0 + s))) break;
-        tc_fence_after();
-        if (elect_one()) logits(k0 + s);
-        __syncwarp();
-      }
-      for (int s = 0; s < n && ok; ++s) {
-        const uint32_t k = k0 + s, w = k & 1u;
-        if (!(ok = wait_warp(wt, b_p + 8 * w, (k >> 1) & 1u))) break;
-        const bool more = s + 2 < n;
-        // S two ahead goes first where its keys are in: the warpgroup waits for it
-        const bool early = more && __all_sync(0xffffffffu, mbar_test(ring.k_full(k + 2), Ring::k_parity(k + 2)));
-        tc_fence_after();
-        if (early) {
-          if (elect_one()) logits(k + 2);
-          __syncwarp();
-        }
-        if (!(ok = wait_warp(wt, ring.v_full(k), Ring::v_parity(k)))) break;
+      ok = wait_warp(wt, b_q + 8 * (seg & 1u), (seg >> 1) & 1u);
+      const uint64_t qd = smem_desc_rows<DH>(base + kQAt + (seg & 1u) * L::kQBytes);
+      for (int s = 0; s < n && ok; ++s, ++k) {
+        if (!(ok = wait_warp(wt, ring.k_full(k), Ring::k_parity(k)))) break;
+        if (k >= NB && !(ok = wait_warp(wt, b_p + 8 * (k % NB), (k / NB - 1) & 1u))) break;
         tc_fence_after();
         if (elect_one()) {
-          const uint64_t vd = ring_desc + (uint64_t)((L::kSlots + k % L::kSlots) * (uint32_t)(L::kSlot >> 4)), pd = p_desc + (uint64_t)(w * (uint32_t)(L::kPBytes >> 4));
+          const uint64_t kd = ring_desc + (uint64_t)((k % L::kSlots) * (uint32_t)(L::kSlot >> 4));
 #pragma unroll
-          for (int i = 0; i < kTile / 32; ++i)
-            tc_mma_e4m3(tmem + 2 * NQ + w * NP, vd + (uint64_t)(i * (32 * DH >> 4)), pd + (uint64_t)(2 * i), idesc_o, (s >= 2) | (i > 0) ? 1u : 0u);
-          tc_commit(b_o + 8 * w);
-          tc_commit(ring.v_empty(k));
+          for (int i = 0; i < DH / 32; ++i) tc_mma_e4m3(tmem + (k % NB) * NQ, kd + (uint64_t)(2 * i), qd + (uint64_t)(2 * i), idesc, i ? 1u : 0u);
+          tc_commit(ring.k_empty(k));
         }
         __syncwarp();
-        if (more && !early) {
-          if (!(ok = keys(k + 2))) break;
-          tc_fence_after();
-          if (elect_one()) logits(k + 2);
-          __syncwarp();
-        }
       }
-      k0 += n;
       ++seg;
       if (left > 0 && ok) next_problem(a, p);
     }
-  } else if (left > 0) {
-    const int wg = warp >> 2, row = tid & 127;
-    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + lane_base + (uint32_t)wg * NQ, o_base = tmem + lane_base + 2 * NQ;
-    uint8_t* p_row = gen + kPAt + wg * L::kPBytes + (row & 15);
-    uint32_t k0 = 0, mine = 0, seg = 0;        // tiles so far, those of this warpgroup, segments
+  } else if (left > 0 && warp == kValues8) {
+    // ---- O += weights of tile k times its values
+    constexpr uint32_t idesc = idesc_e4m3_f32(DH, NP) | (1u << 15);            // V is read along its rows
+    const uint64_t p_desc = smem_desc_rows<128>(base + kPAt);
+    uint32_t k = 0, seg = 0;
     bool ok = true;
     while (left > 0 && ok) {
+      const int n = (int)min((long long)p.nt, p.t + left) - p.t;
+      left -= n;
+      ok = wait_warp(wt, b_free + 8 * (seg & 1u), ((seg >> 1) & 1u) ^ 1u);     // the results of the problem before last have been read
+      const uint32_t o = tmem + NB * NQ + (seg & 1u) * (2 * NP);
+      for (int s = 0; s < n && ok; ++s, ++k) {
+        if (!(ok = wait_warp(wt, ring.v_full(k), Ring::v_parity(k)) && wait_warp(wt, b_p + 8 * (k % NB), (k / NB) & 1u))) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t vd = ring_desc + (uint64_t)((L::kSlots + k % L::kSlots) * (uint32_t)(L::kSlot >> 4)), pd = p_desc + (uint64_t)((k & 1u) * (uint32_t)(L::kPBytes >> 4));
+#pragma unroll
+          for (int i = 0; i < kTile / 32; ++i)
+            tc_mma_e4m3(o + (k & 1u) * NP, vd + (uint64_t)(i * (32 * DH >> 4)), pd + (uint64_t)(2 * i), idesc, (s >= 2) | (i > 0) ? 1u : 0u);
+          tc_commit(ring.v_empty(k));
+          if (s + 1 == n) tc_commit(b_done + 8 * (seg & 1u));
+        }
+        __syncwarp();
+      }
+      ++seg;
+      if (left > 0 && ok) next_problem(a, p);
+    }
+  } else if (left > 0 && warp >= kHelper8 && warp < kProducer8) {
+    // ---- queries of the problem that comes next, results of the one that is done
+    const int ht = tid - kHelper8 * 32;
+    const uint32_t o_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + NB * NQ;
+    bool ok = true;
+    auto queries = [&](const Place& x, uint32_t par) {
+      const int tok0 = x.qp * a.block_tok, rows = min(a.block_tok, x.s.n - tok0) * a.n_rep;
+      const size_t qh0 = ((size_t)(a.l0 + x.l) * a.n_tok + x.s.f0 + tok0) * a.H_q + (size_t)x.g * a.n_rep;
+      constexpr int C = DH / 8;                // lanes of a row, eight elements each
+#pragma unroll
+      for (int i0 = 0; i0 < RB * C; i0 += 128) {
+        const int i = i0 + ht, r = i / C, c = i % C;
+        if (RB * C < 128 && i >= RB * C) break;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        const int tok = (int)(((uint32_t)r * a.rep_inv) >> 16);
+        if (r < rows) v = *reinterpret_cast<const uint4*>(a.q + (qh0 + (size_t)tok * a.H_q + (r - tok * a.n_rep)) * DH + c * 8);
+        uint2 hi, lo;
+        int ex;
+        encode_query<C>(v, &hi, &lo, &ex);
+        uint8_t* at = gen + kQAt + par * L::kQBytes + tile_place<DH>(r, c);
+        *reinterpret_cast<uint2*>(at) = hi;
+        *reinterpret_cast<uint2*>(at + RB * DH) = lo;
+        if (c == 0) {
+          const float qs = __int_as_float((127 + ex) << 23) * a.scale2;
+          info_s[par][0][r] = info_s[par][1][r] = make_float2(qs, r < rows ? -INFINITY : INFINITY);            // (nobody's column: no bound)
+          sub_s[par][0][r] = sub_s[par][1][r] = 0.0f;
+        }
+      }
+      if (ht == 0) bad_s[par] = 0u;
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b_q + 8 * par);
+    };
+    queries(p, 0);
+    uint32_t k0 = 0;
+    for (uint32_t seg = 0; left > 0; ++seg) {
+      const uint32_t par = seg & 1u;
+      const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left), n = t1 - t0;
+      left -= n;
+      Place x = p;
+      if (left > 0) {
+        next_problem(a, p);
+        queries(p, par ^ 1u);
+      }
+      ok = wait_warp(wt, b_done + 8 * par, (seg >> 1) & 1u);
+      tc_fence_after();
+      if (named_bar_any(3, 128, !ok)) break;
+      const int tok0 = x.qp * a.block_tok, rows = min(a.block_tok, x.s.n - tok0) * a.n_rep, new0 = x.s.base + tok0;
+      const size_t qh0 = ((size_t)(a.l0 + x.l) * a.n_tok + x.s.f0 + tok0) * a.H_q + (size_t)x.g * a.n_rep;
+      const bool whole = t0 == 0 && t1 == x.nt;
+      const bool has0 = n > (int)(k0 & 1u), has1 = n > (int)((k0 ^ 1u) & 1u);    // does a warpgroup have tiles of this segment?
+      const int d = DH == 128 ? ht : (warp & 3) * 16 + lane;
+      const bool owns = DH == 128 || lane < 16;
+      const size_t pr = ((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * a.block_rows;
+#pragma unroll 1
+      for (int c0 = 0; c0 < rows; c0 += 4) {
+        float o[2][3][4];
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int g = 0; g < 3; ++g) tmem_ld<4>(o_base + par * (2 * NP) + (uint32_t)(w * NP + g * RB + c0), o[w][g]);
+        tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = c0 + i;
+          if (r >= rows) break;
+          // a warpgroup's maxima; what it has not seen counts nothing
+          const float m0 = info_s[par][0][r].y == -INFINITY ? -INFINITY : sub_s[par][0][r], m1 = info_s[par][1][r].y == -INFINITY ? -INFINITY : sub_s[par][1][r];
+          const float M = fmaxf(m0, m1);
+          const float f0 = m0 == M ? 1.0f : exp2f(m0 - M), f1 = m1 == M ? 1.0f : exp2f(m1 - M);
+          float y = 0.0f, sum = 0.0f;
+          if (has0) {
+            y = f0 * (o[0][0][i] + 0x1p-5f * (o[0][1][i] + 0x1p-5f * o[0][2][i]));
+            sum = f0 * (sum_s[par][0][0][r] + sum_s[par][0][1][r] + sum_s[par][0][2][r] + sum_s[par][0][3][r]);
+          }
+          if (has1) {
+            y += f1 * (o[1][0][i] + 0x1p-5f * (o[1][1][i] + 0x1p-5f * o[1][2][i]));
+            sum += f1 * (sum_s[par][1][0][r] + sum_s[par][1][1][r] + sum_s[par][1][2][r] + sum_s[par][1][3][r]);
+          }
+          uint32_t bad = bad_s[par];
+          while (owns && bad) {                // rows that were taken out, given back to the columns that see them
+            const int tok = __ffs(bad) - 1;
+            bad &= bad - 1u;
+            if (tok * a.n_rep > r) continue;
+            const int jj = new0 + tok, page = a.table[(size_t)x.b * a.max_pages + (jj >> a.page_shift)];
+            const size_t head = ((size_t)(a.l0 + x.l) * a.n_pages + page) * a.H_kv + x.g;
+            if ((a.V8[((head << a.page_shift) + (jj & ((1 << a.page_shift) - 1))) * DH + d] & 0x7f) == 0x7f) y = __int_as_float(0x7fffffff);
+          }
+          if (whole) {
+            const int tok = (int)(((uint32_t)r * a.rep_inv) >> 16);
+            const size_t qh = qh0 + (size_t)tok * a.H_q + (r - tok * a.n_rep);
+            if (owns) a.out[qh * DH + d] = __float2bfloat16_rn(sum == 0.0f ? 0.0f : y / sum);
+            if (ht == 0 && a.lse) a.lse[qh] = sum == 0.0f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
+          } else {
+            if (owns) a.part[(pr + r) * DH + d] = y;
+            if (ht == 0) a.part_ml[pr + r] = make_float2(M, sum);
+          }
+        }
+      }
+      k0 += n;
+      tc_fence_before();
+      named_bar_sync(3, 128);                  // the columns of the problem after next go where another warp may still be reading
+      if (lane == 0) mbar_arrive(b_free + 8 * par);
+    }
+  } else if (left > 0 && warp < kHelper8) {
+    const int wg = warp >> 2, row = tid & 127;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    uint8_t* p_row = gen + kPAt + wg * L::kPBytes + (row & 15);
+    uint32_t k0 = 0, seg = 0;                  // tiles and segments so far
+    bool ok = true, gone = false;              // this warp's waits; the warpgroup has given up
+    while (left > 0 && !gone) {
+      const uint32_t par = seg & 1u;
       const int t0 = p.t, t1 = (int)min((long long)p.nt, p.t + left), n = t1 - t0;
       left -= n;
       const int tok0 = p.qp * a.block_tok, rows = min(a.block_tok, p.s.n - tok0) * a.n_rep;    // query rows
       const int seen = rows_seen(a, p.s, p.qp), new0 = p.s.base + tok0;                        // row of the block's first token
-      const size_t qh0 = ((size_t)(a.l0 + p.l) * a.n_tok + p.s.f0 + tok0) * a.H_q + (size_t)p.g * a.n_rep;
-      auto row_of = [&](int r) {               // place of query row r in q, out, lse
-        const int tok = (int)(((uint32_t)r * a.rep_inv) >> 16);
-        return qh0 + (size_t)tok * a.H_q + (r - tok * a.n_rep);
-      };
-      // ---- queries: two codes an element; 16-byte units swizzled by the row
-      constexpr int C = DH / 8;                // lanes of a row, eight elements each
-#pragma unroll
-      for (int i0 = 0; i0 < NQ * C; i0 += 256) {
-        const int i = i0 + tid, r = i / C, c = i % C;
-        if (NQ * C < 256 && i >= NQ * C) break;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (r < rows) x = *reinterpret_cast<const uint4*>(a.q + row_of(r) * DH + c * 8);
-        uint2 hi, lo;
-        int ex;
-        encode_query<C>(x, &hi, &lo, &ex);
-        uint8_t* at = gen + kQAt + tile_place<DH>(r, c);
-        *reinterpret_cast<uint2*>(at) = hi;
-        *reinterpret_cast<uint2*>(at + L::kQBytes) = lo;
-        if (c == 0 && r < RB) {
-          const float qs = __int_as_float((127 + ex) << 23) * a.scale2;
-          info_s[0][r] = info_s[1][r] = make_float2(qs, r < rows ? -INFINITY : INFINITY);      // (nobody's column: no bound)
-          sub_s[0][r] = sub_s[1][r] = 0.0f;
-        }
-      }
-      if (tid < 2) bad_s[tid] = 0u;
-      fence_proxy_async();
-      named_bar_sync(3, 256);
-      if (lane == 0) mbar_arrive(b_q);
+      ok = ok && wait_warp(wt, b_q + 8 * par, (seg >> 1) & 1u);
+      const float2* info = info_s[par][wg];
+      const float* sub = sub_s[par][wg];
+      const uint32_t o_base = tmem + lane_base + NB * NQ + par * (2 * NP) + (uint32_t)wg * NP;
       float l[RB];
 #pragma unroll
       for (int r = 0; r < RB; ++r) l[r] = 0.0f;
@@ -249,10 +329,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
 
       for (int s = (int)((k0 ^ (uint32_t)wg) & 1u); s < n; s += 2) {
         const uint32_t k = k0 + s;
-        ok = ok && wait_warp(wt, b_s + 8 * wg, mine & 1u) && wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k));
-        tc_fence_after();
-        float z[RB];
-        load_columns<RB>(s_addr, z);
+        ok = ok && wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k));
         const float2 sc = scale_s[k % SR][row >> a.page_shift];
         const float ks = __int_as_float(__float_as_int(sc.x) & 0x7f800000);
         const int ve = (__float_as_int(sc.y) >> 23) & 255;
@@ -261,11 +338,20 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         const bool dead = j >= seen || !(ks > 0.0f) || ve == 0;
         const int from = dead ? RB : max(0, min(j - new0, 64) * a.n_rep);
         const float e = (float)(ve - 127), e_inv = __int_as_float((254 - ve) << 23);
+        ok = ok && wait_warp(wt, ring.k_empty(k), Ring::k_parity(k));
+        tc_fence_after();
+        float z[RB];
+        {
+          float lo[RB];
+          load_columns<RB>(tmem + lane_base + (k % NB) * NQ, z, lo);
+#pragma unroll
+          for (int r = 0; r < RB; ++r) z[r] += lo[r];
+        }
         bool grow = !ok;
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
           if (r % 4 == 0 && r >= rows) break;
-          const float2 col = info_s[wg][r];
+          const float2 col = info[r];
           z[r] = fmaf(z[r], ks * col.x, e);
           z[r] = r >= from ? z[r] : -INFINITY;
           grow |= z[r] > col.y;
@@ -273,9 +359,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         bool waited = false;
         if (named_bar_any(1 + wg, 128, grow)) {
           // ---- a weight would pass its bound (or a wait has run out): maxima move
-          if (ok && mine > 0) ok = wait_warp(wt, b_o + 8 * wg, (mine - 1) & 1u);
+          if (ok && k >= 2) ok = wait_warp(wt, ring.v_empty(k - 2), Ring::v_parity(k - 2));
           waited = true;
-          if (named_bar_any(1 + wg, 128, !ok)) { ok = false; break; }
+          if (named_bar_any(1 + wg, 128, !ok)) { gone = true; break; }
           tc_fence_after();
 #pragma unroll
           for (int r = 0; r < RB; ++r) {
@@ -288,11 +374,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           if (row < RB) {
             const float m = fmaxf(fmaxf(top_s[wg][0][row], top_s[wg][1][row]), fmaxf(top_s[wg][2][row], top_s[wg][3][row]));
             float f = 1.0f;
-            if (row < rows && m > info_s[wg][row].y) {
-              const float old = info_s[wg][row].y;
-              f = old == -INFINITY ? 0.0f : exp2f(sub_s[wg][row] - (m - kSet));
-              sub_s[wg][row] = m - kSet;
-              info_s[wg][row].y = m - kSet + kTop;
+            if (row < rows && m > info[row].y) {
+              f = info[row].y == -INFINITY ? 0.0f : exp2f(sub[row] - (m - kSet));
+              sub_s[par][wg][row] = m - kSet;
+              info_s[par][wg][row].y = m - kSet + kTop;
             }
             fac_s[wg][row] = f;
           }
@@ -308,7 +393,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
 #pragma unroll 1
               for (int c = 0; c < RB; c += 8) {
                 if (c >= rows) break;
-                const uint32_t at = o_base + (uint32_t)(wg * NP + g * RB + c);
+                const uint32_t at = o_base + (uint32_t)(g * RB + c);
                 float o[8];
                 tmem_ld<8>(at, o);
                 tc_wait_ld();
@@ -322,11 +407,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           }
         }
         // ---- weights, as three codes each; the product before has to have read the last ones
-        if (ok && !waited && mine > 0) ok = wait_warp(wt, b_o + 8 * wg, (mine - 1) & 1u);
+        if (ok && !waited && k >= 2) ok = wait_warp(wt, ring.v_empty(k - 2), Ring::v_parity(k - 2));
 #pragma unroll
         for (int r = 0; r < RB; r += 2) {
           if (r % 4 == 0 && r >= rows) break;
-          const float w0 = ex2_approx(z[r] - sub_s[wg][r]), w1 = ex2_approx(z[r + 1] - sub_s[wg][r + 1]);
+          const float w0 = ex2_approx(z[r] - sub[r]), w1 = ex2_approx(z[r + 1] - sub[r + 1]);
           l[r] = fmaf(w0, e_inv, l[r]);
           l[r + 1] = fmaf(w1, e_inv, l[r + 1]);
           const __half2 step = __float2half2_rn(32.0f);
@@ -353,79 +438,22 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
               hit |= m.x | m.y | m.z | m.w;
               v[c] = make_uint4(x.x & ~m.x, x.y & ~m.y, x.z & ~m.z, x.w & ~m.w);
             }
-            if (hit) atomicOr(&bad_s[(j - new0) >> 5], 1u << ((j - new0) & 31));
+            if (hit) atomicOr(&bad_s[par], 1u << (j - new0));
           }
         }
         fence_proxy_async();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0 && ok && !(a.inject & XKV_INJECT_CACHE_NO_HANDOVER)) mbar_arrive(b_p + 8 * wg);
-        ++mine;
+        if (lane == 0 && ok && !(a.inject & XKV_INJECT_CACHE_NO_HANDOVER)) mbar_arrive(b_p + 8 * (k % NB));
         any = true;
       }
-      // ---- the segment's result: both warpgroups meet (a warp whose wait has run out comes here, too)
-      if (ok && any) ok = wait_warp(wt, b_o + 8 * wg, (mine - 1) & 1u);
-      tc_fence_after();
-      sum_columns<RB>(l, sum_s[wg][warp & 3]);
-      if (named_bar_any(3, 256, !ok)) { ok = false; break; }
-      const bool whole = t0 == 0 && t1 == p.nt;
-      const bool has0 = n > (int)(k0 & 1u), has1 = n > (int)((k0 ^ 1u) & 1u);    // does a warpgroup have tiles of this segment?
-      const int d = DH == 128 ? row : (warp & 3) * 16 + lane;
-      const bool owns = DH == 128 || lane < 16;
-      const size_t pr = ((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * RB;
-      constexpr int HALF = RB / 2;
-#pragma unroll 1
-      for (int c0 = wg * HALF; c0 < (wg + 1) * HALF; c0 += 4) {
-        if (c0 >= rows) break;
-        float o[2][3][4];
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int g = 0; g < 3; ++g) tmem_ld<4>(o_base + (uint32_t)(w * NP + g * RB + c0), o[w][g]);
-        tc_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = c0 + i;
-          if (r >= rows) break;
-          // a warpgroup's maxima; what it has not seen counts nothing
-          const float m0 = info_s[0][r].y == -INFINITY ? -INFINITY : sub_s[0][r], m1 = info_s[1][r].y == -INFINITY ? -INFINITY : sub_s[1][r];
-          const float M = fmaxf(m0, m1);
-          const float f0 = !has0 ? 0.0f : m0 == M ? 1.0f : exp2f(m0 - M), f1 = !has1 ? 0.0f : m1 == M ? 1.0f : exp2f(m1 - M);
-          float x = 0.0f, sum = 0.0f;
-          if (has0) {
-            x = f0 * (o[0][0][i] + 0x1p-5f * (o[0][1][i] + 0x1p-5f * o[0][2][i]));
-            sum = f0 * (sum_s[0][0][r] + sum_s[0][1][r] + sum_s[0][2][r] + sum_s[0][3][r]);
-          }
-          if (has1) {
-            x += f1 * (o[1][0][i] + 0x1p-5f * (o[1][1][i] + 0x1p-5f * o[1][2][i]));
-            sum += f1 * (sum_s[1][0][r] + sum_s[1][1][r] + sum_s[1][2][r] + sum_s[1][3][r]);
-          }
-          uint32_t bad0 = bad_s[0], bad1 = bad_s[1];
-          while (owns && (bad0 | bad1)) {      // rows that were taken out, given back to the columns that see them
-            const int tok = bad0 ? __ffs(bad0) - 1 : 31 + __ffs(bad1);
-            if (bad0) bad0 &= bad0 - 1u; else bad1 &= bad1 - 1u;
-            if (tok * a.n_rep > r) continue;
-            const int jj = new0 + tok, page = a.table[(size_t)p.b * a.max_pages + (jj >> a.page_shift)];
-            const size_t head = ((size_t)(a.l0 + p.l) * a.n_pages + page) * a.H_kv + p.g;
-            if ((a.V8[((head << a.page_shift) + (jj & ((1 << a.page_shift) - 1))) * DH + d] & 0x7f) == 0x7f) x = __int_as_float(0x7fffffff);
-          }
-          if (whole) {
-            const size_t qh = row_of(r);
-            if (owns) a.out[qh * DH + d] = __float2bfloat16_rn(sum == 0.0f ? 0.0f : x / sum);
-            if (row == 0 && a.lse) a.lse[qh] = sum == 0.0f ? -INFINITY : (M + log2f(sum)) * 0.6931471805599453f;
-          } else {
-            if (owns) a.part[(pr + r) * DH + d] = x;
-            if (row == 0) a.part_ml[pr + r] = make_float2(M, sum);
-          }
-        }
-      }
-      tc_fence_before();
+      if (gone) break;
+      sum_columns<RB>(l, sum_s[par][wg][warp & 3]);
+      __syncwarp();
+      if (lane == 0 && ok) mbar_arrive(b_done + 8 * par);
       k0 += n;
       ++seg;
-      if (left > 0) {
-        next_problem(a, p);
-        named_bar_sync(3, 256);                // the next problem's columns go where the other warpgroup may still be reading
-      }
+      if (left > 0) next_problem(a, p);
     }
   }
 
@@ -433,13 +461,14 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
   tc_fence_before();
   __syncthreads();
   if (abort_s) {                               // given up: nothing may still write tensor memory when it is freed
-    if (warp == kIssuer8) {
-      if (elect_one()) tc_commit(b_drain);
-      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(b_drain, 0))) break;
+    if (warp == kLogits8 || warp == kValues8) {
+      const uint32_t bar = b_drain + 8 * (warp - kLogits8);
+      if (elect_one()) tc_commit(bar);
+      for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, mbar_try_wait(bar, 0))) break;
     }
     __syncthreads();
   }
-  if (warp == kIssuer8) {
+  if (warp == kLogits8) {
     tc_fence_after();
     tmem_dealloc(tmem, L::kTmem);
   }
@@ -524,7 +553,7 @@ cudaError_t launch_as(const CUtensorMap& k_map, const CUtensorMap& v_map, const 
 template <int DH>
 cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, const Attend8Args& a, int grid, int device, cudaStream_t s) {
   cudaError_t e = a.block_rows == 8 ? launch_as<DH, 8>(k_map, v_map, a, grid, device, s) : a.block_rows == 16 ? launch_as<DH, 16>(k_map, v_map, a, grid, device, s)
-                : a.block_rows == 32 ? launch_as<DH, 32>(k_map, v_map, a, grid, device, s) : a.block_rows == 64 ? launch_as<DH, 64>(k_map, v_map, a, grid, device, s)
+                : a.block_rows == 32 ? launch_as<DH, 32>(k_map, v_map, a, grid, device, s)
                 : launch_attend8_wide(k_map, v_map, DH, a, grid, device, s);
   if (e != cudaSuccess) return e;
   if (grid > 1) e = launch_pdl(attend8_merge_kernel<DH>, dim3(grid - 1, a.block_rows / kMergeWarps8), dim3(kMergeWarps8 * 32), 0, s, a);
@@ -535,7 +564,7 @@ cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, con
 // Query rows of a block: as few as hold the tokens of the longest sequence.
 int block_rows(int max_new, int n_rep) {
   const long long rows = (long long)max_new * n_rep;
-  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
 }
 
 }  // namespace
