@@ -31,8 +31,8 @@ namespace xkv {
 
 namespace {
 
-constexpr int kThreads8 = 512;                 // two warpgroups of softmax, one of queries and results; producer, two issuers
-constexpr int kHelper8 = 8, kProducer8 = 12, kLogits8 = 13, kValues8 = 14;
+constexpr int kThreads8 = 512;                 // two warpgroups of softmax, one of queries and results; two producers, two issuers
+constexpr int kHelper8 = 8, kProducer8 = 12, kLogits8 = 13, kValues8 = 14, kProducerV8 = 15;
 constexpr int kMergeWarps8 = 8;
 constexpr float kTop = 8.0f, kSet = 4.0f;      // log2: a weight's bound; where a column's largest weight is put
 
@@ -97,6 +97,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
   using Ring = Ring8<L::kSlots, L::kSlots, 2 * L::kSlots>;
   constexpr int NQ = L::kQ, NP = L::kP, SR = 2 * L::kSlots, NB = L::kAhead;
   static_assert(L::kSlots >= NB, "S of a tile is read before its keys' slot is multiplied again");
+  static_assert(SR >= L::kSlots + NB, "and its scales before theirs is filled again");
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bars_s[Ring::kBars + 12];
   __shared__ uint32_t tmem_s;
@@ -149,7 +150,9 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
   const uint64_t ring_desc = smem_desc_rows<DH>(base);
 
   if (left > 0 && warp == kProducer8) {
-    n_loaded = ring.template produce<DH>(a, wt, &k_map, &v_map, p, left);
+    n_loaded = ring.template produce<DH, true, false>(a, wt, &k_map, &v_map, p, left);
+  } else if (left > 0 && warp == kProducerV8) {
+    n_loaded = ring.template produce<DH, false, true>(a, wt, &k_map, &v_map, p, left);
   } else if (left > 0 && warp == kLogits8) {
     // ---- S of tile k, as soon as its keys are in and the weights of the tile that had its place are formed
     constexpr uint32_t idesc = idesc_e4m3_f32(128, NQ);
@@ -158,11 +161,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     while (left > 0 && ok) {
       const int n = (int)min((long long)p.nt, p.t + left) - p.t;
       left -= n;
-      ok = wait_warp(wt, b_q + 8 * (seg & 1u), (seg >> 1) & 1u);
+      ok = wait8(wt, b_q + 8 * (seg & 1u), (seg >> 1) & 1u);
       const uint64_t qd = smem_desc_rows<DH>(base + kQAt + (seg & 1u) * L::kQBytes);
       for (int s = 0; s < n && ok; ++s, ++k) {
-        if (!(ok = wait_warp(wt, ring.k_full(k), Ring::k_parity(k)))) break;
-        if (k >= NB && !(ok = wait_warp(wt, b_p + 8 * (k % NB), (k / NB - 1) & 1u))) break;
+        if (!(ok = wait8(wt, ring.k_full(k), Ring::k_parity(k)))) break;
+        if (k >= NB && !(ok = wait8(wt, b_p + 8 * (k % NB), (k / NB - 1) & 1u))) break;
         tc_fence_after();
         if (elect_one()) {
           const uint64_t kd = ring_desc + (uint64_t)((k % L::kSlots) * (uint32_t)(L::kSlot >> 4));
@@ -184,10 +187,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     while (left > 0 && ok) {
       const int n = (int)min((long long)p.nt, p.t + left) - p.t;
       left -= n;
-      ok = wait_warp(wt, b_free + 8 * (seg & 1u), ((seg >> 1) & 1u) ^ 1u);     // the results of the problem before last have been read
+      ok = wait8(wt, b_free + 8 * (seg & 1u), ((seg >> 1) & 1u) ^ 1u);     // the results of the problem before last have been read
       const uint32_t o = tmem + NB * NQ + (seg & 1u) * (2 * NP);
       for (int s = 0; s < n && ok; ++s, ++k) {
-        if (!(ok = wait_warp(wt, ring.v_full(k), Ring::v_parity(k)) && wait_warp(wt, b_p + 8 * (k % NB), (k / NB) & 1u))) break;
+        if (!(ok = wait8(wt, ring.v_full(k), Ring::v_parity(k)) && wait8(wt, b_p + 8 * (k % NB), (k / NB) & 1u))) break;
         tc_fence_after();
         if (elect_one()) {
           const uint64_t vd = ring_desc + (uint64_t)((L::kSlots + k % L::kSlots) * (uint32_t)(L::kSlot >> 4)), pd = p_desc + (uint64_t)((k & 1u) * (uint32_t)(L::kPBytes >> 4));
@@ -246,7 +249,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         next_problem(a, p);
         queries(p, par ^ 1u);
       }
-      ok = wait_warp(wt, b_done + 8 * par, (seg >> 1) & 1u);
+      ok = wait8(wt, b_done + 8 * par, (seg >> 1) & 1u);
       tc_fence_after();
       if (named_bar_any(3, 128, !ok)) break;
       const int tok0 = x.qp * a.block_tok, rows = min(a.block_tok, x.s.n - tok0) * a.n_rep, new0 = x.s.base + tok0;
@@ -318,7 +321,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
       left -= n;
       const int tok0 = p.qp * a.block_tok, rows = min(a.block_tok, p.s.n - tok0) * a.n_rep;    // query rows
       const int seen = rows_seen(a, p.s, p.qp), new0 = p.s.base + tok0;                        // row of the block's first token
-      ok = ok && wait_warp(wt, b_q + 8 * par, (seg >> 1) & 1u);
+      ok = ok && wait8(wt, b_q + 8 * par, (seg >> 1) & 1u);
       const float2* info = info_s[par][wg];
       const float* sub = sub_s[par][wg];
       const uint32_t o_base = tmem + lane_base + NB * NQ + par * (2 * NP) + (uint32_t)wg * NP;
@@ -329,7 +332,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
 
       for (int s = (int)((k0 ^ (uint32_t)wg) & 1u); s < n; s += 2) {
         const uint32_t k = k0 + s;
-        ok = ok && wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k));
+        ok = ok && wait8(wt, ring.scales_full(k), Ring::scales_parity(k));
         const float2 sc = scale_s[k % SR][row >> a.page_shift];
         const float ks = __int_as_float(__float_as_int(sc.x) & 0x7f800000);
         const int ve = (__float_as_int(sc.y) >> 23) & 255;
@@ -338,7 +341,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         const bool dead = j >= seen || !(ks > 0.0f) || ve == 0;
         const int from = dead ? RB : max(0, min(j - new0, 64) * a.n_rep);
         const float e = (float)(ve - 127), e_inv = __int_as_float((254 - ve) << 23);
-        ok = ok && wait_warp(wt, ring.k_empty(k), Ring::k_parity(k));
+        ok = ok && wait8(wt, ring.k_empty(k), Ring::k_parity(k));
         tc_fence_after();
         float z[RB];
         {
@@ -359,7 +362,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         bool waited = false;
         if (named_bar_any(1 + wg, 128, grow)) {
           // ---- a weight would pass its bound (or a wait has run out): maxima move
-          if (ok && k >= 2) ok = wait_warp(wt, ring.v_empty(k - 2), Ring::v_parity(k - 2));
+          if (ok && k >= 2) ok = wait8(wt, ring.v_empty(k - 2), Ring::v_parity(k - 2));
           waited = true;
           if (named_bar_any(1 + wg, 128, !ok)) { gone = true; break; }
           tc_fence_after();
@@ -407,7 +410,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           }
         }
         // ---- weights, as three codes each; the product before has to have read the last ones
-        if (ok && !waited && k >= 2) ok = wait_warp(wt, ring.v_empty(k - 2), Ring::v_parity(k - 2));
+        if (ok && !waited && k >= 2) ok = wait8(wt, ring.v_empty(k - 2), Ring::v_parity(k - 2));
 #pragma unroll
         for (int r = 0; r < RB; r += 2) {
           if (r % 4 == 0 && r >= rows) break;
@@ -427,7 +430,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         }
         if (__any_sync(0xffffffffu, dead || from > 0)) {
           // thread = value row: what no column sees is zeroed, NaN is taken out of what only some see, and listed
-          ok = ok && wait_warp(wt, ring.v_full(k), Ring::v_parity(k));
+          ok = ok && wait8(wt, ring.v_full(k), Ring::v_parity(k));
           if (ok && (dead || from > 0)) {
             uint4* v = reinterpret_cast<uint4*>(gen + (L::kSlots + k % L::kSlots) * L::kSlot + row * DH);      // (the order of its units does not matter)
             uint32_t hit = 0;
@@ -473,9 +476,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     tmem_dealloc(tmem, L::kTmem);
   }
   if (abort_s && warp == kProducer8) {
-    ring.drain(n_loaded);
+    ring.template drain<true, false>(n_loaded);
     results_are_nan<DH>(a, place_s, count_s);
   }
+  if (abort_s && warp == kProducerV8) ring.template drain<false, true>(n_loaded);
 }
 
 // Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A problem that lies in several pieces is joined where its second

@@ -9,6 +9,24 @@
 
 namespace xkv {
 
+// A whole warp waits (as wait_warp does), asleep for most of the time: warps that poll take their SM's issue slots from those that work.
+static __device__ bool wait8_slow(const Wait& w, uint32_t bar, uint32_t parity) {
+  unsigned long long t0, t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t0));
+  do {
+    if (ptx::mbar_try_wait_for(bar, parity, 10000u)) return true;
+    if (*w.abort) return false;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  } while (t - t0 < w.limit_ns);
+  *w.abort = 1;
+  if (w.flags) atomicOr(w.flags, XKV_FLAG_TIMEOUT);
+  return false;
+}
+__device__ __forceinline__ bool wait8(const Wait& w, uint32_t bar, uint32_t parity) {
+  const bool ok = ptx::mbar_test(bar, parity) || wait8_slow(w, bar, parity);
+  return __all_sync(0xffffffffu, ok);
+}
+
 struct Attend8Args {
   int batch, H_kv, H_q, n_rep, n_pages, max_pages, page_shift, n_tok, max_new, l0, layers;
   int block_tok;                               // tokens of a block of query rows
@@ -221,10 +239,10 @@ __device__ __forceinline__ void results_are_nan(const Attend8Args& a, Place x, l
   }
 }
 
-// The copies of a CTA's tiles, by its producer's warp: a page is one box of the copy engine; lane i has the i-th page of a tile, its
+// The copies of a CTA's tiles, by one producer's warp or one for keys and one for values: a page is one box of the copy engine; lane i has the i-th page of a tile, its
 // entry of the table and its scales (asynchronous copies of four bytes, which report to a barrier of their own: a tile's scales are read
 // until its values have met their weights, and its keys' slot may be filled again before).  Keys go through a ring of KS slots, values
-// through one of VS behind it, scales through one of SR > VS + 2 tiles.  Barriers: keys full, keys empty, values full, values empty,
+// through one of VS behind it, scales through one of SR tiles.  Barriers: keys full, keys empty, values full, values empty,
 // scales full.  Returns how many tiles were asked for.
 template <int KS, int VS, int SR>
 struct Ring8 {
@@ -245,7 +263,7 @@ struct Ring8 {
     for (int i = 0; i < VS; ++i) { ptx::mbar_init(v_full(i), 1); ptx::mbar_init(v_empty(i), v_done); }
     for (int i = 0; i < SR; ++i) ptx::mbar_init(scales_full(i), 32);           // (every lane reports)
   }
-  template <int DH>
+  template <int DH, bool KEYS, bool VALUES>
   __device__ __forceinline__ uint32_t produce(const Attend8Args& a, const Wait& wt, const CUtensorMap* k_map, const CUtensorMap* v_map, Place p, long long left) const {
     const int lane = threadIdx.x & 31;
     const int ppt_shift = 7 - a.page_shift, ppt = 1 << ppt_shift, tpb = 32 >> ppt_shift;       // pages of a tile, tiles of a batch of entries
@@ -262,7 +280,7 @@ struct Ring8 {
         if (i >= pages) return -1;
         const int e = entries[i];
         if (e >= 0 && e < a.n_pages) return e;
-        if (a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
+        if (KEYS && a.flags) atomicOr(a.flags, XKV_FLAG_INDEX_RANGE);
         return -1;
       };
       int now = 0, next = entry(t0);
@@ -273,32 +291,37 @@ struct Ring8 {
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, id >= 0)) * page_bytes;
         const size_t head = ((size_t)(a.l0 + p.l) * a.n_pages + (id >= 0 ? id : 0)) * a.H_kv + p.g;
         const int y = (int)(head << a.page_shift);
-        if (!(ok = wait_warp(wt, k_empty(k), k_parity(k) ^ 1u))) break;
-        if (lane == 0) ptx::mbar_expect_tx(k_full(k), bytes);
-        __syncwarp();
-        if (id >= 0) ptx::tma_load_2d(slots + (k % KS) * (kTile * DH) + lane * page_bytes, k_map, 0, y, k_full(k));
-        if (lane < ppt) {
-          const uint32_t at = ptx::smem_u32(&scales[k % SR][lane]), n = id >= 0 ? 4u : 0u;    // (a page that is not there gets zeros)
-          ptx::cp_async4(at, a.k_scale + head, n);
-          ptx::cp_async4(at + 4, a.v_scale + head, n);
+        if constexpr (KEYS) {
+          if (!(ok = wait8(wt, k_empty(k), k_parity(k) ^ 1u))) break;
+          if (lane == 0) ptx::mbar_expect_tx(k_full(k), bytes);
+          __syncwarp();
+          if (id >= 0) ptx::tma_load_2d(slots + (k % KS) * (kTile * DH) + lane * page_bytes, k_map, 0, y, k_full(k));
+          if (lane < ppt) {
+            const uint32_t at = ptx::smem_u32(&scales[k % SR][lane]), n = id >= 0 ? 4u : 0u;  // (a page that is not there gets zeros)
+            ptx::cp_async4(at, a.k_scale + head, n);
+            ptx::cp_async4(at + 4, a.v_scale + head, n);
+          }
+          ptx::cp_async_arrive_noinc(scales_full(k));
         }
-        ptx::cp_async_arrive_noinc(scales_full(k));
-        if (!(ok = wait_warp(wt, v_empty(k), v_parity(k) ^ 1u))) { ++k; break; }
-        if (lane == 0) ptx::mbar_expect_tx(v_full(k), bytes);
-        __syncwarp();
-        if (id >= 0) ptx::tma_load_2d(slots + (KS + k % VS) * (kTile * DH) + lane * page_bytes, v_map, 0, y, v_full(k));
+        if constexpr (VALUES) {
+          if (!(ok = wait8(wt, v_empty(k), v_parity(k) ^ 1u))) { k += KEYS ? 1u : 0u; break; }
+          if (lane == 0) ptx::mbar_expect_tx(v_full(k), bytes);
+          __syncwarp();
+          if (id >= 0) ptx::tma_load_2d(slots + (KS + k % VS) * (kTile * DH) + lane * page_bytes, v_map, 0, y, v_full(k));
+        }
       }
       if (left > 0) next_problem(a, p);
     }
     __syncwarp();
     return k;
   }
-  // By the producer's warp of a CTA that has given up: tiles may still be on their way into its shared memory; stay (with a limit) for them.
+  // By a producer's warp of a CTA that has given up: tiles may still be on their way into its shared memory; stay (with a limit) for them.
+  template <bool KEYS, bool VALUES>
   __device__ __forceinline__ void drain(uint32_t loaded) const {
     asm volatile("cp.async.wait_all;" ::: "memory");
-    for (uint32_t k = loaded > KS ? loaded - KS : 0u; k < loaded; ++k)
+    for (uint32_t k = loaded > KS ? loaded - KS : 0u; KEYS && k < loaded; ++k)
       for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, ptx::mbar_try_wait(k_full(k), k_parity(k)))) break;
-    for (uint32_t k = loaded > VS ? loaded - VS : 0u; k < loaded; ++k)
+    for (uint32_t k = loaded > VS ? loaded - VS : 0u; VALUES && k < loaded; ++k)
       for (uint32_t i = 0; i < (1u << 16); ++i) if (__all_sync(0xffffffffu, ptx::mbar_try_wait(v_full(k), v_parity(k)))) break;
   }
 };

@@ -159,7 +159,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       for (int s = 0; s < steps; ++s, ++st) {
         const int half = s % SPT;
         const uint32_t buf = st & 1u, k = k0 + (uint32_t)(s / SPT);
-        if (!(ok = wait_warp(wt, b_pg + 8 * (k % SR), (k / SR) & 1u) && wait_warp(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
+        if (!(ok = wait8(wt, b_pg + 8 * (k % SR), (k / SR) & 1u) && wait8(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
         tc_fence_after();
         const uint32_t s_addr = tmem + lane_base + (uint32_t)qt * 128u + buf * KW;
         const int j0 = (t0 + s / SPT) * kTile + half * KW;     // first row of the step
@@ -204,7 +204,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             if (__any_sync(0xffffffffu, grow)) {
               // O holds the steps before this one once the last product is done, which the next logits' commit tells, or its own
               const bool next = s + 1 < steps;
-              if (!(ok = wait_warp(wt, (next ? b_s + 8 * (buf ^ 1u) : b_o + 8 * (n_o & 1u)) + 16 * qt, ((next ? st + 1 : n_o) >> 1) & 1u))) break;
+              if (!(ok = wait8(wt, (next ? b_s + 8 * (buf ^ 1u) : b_o + 8 * (n_o & 1u)) + 16 * qt, ((next ? st + 1 : n_o) >> 1) & 1u))) break;
               tc_fence_after();
               const float g = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
               if (grow) m_used = m_new;
@@ -252,7 +252,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       if (!ok) break;
       // ---- the segment's result (the last two products commit to two barriers in turn: by now both may be done)
       n_o += (uint32_t)min(2, steps);
-      if (!(ok = wait_warp(wt, b_o + 16 * qt + 8 * ((n_o - 1u) & 1u), ((n_o - 1u) >> 1) & 1u))) break;
+      if (!(ok = wait8(wt, b_o + 16 * qt + 8 * ((n_o - 1u) & 1u), ((n_o - 1u) >> 1) & 1u))) break;
       k0 += (uint32_t)(t1 - t0);
       tc_fence_after();
       const bool whole = t0 == 0 && t1 == p.nt;
@@ -325,8 +325,8 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       const int seen = rows_seen(a, p.s, p.qp), new0 = p.s.base + p.qp * a.block_tok;
       if (ct < 8) bad_s[(seg + 8) & 15u][ct] = 0u;
       for (int t = t0; t < t1; ++t, ++k) {
-        if (!(ok = wait_warp(wt, ring.v_full(k), Ring::v_parity(k)) && wait_warp(wt, b_pg + 8 * (k % SR), (k / SR) & 1u) &&
-                   wait_warp(wt, b_ve + 8 * (k & 1u), ((k >> 1) & 1u) ^ 1u))) break;
+        if (!(ok = wait8(wt, ring.v_full(k), Ring::v_parity(k)) && wait8(wt, b_pg + 8 * (k % SR), (k / SR) & 1u) &&
+                   wait8(wt, b_ve + 8 * (k & 1u), ((k >> 1) & 1u) ^ 1u))) break;
         const uint8_t* src = gen + (L::kKeys + k % L::kCodes) * L::kSlot;
         uint8_t* dst = gen + kVAt + (k & 1u) * L::kValues;
         const bool some = (t + 1) * kTile > new0 + 1;          // rows that not all tokens of the block see
@@ -372,10 +372,10 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
   } else if (left > 0) {
     regs_fewer<kOtherRegs<QT>>();
     if (warp == kProducer) {
-      n_loaded = ring.template produce<DH>(a, wt, &k_map, &v_map, p, left);
+      n_loaded = ring.template produce<DH, true, true>(a, wt, &k_map, &v_map, p, left);
     } else if (warp == kScales) {
       for (uint32_t k = 0; k < (uint32_t)count_s; ++k) {
-        if (!wait_warp(wt, ring.scales_full(k), Ring::scales_parity(k))) break;
+        if (!wait8(wt, ring.scales_full(k), Ring::scales_parity(k))) break;
         const float2 sc = scale_s[k % SR][min(lane, 127 >> a.page_shift)];
         const int kb = __float_as_int(sc.x) & 0x7f800000, ve = (__float_as_int(sc.y) >> 23) & 255;
         const uint32_t dead = __ballot_sync(0xffffffffu, kb == 0 || ve == 0);
@@ -404,11 +404,11 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         tc_commit(b_s + 16 * qt + 8 * buf);
         if (half == SPT - 1) tc_commit(ring.k_empty(k));
       };
-      auto keys = [&](uint32_t k) { return wait_warp(wt, ring.k_full(k), Ring::k_parity(k)); };
+      auto keys = [&](uint32_t k) { return wait8(wt, ring.k_full(k), Ring::k_parity(k)); };
       while (left > 0 && ok) {
         const int n = (int)min((long long)p.nt, p.t + left) - p.t, steps = n * SPT;
         left -= n;
-        ok = wait_warp(wt, b_q + 8 * qt, seg & 1u);
+        ok = wait8(wt, b_q + 8 * qt, seg & 1u);
         for (int s = 0; s < min(2, steps) && ok; ++s) {        // two steps of logits ahead
           if (s % SPT == 0 && !(ok = keys(k0 + s / SPT))) break;
           tc_fence_after();
@@ -418,9 +418,9 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         for (int s = 0; s < steps && ok; ++s) {
           const uint32_t buf = (st + s) & 1u, k = k0 + s / SPT, kn = k0 + (s + 2) / SPT;
           const bool more = s + 2 < steps;
-          if (s % SPT == 0 && !(ok = wait_warp(wt, b_vf + 8 * (k & 1u), (k >> 1) & 1u))) break;
+          if (s % SPT == 0 && !(ok = wait8(wt, b_vf + 8 * (k & 1u), (k >> 1) & 1u))) break;
           if (more && s % SPT == 0 && !(ok = keys(kn))) break;
-          if (!(ok = wait_warp(wt, b_p + 16 * qt + 8 * buf, ((st + s) >> 1) & 1u))) break;
+          if (!(ok = wait8(wt, b_p + 16 * qt + 8 * buf, ((st + s) >> 1) & 1u))) break;
           tc_fence_after();
           if (elect_one()) {
             const uint64_t vd = v_desc + (uint64_t)((k & 1u) * (uint32_t)(L::kValues >> 4) + (uint32_t)(s % SPT) * (KW * 8));
@@ -458,7 +458,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
     tmem_dealloc(tmem, 512);
   }
   if (abort_s && warp == kProducer) {
-    ring.drain(n_loaded);
+    ring.template drain<true, true>(n_loaded);
     results_are_nan<DH>(a, place_s, count_s);
   }
 }
