@@ -106,6 +106,9 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
 
   if (left > 0 && warp < kConvert) {
     regs_more<kSoftmaxRegs<QT>>();
+    // A warpgroup alone polls (412 us for 32 tokens over 128k rows of four layers of eight heads, asleep 483); two sleep (a chunk of 512
+    // tokens over 12k rows 231 us, polling 237).
+    auto wait = [&](uint32_t bar, uint32_t parity) { return QT == 1 ? wait_warp(wt, bar, parity) : wait8(wt, bar, parity); };
     const int qt = warp >> 2, row = tid & 127;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     uint8_t* q_gen = gen + kQAt + qt * L::kQBytes;
@@ -159,7 +162,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       for (int s = 0; s < steps; ++s, ++st) {
         const int half = s % SPT;
         const uint32_t buf = st & 1u, k = k0 + (uint32_t)(s / SPT);
-        if (!(ok = wait8(wt, b_pg + 8 * (k % SR), (k / SR) & 1u) && wait8(wt, b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
+        if (!(ok = wait(b_pg + 8 * (k % SR), (k / SR) & 1u) && wait(b_s + 16 * qt + 8 * buf, (st >> 1) & 1u))) break;
         tc_fence_after();
         const uint32_t s_addr = tmem + lane_base + (uint32_t)qt * 128u + buf * KW;
         const int j0 = (t0 + s / SPT) * kTile + half * KW;     // first row of the step
@@ -204,7 +207,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             if (__any_sync(0xffffffffu, grow)) {
               // O holds the steps before this one once the last product is done, which the next logits' commit tells, or its own
               const bool next = s + 1 < steps;
-              if (!(ok = wait8(wt, (next ? b_s + 8 * (buf ^ 1u) : b_o + 8 * (n_o & 1u)) + 16 * qt, ((next ? st + 1 : n_o) >> 1) & 1u))) break;
+              if (!(ok = wait((next ? b_s + 8 * (buf ^ 1u) : b_o + 8 * (n_o & 1u)) + 16 * qt, ((next ? st + 1 : n_o) >> 1) & 1u))) break;
               tc_fence_after();
               const float g = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
               if (grow) m_used = m_new;
@@ -252,7 +255,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       if (!ok) break;
       // ---- the segment's result (the last two products commit to two barriers in turn: by now both may be done)
       n_o += (uint32_t)min(2, steps);
-      if (!(ok = wait8(wt, b_o + 16 * qt + 8 * ((n_o - 1u) & 1u), ((n_o - 1u) >> 1) & 1u))) break;
+      if (!(ok = wait(b_o + 16 * qt + 8 * ((n_o - 1u) & 1u), ((n_o - 1u) >> 1) & 1u))) break;
       k0 += (uint32_t)(t1 - t0);
       tc_fence_after();
       const bool whole = t0 == 0 && t1 == p.nt;
