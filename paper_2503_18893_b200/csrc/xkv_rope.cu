@@ -5,8 +5,9 @@
 // but for the fraction's own 2^-64 per position.  What is left of it beyond the nearest quarter turn goes through sincospi; a product
 // of a position and a frequency in 32 bits would be off by 0.01 at position 10^5.
 //
-// A CTA takes a few rows: it forms their cosines and sines once, in shared memory, for all heads of both tensors.  A thread then has
-// one place in the head and goes over heads and rows, four at a time in flight.  Bound by memory: each element is read and written once.
+// A CTA takes up to eight rows: it forms their cosines and sines once, in shared memory, for all heads of both tensors, while the first
+// elements are on their way.  A thread has one place in the head and goes over heads and rows, four at a time in flight.  Bound by memory:
+// each element is read and written once.
 #include <math.h>
 
 #include <cuda_fp16.h>
@@ -68,67 +69,88 @@ __device__ __forceinline__ float2 cos_sin(uint64_t phase) {
 
 template <typename T, int P, bool HALF>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
-  __shared__ float2 turn_s[kRopeMaxRows * (XKV_ROPE_MAX_ROT / 2)];
-  const int pairs = a.plan.rot >> 1, tid = threadIdx.x;
+  // Cosine and sine of a row's pairs, those of one unit in pieces of 16 bytes a whole row of units apart: lanes side by side meet all banks.
+  __shared__ __align__(16) float2 turn_s[kRopeMaxRows * (XKV_ROPE_MAX_ROT / 2)];
+  const int pairs = a.plan.rot >> 1, turning = pairs / P, tid = threadIdx.x;
   const long long row0 = (long long)blockIdx.x * a.rows_per_cta;
   const int rows = (int)min((long long)a.rows_per_cta, a.rows - row0);
-  ptx::grid_dependency_wait();
-  ptx::grid_dependency_launch();
-  for (int i = tid; i < rows * pairs; i += kRopeThreads) {
-    const int r = i / pairs, p = i - r * pairs;
-    const float2 t = cos_sin((uint64_t)(long long)a.pos[(row0 + r) % a.n_pos] * a.plan.turns[p]);
-    turn_s[i] = make_float2(t.x * a.gain, t.y * a.gain * a.sign);
-  }
-  __syncthreads();
   constexpr int U = 4;
   const int width = min(a.units, kRopeThreads), step = kRopeThreads / width;     // threads of a head, heads at a time
-  if (tid >= width * step) return;
-  const int h_first = tid / width + step * (int)blockIdx.y, h_step = step * (int)gridDim.y;
-  for (int u = tid % width; u < a.units; u += width) {
-    const int e0 = u * 2 * P;                  // the unit is 2 P elements of the head's pairs, or of what is copied behind them
-    const bool turns = e0 < a.plan.rot;
-    const int ea = HALF && turns ? u * P : e0, eb = HALF && turns ? u * P + pairs : e0 + P;
-    int r = 0, h = h_first;
-    while (h >= a.heads && r < rows) { h -= a.heads; ++r; }
-    while (r < rows) {
-      Piece<T, P> xa[U], xb[U];
-      T* y[U];
-      int row[U], n = 0;
+  const bool works = tid < width * step;
+  int u = tid % width, r = 0, h = tid / width;
+  auto settle = [&] { while (h >= a.heads && r < rows) { h -= a.heads; ++r; } };
+  settle();
+  Piece<T, P> xa[U], xb[U];
+  T* y[U];
+  int row[U], n = 0;
+  // a unit is 2 P elements of the head's pairs, or of what is copied behind them
+  auto place_a = [&] { return HALF && u < turning ? u * P : u * 2 * P; };
+  auto place_b = [&] { return HALF && u < turning ? u * P + pairs : u * 2 * P + P; };
+  auto load = [&] {                            // the next U rows or heads of this thread's place
+    n = 0;
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (r < rows) {
-          const RopeTensor& t = a.t[h < a.heads0 ? 0 : 1];
-          const int ht = h < a.heads0 ? h : h - a.heads0;
-          const T* x = (const T*)t.x + (row0 + r) * t.x_row + ht * t.x_head;
-          y[i] = (T*)t.y + (row0 + r) * t.y_row + ht * t.y_head;
-          xa[i].load(x + ea);
-          xb[i].load(x + eb);
-          row[i] = r;
-          n = i + 1;
-          h += h_step;
-          while (h >= a.heads) { h -= a.heads; ++r; }
-        }
+    for (int i = 0; i < U; ++i) {
+      if (works && r < rows) {
+        const RopeTensor& t = a.t[h < a.heads0 ? 0 : 1];
+        const long long ht = h < a.heads0 ? h : h - a.heads0;
+        const T* x = (const T*)t.x + (row0 + r) * t.x_row + ht * t.x_head;
+        y[i] = (T*)t.y + (row0 + r) * t.y_row + ht * t.y_head;
+        xa[i].load(x + place_a());
+        xb[i].load(x + place_b());
+        row[i] = r;
+        n = i + 1;
+        h += step;
+        settle();
       }
+    }
+  };
+  ptx::grid_dependency_wait();
+  ptx::grid_dependency_launch();
+  load();                                      // (under way while the turns are formed)
+  for (int i = tid; i < rows * pairs; i += kRopeThreads) {
+    const int ri = i / pairs, p = i - ri * pairs, k = p % P;
+    const long long at = row0 + ri;
+    const float2 t = cos_sin((uint64_t)(long long)a.pos[a.rows == a.n_pos ? at : at % a.n_pos] * a.plan.turns[p]);
+    turn_s[ri * pairs + (P == 1 ? p : ((k >> 1) * turning + p / P) * 2 + (k & 1))] = make_float2(t.x * a.gain, t.y * a.gain * a.sign);
+  }
+  __syncthreads();
+  if (!works) return;
+  while (true) {
+    while (n > 0) {
+      const int ea = place_a(), eb = place_b();
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         if (i >= n) break;
-        if (turns) {
-          const float2* t = turn_s + row[i] * pairs + u * P;
+        if (u < turning) {
+          const float2* t = turn_s + row[i] * pairs;
+          float2 cs[P];
+          if constexpr (P == 1) {
+            cs[0] = t[u];
+          } else {
+#pragma unroll
+            for (int k = 0; k < P; k += 2) *reinterpret_cast<float4*>(cs + k) = *reinterpret_cast<const float4*>(t + ((k >> 1) * turning + u) * 2);
+          }
 #pragma unroll
           for (int k = 0; k < P; ++k) {
-            const float2 cs = t[k];
             // pair k: the k-th element of both pieces, or two neighbours of the 2 P elements
             T& va = HALF ? xa[i].v[k] : (2 * k < P ? xa[i].v[2 * k % P] : xb[i].v[2 * k % P]);
             T& vb = HALF ? xb[i].v[k] : (2 * k + 1 < P ? xa[i].v[(2 * k + 1) % P] : xb[i].v[(2 * k + 1) % P]);
             const float fa = to_float(va), fb = to_float(vb);
-            from_float(fa * cs.x - fb * cs.y, &va);
-            from_float(fb * cs.x + fa * cs.y, &vb);
+            from_float(fa * cs[k].x - fb * cs[k].y, &va);
+            from_float(fb * cs[k].x + fa * cs[k].y, &vb);
           }
         }
         xa[i].store(y[i] + ea);
         xb[i].store(y[i] + eb);
       }
+      load();
     }
+    u += width;                                // (heads of more units than threads)
+    if (u >= a.units) break;
+    r = 0;
+    h = tid / width;
+    settle();
+    load();
   }
 }
 
@@ -150,8 +172,10 @@ cudaError_t launch_type(RopeArgs a, bool in_place, cudaStream_t s) {
   }
   const int p = wide ? P : 1;
   a.units = (in_place ? a.plan.rot : a.plan.d_h) / (2 * p);    // (in place there is nothing to copy)
+  // Few rows: a CTA each.  Many: as many as make a thread's loads worth its way, as long as there are six CTAs an SM.
   a.rows_per_cta = 1;
-  const dim3 grid((unsigned)((a.rows + a.rows_per_cta - 1) / a.rows_per_cta), 1);
+  while (a.rows_per_cta < kRopeMaxRows && a.rows / (2 * a.rows_per_cta) >= kPlanSms * 6) a.rows_per_cta *= 2;
+  const dim3 grid((unsigned)((a.rows + a.rows_per_cta - 1) / a.rows_per_cta));
   return wide ? launch_as<T, P>(a, grid, s) : launch_as<T, 1>(a, grid, s);
 }
 
