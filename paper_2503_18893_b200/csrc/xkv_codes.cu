@@ -63,7 +63,7 @@ __device__ __forceinline__ uint32_t magnitudes(uint32_t x) {
 
 // W: 32-bit words of a row that a lane holds (two values each): 2 for d_h = 128, 1 for 64.
 template <int W>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const CodesArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const CodesArgs a) {
   constexpr int DH = W * 64;
   __shared__ uint32_t top_s[kAppendThreads / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -217,7 +217,7 @@ cudaError_t launch_cache8_append(const xkv_cache8_config* c, int l0, int l1, con
   a.x[0] = k; a.x[1] = v; a.slot = slot; a.n_tok = n_tok;
   // A group looks after one token as long as that gives two waves of CTAs at most (decode: every token is a run of its own, and runs
   // of a group come one after the other), then after as many as a page has rows, 32 at least: most of a prompt's tokens begin no run.
-  // (4099 tokens of four heads in four layers, pages of 128: 25 us with 32 tokens a group, 17 with 128.)
+  // (4099 tokens of four heads in four layers, pages of 128: 25 us with 32 tokens a group, 22 with 128, 18 with four CTAs an SM besides.)
   const int groups = kAppendThreads / 32 / (c->page / kRunRows);
   const long long per_token = (long long)c->H_kv * 2 * a.layers;
   auto ctas = [&](int per_group) { return (n_tok + groups * per_group - 1) / (groups * per_group); };

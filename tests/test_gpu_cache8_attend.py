@@ -255,7 +255,7 @@ def test_logits_that_climb_from_tile_to_tile(xkv):
 def reference(c, layer=0):
     """All tokens of a large case at once, on the device in 64 bits; bounds as in the small ones."""
     K, V = (t[layer].view(torch.float8_e4m3fn).double() for t in (c.K, c.V))
-    at = 0
+    at = c.first[0]
     for b, (rows, n) in enumerate(zip(c.lens, c.news)):
         pages = torch.tensor(c.table[b][:-(-rows // c.page)], device="cuda")
         for g in range(K.shape[1]):
