@@ -1,13 +1,14 @@
 // Attention over a paged cache of 8-bit codes (xkv_cache8_attend): out_i = softmax(scale q_i K^T) V over the rows of token i's sequence
 // up to its own, K and V being e4m3 codes times their pages' scales, powers of two.
 //
-// The codes go from memory into the tensor core as they are, and the products are turned around, so that the 128 rows of a tile of the
-// cache are the wide side and a block of query rows (tokens times the query heads of a KV head, 8 to 64) the narrow one:
-//   S^T = K8 Q8^T       M = 128 rows of the cache, N = query rows
-//   O^T += V8^T P8^T    M = d_h, N = query rows, K = 128 rows of the cache
+// For few query rows, 8 or 16 of a KV head (decode steps, a draft or two): the codes go from memory into the tensor core as they are, and
+// the products are turned around, so that the 128 rows of a tile of the cache are the wide side and the block of query rows (tokens times
+// the query heads of a KV head) the narrow one:
+//   S^T = K8 Q8^T       M = 128 rows of the cache, N = 2 x query rows
+//   O^T += V8^T P8^T    M = d_h, N = 3 x query rows, K = 128 rows of the cache
 // Both operands of such a product have to be e4m3, which holds 4 significant bits; a query and a weight are split into several:
 //   q 2^-x = q_hi + q_lo   (x: its row's largest element lies in [128, 256)): a bf16 value's 8 bits are two codes, exactly for elements
-//                          above 2^-10 of the largest, to 2^-18 of it below.  Two products into the same S.
+//                          above 2^-10 of the largest, to 2^-18 of it below.  Two columns of S, added.
 //   w = w_0 + 2^-5 w_1 + 2^-10 w_2   of a weight in 16 bits (fp16): each code is the rounding of 2^5 times what the one before left.
 //                          Three groups of columns of O, joined at the end.  Weights lie below 2^8 and the largest of a column above
 //                          2^4, so a weight is exact to 2^-12 of itself or 2^-24 of the largest: a long even rest beside a row that
@@ -15,13 +16,19 @@
 // A key's scale multiplies the row's logits.  A value's scale 2^e joins the exponent: w_j = 2^(z_j + e_j - m), so that codes meet weights
 // that hold their scale, and m is the maximum of z_j + e_j; the denominator sums w_j 2^-e_j in fp32.
 //
-//   producer  pages by the copy engine, with their scales (Ring8)
-//   issuer    S of a tile two ahead, O of this one
+//   producers pages by the copy engine, with their scales (Ring8): a warp for keys, one for values (pages of 16 rows are 16 boxes a tile)
+//   issuers   a warp for S, up to four tiles ahead, and one for O; the commits that free a tile's slots are what tells of S and O, too
 //   softmax   two warpgroups, tile by tile in turns, each with its own maxima, sums and O; thread = row of the cache, so that a token's
 //             view (rows up to its own) is a comparison of the column with one number per thread.  Maxima move only when a weight would
 //             pass 2^8: one vote per tile.
+//   helpers   a warpgroup: queries of the next problem while this one is worked on, results of the last (S, queries and O are there twice)
 // All tiles of all problems form one list that is cut into as many even pieces as there are CTAs; a piece that holds a whole problem
 // writes its output, the others leave (O, m, l) for the merge.  Lengths are read on the device only.
+//
+// Bound by HBM.  131072 rows of four layers of eight heads, four query heads each: 171-174 us for pages of 16 to 128 rows (6.2 TB/s, 0.96 of
+// the copy's rate); eight sequences of up to 8191 rows 76; 32 of 2047 rows 99 (floor 84); 300 rows 10, latencies of two kernels.  What a
+// step brought (128k rows; eight sequences; pages of 16): warps that wait asleep instead of polling 187 -> 174, 99 -> 77, 105 -> 76; one
+// issuing warp, two products for the two codes of a query 199, 102; the merge finding places for itself 105.
 #include <cuda.h>
 #include <math.h>
 
@@ -39,18 +46,9 @@ constexpr float kTop = 8.0f, kSet = 4.0f;      // log2: a weight's bound; where 
 // N columns, and the N behind them.
 template <int N>
 __device__ __forceinline__ void load_columns(uint32_t addr, float (&u)[N], float (&v)[N]) {
-  if constexpr (N <= 16) {
-    ptx::tmem_ld<N>(addr, u);
-    ptx::tmem_ld<N>(addr + N, v);
-    ptx::tc_wait_ld();
-  } else {
-    auto& x = *reinterpret_cast<uint32_t(*)[32]>(u);
-    auto& y = *reinterpret_cast<uint32_t(*)[32]>(v);
-    ptx::tmem_ld32_nb(addr, x);
-    ptx::tmem_ld32_nb(addr + 32, y);
-    ptx::tc_wait_ld32_nb(x);
-    ptx::tc_wait_ld32_nb(y);
-  }
+  ptx::tmem_ld<N>(addr, u);
+  ptx::tmem_ld<N>(addr + N, v);
+  ptx::tc_wait_ld();
 }
 
 template <int DH, int RB>
@@ -59,7 +57,7 @@ struct Shape8 {
   static constexpr int kP = (3 * RB + 15) / 16 * 16;           // columns of O: three codes of a weight
   static constexpr int kSlot = kTile * DH;
   static constexpr int kSlots = DH == 64 ? 8 : 5;              // tiles of keys, and as many of values
-  static constexpr int kAhead = RB == 32 ? 2 : 4;              // tiles of S in tensor memory
+  static constexpr int kAhead = 4;                             // tiles of S in tensor memory
   static constexpr int kQBytes = kQ * DH, kPBytes = kP * kTile;
   static constexpr int kBytes = 1024 + 2 * kSlots * kSlot + 2 * kPBytes + 2 * kQBytes;
   static constexpr int kTmem = RB == 8 ? 256 : 512;            // S of tiles ahead, O of two warpgroups for two problems; rounded up
@@ -557,7 +555,6 @@ cudaError_t launch_as(const CUtensorMap& k_map, const CUtensorMap& v_map, const 
 template <int DH>
 cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, const Attend8Args& a, int grid, int device, cudaStream_t s) {
   cudaError_t e = a.block_rows == 8 ? launch_as<DH, 8>(k_map, v_map, a, grid, device, s) : a.block_rows == 16 ? launch_as<DH, 16>(k_map, v_map, a, grid, device, s)
-                : a.block_rows == 32 ? launch_as<DH, 32>(k_map, v_map, a, grid, device, s)
                 : launch_attend8_wide(k_map, v_map, DH, a, grid, device, s);
   if (e != cudaSuccess) return e;
   if (grid > 1) e = launch_pdl(attend8_merge_kernel<DH>, dim3(grid - 1, a.block_rows / kMergeWarps8), dim3(kMergeWarps8 * 32), 0, s, a);
@@ -565,10 +562,12 @@ cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, con
   return e;
 }
 
-// Query rows of a block: as few as hold the tokens of the longest sequence.
+// Query rows of a block: as few as hold the tokens of the longest sequence.  From 17 on they are the wide side of the products (32 rows a
+// head over 131072 rows of four layers of eight heads: 321 us, as the narrow side 357; over 8191 rows of one layer 29 and 38; 21 rows over
+// 3000 of three sequences 32.5 and 34.5).
 int block_rows(int max_new, int n_rep) {
   const long long rows = (long long)max_new * n_rep;
-  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : 128;
 }
 
 }  // namespace

@@ -358,7 +358,7 @@ __device__ __forceinline__ uint32_t tile_place(int r, int c) {
   return (uint32_t)(r * DH + unit * 16 + (c & 1) * 8);
 }
 
-// xkv_attend8_wide.cu: blocks of 128 or 256 query rows
+// xkv_attend8_wide.cu: blocks of 128 query rows
 cudaError_t launch_attend8_wide(const CUtensorMap& k_map, const CUtensorMap& v_map, int d_h, const Attend8Args& a, int grid, int device,
                                 cudaStream_t s);
 
