@@ -482,9 +482,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
 
 // Joins the pieces of a problem: O = sum_c 2^(m_c - M) O_c, l likewise.  A problem that lies in several pieces is joined where its second
 // piece begins (so there are at most as many as CTAs); a warp has one of its query rows, lane = d_h / 32 columns.
-template <int DH>
+// AT_ONCE pieces of a row are in flight: sixteen where there are few rows, four where there are many (four CTAs an SM instead of two).
+template <int DH, int AT_ONCE>
 __global__ void __launch_bounds__(kMergeWarps8 * 32) attend8_merge_kernel(const Attend8Args a) {
-  constexpr int V = DH / 32, AT_ONCE = 16;
+  constexpr int V = DH / 32;
   const int lane = threadIdx.x & 31, r = blockIdx.y * kMergeWarps8 + (threadIdx.x >> 5), c_second = blockIdx.x + 1;
   ptx::grid_dependency_wait();                 // every CTA waits, so that who waits for this kernel has waited for the one before
   ptx::grid_dependency_launch();
@@ -557,7 +558,10 @@ cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, con
   cudaError_t e = a.block_rows == 8 ? launch_as<DH, 8>(k_map, v_map, a, grid, device, s) : a.block_rows == 16 ? launch_as<DH, 16>(k_map, v_map, a, grid, device, s)
                 : launch_attend8_wide(k_map, v_map, DH, a, grid, device, s);
   if (e != cudaSuccess) return e;
-  if (grid > 1) e = launch_pdl(attend8_merge_kernel<DH>, dim3(grid - 1, a.block_rows / kMergeWarps8), dim3(kMergeWarps8 * 32), 0, s, a);
+  if (grid > 1) {
+    const dim3 ctas(grid - 1, a.block_rows / kMergeWarps8), threads(kMergeWarps8 * 32);
+    e = a.block_rows <= 16 ? launch_pdl(attend8_merge_kernel<DH, 16>, ctas, threads, 0, s, a) : launch_pdl(attend8_merge_kernel<DH, 4>, ctas, threads, 0, s, a);
+  }
   count_launch(kFamAttend8, 2);
   return e;
 }

@@ -7,7 +7,8 @@
 //
 // Append: the rows that a call brings to a page are one run of tokens.  For every run, head and tensor (keys, values) page / 16 warps
 // keep 16 rows each in registers: one read of the new rows, the maximum over the warps, one write of codes.  Read: 16 codes a thread.
-// Both are bound by memory.
+// Both are meant to be bound by memory.  4099 tokens of four heads in four layers: append 15.5 us (3.2 TB/s; instructions: 65 % of issue slots
+// busy), their read back 10.4; 32768 rows of eight heads in four layers read back in 131-138 us (5.8-6.1 TB/s); 32 sequences' tokens 4.5.
 #include <cuda_fp16.h>
 
 #include "xkv_internal.cuh"

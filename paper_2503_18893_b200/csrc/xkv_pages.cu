@@ -4,6 +4,8 @@
 // what shrinking sequences give back is another, and the places of new tokens a third.  One CTA goes over the sequences in blocks of
 // its threads, carrying the three sums; within a block, pages and tokens are then dealt out by whole warps and by binary search.
 // Pages given back go to places of the ring that held no free page before the call, so nothing that is read is written.
+// Bound by latency: 48 sequences with eight drafts each 4.3 us a call, 300 with up to 128 new tokens and back 5.8 (a cluster of eight from
+// 2048 tokens on).  Dealt out sequence after sequence by whole warps they took 18 and 26: a page's way is a load and a store that waits for it.
 #include "xkv_internal.cuh"
 #include "xkv_ptx.cuh"
 
@@ -136,8 +138,8 @@ __global__ void __launch_bounds__(kSeqs) page_assign_kernel(const PageArgs a) {
     }
     if (a.slot) {
       const int n = (int)max(0ll, min(all.fresh, (long long)a.n_tok - fresh0));
-      for (int t = rank * kSeqs + tid; t < n; t += ranks * kSeqs) {
-        const int x = sequence_of(fresh_s, t), h = held_s[x], held_x = h >= 0 ? h : -1 - h, pos = held_x + t - fresh_s[x];
+      for (uint32_t t = rank * kSeqs + tid; t < (uint32_t)n; t += ranks * kSeqs) {
+        const int x = sequence_of(fresh_s, (int)t), h = held_s[x], held_x = h >= 0 ? h : -1 - h, pos = held_x + (int)t - fresh_s[x];
         int slot = -1;
         if (h >= 0) {
           // a page that was taken just now is still in the ring, in whatever order the table is written
