@@ -12,12 +12,12 @@
 //   issuer     S of a tile two ahead, O += P V with P in tensor memory, where it lies over S
 //   softmax    two warpgroups; a query row is a TMEM lane, which two threads share, each with half of a tile's columns.  O is rescaled only
 //              when a maximum has grown by more than 2^8 (fp16 holds weights of 2^8, and of 2^-24): one vote of the two warps per tile.
-// Bound by the softmax: what one warp does in a row (logits from tensor memory, maximum, exponentials, weights back) is longer than its
-// instructions, and two warps of an SM's quarter do not fill it; warps that poll beside them make it worse.  131072 rows of four layers of
-// eight heads: 8 tokens of four query heads a KV head 323 us, 16 333, 32 356; a chunk of 512 tokens over 12301 rows of two sequences, seven
-// query heads, 220 (0.65 PFLOP/s).  Steps on the way, by their times then (with a merge that took 12 us more):  With one thread a row and 256 rows of Q (steps of half a tile) the chunk took 231 and 32 tokens 412; with
-// softmax warps that poll instead of sleeping 275 and 431; with two threads a row and 256 rows 323 (registers); steps of a tile with one S for
-// 256 rows 251.
+// Bound by the softmax: what a warp does for a row of a tile (logits from tensor memory, maximum, exponentials, weights back) is longer than
+// its instructions, and two warps of an SM's quarter do not fill it; warps that poll beside them make it worse.  131072 rows of four layers of
+// eight heads with four query heads: 8 tokens 323 us, 16 333, 32 356; a chunk of 512 tokens over 12301 rows of two sequences, seven query
+// heads, 220 (0.65 PFLOP/s).  What did not help, with a merge that took 12 us more: one thread a row and blocks of 256 rows (steps of half a
+// tile) 231 for the chunk and 412 for 32 tokens; softmax warps that poll 275 and 431; two threads a row and 256 rows 323 (registers); 256
+// rows with whole tiles, S once, 251.
 #include <math.h>
 
 #include "xkv_attend8.cuh"
