@@ -107,6 +107,13 @@ def test_prompts_from_their_start_and_tokens_that_see_nothing(xkv, lens, news):
     c.check(out, lse)
 
 
+def test_no_tokens_at_all(xkv):
+    c = Case(xkv, [100, 40], [0, 0], H_kv=1, n_rep=4, seed=1, gap=2)
+    for c.max_new in (1, 4):
+        out, lse = c.run()
+        assert bool((out == 7.0).all()) and bool((lse == 7.0).all()) and int(c.flags) == 0
+
+
 def test_many_sequences(xkv):
     lens = [(37 * b) % 150 for b in range(150)]
     c = Case(xkv, lens, [1 + (b % 5 == 0) for b in range(150)], H_kv=1, n_rep=2, d=64, page=16, seed=5)
