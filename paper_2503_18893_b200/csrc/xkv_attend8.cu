@@ -5,14 +5,15 @@
 // the products are turned around, so that the 128 rows of a tile of the cache are the wide side and the block of query rows (tokens times
 // the query heads of a KV head) the narrow one:
 //   S^T = K8 Q8^T       M = 128 rows of the cache, N = 2 x query rows
-//   O^T += V8^T P8^T    M = d_h, N = 3 x query rows, K = 128 rows of the cache
-// Both operands of such a product have to be e4m3, which holds 4 significant bits; a query and a weight are split into several:
+//   O^T += V8^T P8^T    M = d_h, N = 4 x query rows, K = 128 rows of the cache
+// Both operands of such a product have to be 8-bit codes; a query and a weight are split into several:
 //   q 2^-x = q_hi + q_lo   (x: its row's largest element lies in [128, 256)): a bf16 value's 8 bits are two codes, exactly for elements
 //                          above 2^-10 of the largest, to 2^-18 of it below.  Two columns of S, added.
-//   w = w_0 + 2^-5 w_1 + 2^-10 w_2   of a weight in 16 bits (fp16): each code is the rounding of 2^5 times what the one before left.
-//                          Three groups of columns of O, joined at the end.  Weights lie below 2^8 and the largest of a column above
-//                          2^4, so a weight is exact to 2^-12 of itself or 2^-24 of the largest: a long even rest beside a row that
-//                          draws most of the weight keeps its own.
+//   w = w_0 + 2^-3 w_1 + 2^-6 w_2 + 2^-9 w_3   of a weight in 16 bits (fp16), exactly, in e5m2: that is an fp16 number's upper byte, so a code
+//                          is cut off, not converted, and the next is that of 2^3 times what it left (3 bits of 11 each; 2^-9 times the
+//                          smallest code is 2^-25).  Four groups of columns of O, joined at the end.  What 16 bits mean to a weight
+//                          stands at kTop.  (Three e4m3 codes, 2^-10 of the first's steps, lost an even rest below 2^-24 of the
+//                          largest weight and were off by 6 % at 2^-20.)
 // A key's scale multiplies the row's logits.  A value's scale 2^e joins the exponent: w_j = 2^(z_j + e_j - m), so that codes meet weights
 // that hold their scale, and m is the maximum of z_j + e_j; the denominator sums w_j 2^-e_j in fp32.
 //
@@ -20,7 +21,7 @@
 //   issuers   a warp for S, up to four tiles ahead, and one for O; the commits that free a tile's slots are what tells of S and O, too
 //   softmax   two warpgroups, tile by tile in turns, each with its own maxima, sums and O; thread = row of the cache, so that a token's
 //             view (rows up to its own) is a comparison of the column with one number per thread.  Maxima move only when a weight would
-//             pass 2^8: one vote per tile.
+//             pass its bound: one vote per tile.
 //   helpers   a warpgroup: queries of the next problem while this one is worked on, results of the last (S, queries and O are there twice)
 // All tiles of all problems form one list that is cut into as many even pieces as there are CTAs; a piece that holds a whole problem
 // writes its output, the others leave (O, m, l) for the merge.  Lengths are read on the device only.
@@ -41,7 +42,7 @@ namespace {
 constexpr int kThreads8 = 512;                 // two warpgroups of softmax, one of queries and results; two producers, two issuers
 constexpr int kHelper8 = 8, kProducer8 = 12, kLogits8 = 13, kValues8 = 14, kProducerV8 = 15;
 constexpr int kMergeWarps8 = 8;
-constexpr float kTop = 8.0f, kSet = 4.0f;      // log2: a weight's bound; where a column's largest weight is put
+constexpr int kCodes8 = 4;                     // of a weight
 
 // N columns, and the N behind them.
 template <int N>
@@ -54,7 +55,7 @@ __device__ __forceinline__ void load_columns(uint32_t addr, float (&u)[N], float
 template <int DH, int RB>
 struct Shape8 {
   static constexpr int kQ = 2 * RB;                            // columns of S: two codes of a query
-  static constexpr int kP = (3 * RB + 15) / 16 * 16;           // columns of O: three codes of a weight
+  static constexpr int kP = kCodes8 * RB;                      // columns of O: the codes of a weight
   static constexpr int kSlot = kTile * DH;
   static constexpr int kSlots = DH == 64 ? 8 : 5;              // tiles of keys, and as many of values
   static constexpr int kAhead = 4;                             // tiles of S in tensor memory
@@ -168,7 +169,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         if (elect_one()) {
           const uint64_t kd = ring_desc + (uint64_t)((k % L::kSlots) * (uint32_t)(L::kSlot >> 4));
 #pragma unroll
-          for (int i = 0; i < DH / 32; ++i) tc_mma_e4m3(tmem + (k % NB) * NQ, kd + (uint64_t)(2 * i), qd + (uint64_t)(2 * i), idesc, i ? 1u : 0u);
+          for (int i = 0; i < DH / 32; ++i) tc_mma_8bit(tmem + (k % NB) * NQ, kd + (uint64_t)(2 * i), qd + (uint64_t)(2 * i), idesc, i ? 1u : 0u);
           tc_commit(ring.k_empty(k));
         }
         __syncwarp();
@@ -178,7 +179,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     }
   } else if (left > 0 && warp == kValues8) {
     // ---- O += weights of tile k times its values
-    constexpr uint32_t idesc = idesc_e4m3_f32(DH, NP) | (1u << 15);            // V is read along its rows
+    constexpr uint32_t idesc = idesc_e4m3_f32(DH, NP) | (1u << 10) | (1u << 15);             // P is e5m2; V is read along its rows
     const uint64_t p_desc = smem_desc_rows<128>(base + kPAt);
     uint32_t k = 0, seg = 0;
     bool ok = true;
@@ -194,7 +195,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           const uint64_t vd = ring_desc + (uint64_t)((L::kSlots + k % L::kSlots) * (uint32_t)(L::kSlot >> 4)), pd = p_desc + (uint64_t)((k & 1u) * (uint32_t)(L::kPBytes >> 4));
 #pragma unroll
           for (int i = 0; i < kTile / 32; ++i)
-            tc_mma_e4m3(o + (k & 1u) * NP, vd + (uint64_t)(i * (32 * DH >> 4)), pd + (uint64_t)(2 * i), idesc, (s >= 2) | (i > 0) ? 1u : 0u);
+            tc_mma_8bit(o + (k & 1u) * NP, vd + (uint64_t)(i * (32 * DH >> 4)), pd + (uint64_t)(2 * i), idesc, (s >= 2) | (i > 0) ? 1u : 0u);
           tc_commit(ring.v_empty(k));
           if (s + 1 == n) tc_commit(b_done + 8 * (seg & 1u));
         }
@@ -259,11 +260,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
       const size_t pr = ((size_t)blockIdx.x * 2 + (seg == 0 ? 0 : 1)) * a.block_rows;
 #pragma unroll 1
       for (int c0 = 0; c0 < rows; c0 += 4) {
-        float o[2][3][4];
+        float o[2][kCodes8][4];
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
-          for (int g = 0; g < 3; ++g) tmem_ld<4>(o_base + par * (2 * NP) + (uint32_t)(w * NP + g * RB + c0), o[w][g]);
+          for (int g = 0; g < kCodes8; ++g) tmem_ld<4>(o_base + par * (2 * NP) + (uint32_t)(w * NP + g * RB + c0), o[w][g]);
         tc_wait_ld();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -275,11 +276,11 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           const float f0 = m0 == M ? 1.0f : exp2f(m0 - M), f1 = m1 == M ? 1.0f : exp2f(m1 - M);
           float y = 0.0f, sum = 0.0f;
           if (has0) {
-            y = f0 * (o[0][0][i] + 0x1p-5f * (o[0][1][i] + 0x1p-5f * o[0][2][i]));
+            y = f0 * (o[0][0][i] + 0x1p-3f * (o[0][1][i] + 0x1p-3f * (o[0][2][i] + 0x1p-3f * o[0][3][i])));
             sum = f0 * (sum_s[par][0][0][r] + sum_s[par][0][1][r] + sum_s[par][0][2][r] + sum_s[par][0][3][r]);
           }
           if (has1) {
-            y += f1 * (o[1][0][i] + 0x1p-5f * (o[1][1][i] + 0x1p-5f * o[1][2][i]));
+            y += f1 * (o[1][0][i] + 0x1p-3f * (o[1][1][i] + 0x1p-3f * (o[1][2][i] + 0x1p-3f * o[1][3][i])));
             sum += f1 * (sum_s[par][1][0][r] + sum_s[par][1][1][r] + sum_s[par][1][2][r] + sum_s[par][1][3][r]);
           }
           uint32_t bad = bad_s[par];
@@ -390,7 +391,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           }
           if (any) {
 #pragma unroll 1
-            for (int g = 0; g < 3; ++g) {
+            for (int g = 0; g < kCodes8; ++g) {
 #pragma unroll 1
               for (int c = 0; c < RB; c += 8) {
                 if (c >= rows) break;
@@ -407,7 +408,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
             tc_wait_st();
           }
         }
-        // ---- weights, as three codes each; the product before has to have read the last ones
+        // ---- weights, as four codes each; the product before has to have read the last ones
         if (ok && !waited && k >= 2) ok = wait8(wt, ring.v_empty(k - 2), Ring::v_parity(k - 2));
 #pragma unroll
         for (int r = 0; r < RB; r += 2) {
@@ -415,15 +416,15 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           const float w0 = ex2_approx(z[r] - sub[r]), w1 = ex2_approx(z[r + 1] - sub[r + 1]);
           l[r] = fmaf(w0, e_inv, l[r]);
           l[r + 1] = fmaf(w1, e_inv, l[r + 1]);
-          const __half2 step = __float2half2_rn(32.0f);
+          const __half2 step = __float2half2_rn(8.0f);
           __half2 h = __floats2half2_rn(w0, w1);
 #pragma unroll
-          for (int g = 0; g < 3; ++g) {
-            const uint32_t c = encode_f16x2(h);
+          for (int g = 0; g < kCodes8; ++g) {
+            const uint32_t c = *reinterpret_cast<const uint32_t*>(&h) & 0xff00ff00u;
             const int n0 = g * RB + r, n1 = n0 + 1;
-            p_row[n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4)] = (uint8_t)c;
-            p_row[n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4)] = (uint8_t)(c >> 8);
-            if (g < 2) h = __hmul2(__hsub2(h, decode_f16x2(c)), step);
+            p_row[n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4)] = (uint8_t)(c >> 8);
+            p_row[n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4)] = (uint8_t)(c >> 24);
+            if (g < kCodes8 - 1) h = __hmul2(__hsub2(h, *reinterpret_cast<const __half2*>(&c)), step);
           }
         }
         if (__any_sync(0xffffffffu, dead || from > 0)) {

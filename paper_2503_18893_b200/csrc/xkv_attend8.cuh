@@ -9,6 +9,14 @@
 
 namespace xkv {
 
+// A weight is 2^(z - m) in 16 bits (fp16): 11 bits from 2^-14 up, steps of 2^-24 below, 2^16 at most.  The largest of a query row is put
+// between 2^9 and 2^15.75: m moves when one would pass that, and then so that it becomes 2^9.  So a weight is off by 2^-11 of itself or
+// 2^-34 of the largest; 2^22 rows together by 2^-12 of it.  (With the largest between 1 and 2^8, an even rest of weights 2^-24 of the
+// largest beside it was off by a third, and gone from 2^-26 on.  The higher the largest is put, the more often it moves: a chunk of 512
+// tokens over 12301 rows takes 221 us with 2^8, 226 with 2^9, 236 with 2^11; 16 query rows of 131072 220, 220, 228.  m moves for its own
+// row's sake only: what a token attends to does not depend on the tokens beside it.)
+constexpr float kTop = 15.75f, kSet = 9.0f;    // log2
+
 // A whole warp waits (as wait_warp does), asleep for most of the time: warps that poll take their SM's issue slots from those that work.
 static __device__ bool wait8_slow(const Wait& w, uint32_t bar, uint32_t parity) {
   unsigned long long t0, t;
@@ -203,11 +211,6 @@ __device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int gri
 __device__ __forceinline__ uint32_t encode_f32x2(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t encode_f16x2(__half2 x) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&x)));
   return r;
 }
 __device__ __forceinline__ __half2 decode_f16x2(uint32_t codes) {

@@ -11,7 +11,7 @@
 //              taken out of rows that only some see, and listed
 //   issuer     S of a tile two ahead, O += P V with P in tensor memory, where it lies over S
 //   softmax    two warpgroups; a query row is a TMEM lane, which two threads share, each with half of a tile's columns.  O is rescaled only
-//              when a maximum has grown by more than 2^8 (fp16 holds weights of 2^8, and of 2^-24): one vote of the two warps per tile.
+//              when a weight would pass 2^15.75 (kTop): one vote of the two warps per tile
 // Bound by the softmax: what a warp does for a row of a tile (logits from tensor memory, maximum, exponentials, weights back) is longer than
 // its instructions, and two warps of an SM's quarter do not fill it; warps that poll beside them make it worse.  131072 rows of four layers of
 // eight heads with four query heads: 8 tokens 323 us, 16 333, 32 356; a chunk of 512 tokens over 12301 rows of two sequences, seven query
@@ -27,7 +27,6 @@ namespace xkv {
 namespace {
 
 constexpr int kRows8 = 128;                    // query rows of a block
-constexpr float kGrow8 = 8.0f;                 // log2 of the growth of a maximum that makes O be rescaled
 
 template <int DH>
 struct Wide8 {
@@ -163,7 +162,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       const int m = row;
       const bool live = m < rows, warp_live = (m & ~31) < rows;
       const int limit = new0 + (live ? token_of(m) : 0) + 1;   // rows of the cache that this query row sees
-      float m_used = -INFINITY, l = 0.0f;
+      float m_used = -INFINITY, l = 0.0f;      // what is taken off z, the sum of weights
       const int n = t1 - t0;
       for (int s = 0; s < n; ++s) {
         constexpr int CW = kTile / 2, NC = CW / 32, NP = CW / 16;              // columns of a thread
@@ -208,7 +207,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         }
         // Both have their logits in registers now: weights may go where the other's lay.  Does a maximum move (or has a wait run out)?
         tc_fence_before();
-        const bool vote = !ok || (warp_live && (top > m_used + kGrow8 || (m_used == -INFINITY && top > -INFINITY)));
+        const bool vote = !ok || (warp_live && top > m_used + kTop);
         if (named_bar_any(pair, 64, vote)) {
           // O holds the tiles before this one once the last product is done, which the commit of the next S tells, or its own
           const bool next = s + 1 < n;
@@ -216,10 +215,10 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
           tell_s[side][row] = top;
           if (named_bar_any(pair, 64, !ok)) { gone = true; break; }
           tc_fence_after();
-          const float m_new = fmaxf(m_used, fmaxf(top, tell_s[side ^ 1][row]));
-          const bool grow = m_new > m_used + kGrow8 || (m_used == -INFINITY && m_new > -INFINITY);
-          const float g = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - m_new)) : 1.0f;
-          if (grow) m_used = m_new;
+          const float m = fmaxf(top, tell_s[side ^ 1][row]);
+          const bool grow = m > m_used + kTop;
+          const float g = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - (m - kSet))) : 1.0f;
+          if (grow) m_used = m - kSet;
           l *= g;
           if (s > 0 && __any_sync(0xffffffffu, grow)) {
 #pragma unroll 1
@@ -420,7 +419,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < DH / 32; ++i)
-            tc_mma_e4m3(tmem + (k & 1u) * 128u, q_desc + (uint64_t)(h * (L::kQPart >> 4) + 2 * i), kd + (uint64_t)(2 * i), idesc_s, h | i ? 1u : 0u);
+            tc_mma_8bit(tmem + (k & 1u) * 128u, q_desc + (uint64_t)(h * (L::kQPart >> 4) + 2 * i), kd + (uint64_t)(2 * i), idesc_s, h | i ? 1u : 0u);
         tc_commit(b_s + 8 * (k & 1u));
         tc_commit(ring.k_empty(k));
       };
