@@ -7,8 +7,8 @@
 //   S^T = K8 Q8^T       M = 128 rows of the cache, N = 2 x query rows
 //   O^T += V8^T P8^T    M = d_h, N = 4 x query rows, K = 128 rows of the cache
 // Both operands of such a product have to be 8-bit codes; a query and a weight are split into several:
-//   q 2^-x = q_hi + q_lo   (x: its row's largest element lies in [128, 256)): a bf16 value's 8 bits are two codes, exactly for elements
-//                          above 2^-10 of the largest, to 2^-18 of it below.  Two columns of S, added.
+//   q 2^-x = q_hi + 2^-5 q_lo   (x: its row's largest element lies in [128, 256)): a bf16 value's 8 bits are two e4m3 codes (encode_query),
+//                          two columns of S
 //   w = w_0 + 2^-3 w_1 + 2^-6 w_2 + 2^-9 w_3   of a weight in 16 bits (fp16), exactly, in e5m2: that is an fp16 number's upper byte, so a code
 //                          is cut off, not converted, and the next is that of 2^3 times what it left (3 bits of 11 each; 2^-9 times the
 //                          smallest code is 2^-25).  Four groups of columns of O, joined at the end.  What 16 bits mean to a weight
@@ -222,7 +222,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         if (r < rows) v = *reinterpret_cast<const uint4*>(a.q + (qh0 + (size_t)tok * a.H_q + (r - tok * a.n_rep)) * DH + c * 8);
         uint2 hi, lo;
         int ex;
-        encode_query<C>(v, &hi, &lo, &ex);
+        encode_query<C, true>(v, &hi, &lo, &ex);
         uint8_t* at = gen + kQAt + par * L::kQBytes + tile_place<DH>(r, c);
         *reinterpret_cast<uint2*>(at) = hi;
         *reinterpret_cast<uint2*>(at + RB * DH) = lo;
@@ -347,7 +347,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
           float lo[RB];
           load_columns<RB>(tmem + lane_base + (k % NB) * NQ, z, lo);
 #pragma unroll
-          for (int r = 0; r < RB; ++r) z[r] += lo[r];
+          for (int r = 0; r < RB; ++r) z[r] = fmaf(lo[r], 0x1p-5f, z[r]);
         }
         bool grow = !ok;
 #pragma unroll

@@ -207,10 +207,15 @@ __device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int gri
   return p;
 }
 
-// ---- e4m3
+// ---- 8-bit codes
 __device__ __forceinline__ uint32_t encode_f32x2(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t encode_e5m2x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
 __device__ __forceinline__ __half2 decode_f16x2(uint32_t codes) {
@@ -330,8 +335,10 @@ struct Ring8 {
 };
 
 // Eight elements of a query row as two codes each, by a lane of the C that hold the row side by side: the row's largest element lies in
-// [128, 256) times 2^ex.  A row with an element that is not finite becomes NaN.
-template <int C>
+// [128, 256) times 2^ex, the first code is e4m3, and what it leaves goes to the second, as 2^5 times it in e4m3 (SCALED: columns of their
+// own) or as it is in e5m2 (a product into the same columns).  A bf16 value's 8 bits are exact from 2^-14 of the largest element up
+// (e5m2: 2^-13); below, off by 2^-22 of it at most (2^-21).  (Both codes in e4m3 without a factor: 2^-17, from 2^-9 down.)  A row with an element that is not finite becomes NaN.
+template <int C, bool SCALED>
 __device__ __forceinline__ void encode_query(const uint4& x, uint2* hi, uint2* lo, int* ex) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t top = 0;
@@ -348,7 +355,7 @@ __device__ __forceinline__ void encode_query(const uint4& x, uint2* hi, uint2* l
     const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
     h[e] = encode_f32x2(x0, x1);
     const float2 b = __half22float2(decode_f16x2(h[e]));
-    l[e] = encode_f32x2(x0 - b.x, x1 - b.y);
+    l[e] = SCALED ? encode_f32x2((x0 - b.x) * 32.0f, (x1 - b.y) * 32.0f) : encode_e5m2x2(x0 - b.x, x1 - b.y);
   }
   *hi = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
   *lo = make_uint2(l[0] | (l[1] << 16), l[2] | (l[3] << 16));

@@ -1,6 +1,6 @@
 // Attention over a paged cache of 8-bit codes for many query rows (drafted tokens, a prompt's chunk): blocks of 128 rows, the rows of Q
 // being the wide side of both products.
-//   S = Q8 K8^T      e4m3 as the keys lie in memory, queries as two codes (see xkv_attend8.cu): two products into the same S
+//   S = Q8 K8^T      e4m3 as the keys lie in memory, queries as two codes (e4m3 and e5m2: encode_query): two products into the same S
 //   O += P V         16 bits (fp16, which holds every code): a tile's values are converted once for all rows of the block, and weights need
 //                    no splitting, so that this product takes two thirds of what three e4m3 ones would
 // Scales as there: a key's multiplies the logits, a value's exponent joins the weight's.
@@ -147,7 +147,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
             const int r = (warp & 3) * 32 + i0 + i * STEP + lane / C;
             uint2 hi, lo;
             int ex;
-            encode_query<C>(v[i], &hi, &lo, &ex);
+            encode_query<C, false>(v[i], &hi, &lo, &ex);
             uint8_t* at = q_gen + tile_place<DH>(r, c);
             *reinterpret_cast<uint2*>(at) = hi;
             *reinterpret_cast<uint2*>(at + L::kQPart) = lo;
@@ -407,7 +407,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       }
     } else if (warp == kIssuer8) {
       // ---- branches outside the issue are taken on a vote and descriptors differ by constants, so that they stay in uniform registers
-      constexpr uint32_t idesc_s = idesc_e4m3_f32(128, 128);
+      constexpr uint32_t idesc_s = idesc_e4m3_f32(128, 128), e5m2_a = 1u << 7;
       constexpr uint32_t idesc_o = (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((128u >> 4) << 24);   // fp16; V is read along its rows
       const uint64_t q_desc = smem_desc_rows<DH>(base + kQAt), k_desc = smem_desc_rows<DH>(base);
       const uint64_t v_desc = (smem_desc_sw128(base + kVAt, 0) & ~(0xFFFFull << 16)) | ((uint64_t)(L::kSlab >> 4) << 16);
@@ -419,7 +419,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < DH / 32; ++i)
-            tc_mma_8bit(tmem + (k & 1u) * 128u, q_desc + (uint64_t)(h * (L::kQPart >> 4) + 2 * i), kd + (uint64_t)(2 * i), idesc_s, h | i ? 1u : 0u);
+            tc_mma_8bit(tmem + (k & 1u) * 128u, q_desc + (uint64_t)(h * (L::kQPart >> 4) + 2 * i), kd + (uint64_t)(2 * i), h ? idesc_s | e5m2_a : idesc_s, h | i ? 1u : 0u);
         tc_commit(b_s + 8 * (k & 1u));
         tc_commit(ring.k_empty(k));
       };
