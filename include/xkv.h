@@ -546,7 +546,8 @@ XKV_API int xkv_cache8_read(const xkv_cache8_config* cfg, int layer_begin, int l
  * Tokens that belong to no sequence (before first[0], behind first[batch]) are left as they were.  A token that attends to nothing
  * (length[b] - n_b + i < 0, or all its rows' pages out of range), or whose logits are all minus infinity, gets 0 and lse -inf.
  * A row that a token does not attend to has no influence on it, also where its codes are NaN.  A query with an element that is not
- * finite gets NaN.  Scales are read as powers of two (their exponents); one of 0 marks a page that holds nothing: it is left out.
+ * finite gets NaN.  Scales are read as powers of two (their exponents), values' between 2^-90 and 2^120; one of 0 marks a page that holds nothing: it is left out,
+ * whatever its other one is.  One that is not finite makes NaN of the tokens that attend to its page's rows.
  * Queries enter the product with the keys to 2^-21 of their largest element, weights the one with the values to 2^-11 of themselves or
  * 2^-34 of the largest weight (times its value's scale); sums, maxima and the products' accumulation are fp32.  What values of one head
  * stand for may differ by 2^60 between its pages; beyond that the denominator loses the fainter page's share.

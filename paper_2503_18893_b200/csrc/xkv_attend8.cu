@@ -333,13 +333,13 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         const uint32_t k = k0 + s;
         ok = ok && wait8(wt, ring.scales_full(k), Ring::scales_parity(k));
         const float2 sc = scale_s[k % SR][row >> a.page_shift];
-        const float ks = __int_as_float(__float_as_int(sc.x) & 0x7f800000);
-        const int ve = (__float_as_int(sc.y) >> 23) & 255;
+        const int ke = (__float_as_int(sc.x) >> 23) & 255, ve = (__float_as_int(sc.y) >> 23) & 255;
+        const float ks = __int_as_float(ke << 23);
         const int j = (t0 + s) * kTile + row;
         // columns from `from` on see the row
-        const bool dead = j >= seen || !(ks > 0.0f) || ve == 0;
+        const bool dead = j >= seen || ke == 0 || ve == 0;
         const int from = dead ? RB : max(0, min(j - new0, 64) * a.n_rep);
-        const float e = (float)(ve - 127), e_inv = __int_as_float((254 - ve) << 23);
+        const float e = ke == 255 || ve == 255 ? __int_as_float(0x7fffffff) : (float)(ve - 127), e_inv = turned_over(ve);
         ok = ok && wait8(wt, ring.k_empty(k), Ring::k_parity(k));
         tc_fence_after();
         float z[RB];

@@ -223,6 +223,8 @@ __device__ __forceinline__ __half2 decode_f16x2(uint32_t codes) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
   return *reinterpret_cast<__half2*>(&h);
 }
+// 2^(127 - e), finite for every e of 0 .. 255: rows that are left out are multiplied by it, too.
+__device__ __forceinline__ float turned_over(int e) { return __int_as_float(max((254 - e) << 23, 0x400000)); }
 // Does one of four codes say NaN?
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu); }
 

@@ -62,7 +62,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
   __shared__ long long count_s;
   __shared__ float2 scale_s[SR][8];
   __shared__ float4 page_s[SR][8];             // of a tile's pages: keys' scale, values' exponent, its power of two turned over
-  __shared__ uint32_t dead_s[SR];              // which of them hold nothing
+  __shared__ uint32_t dead_s[SR];              // which of them hold nothing (bits 0-7), which have a scale that is not finite (8-15)
   // New rows of a block with value codes that are NaN, by segment: converters are less than eight segments ahead of the softmax.
   __shared__ uint32_t bad_s[16][4];
   // Of a query row: its factor; what the two threads that share it tell one another
@@ -191,9 +191,10 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
           if (j0 + CW > new0 + 1 || dead) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-              const int see = dead >> ((col0 + 16 * i) >> a.page_shift) & 1u ? 0 : limit - (j0 + 16 * i);
+              const uint32_t is = dead >> ((col0 + 16 * i) >> a.page_shift), nan = is & 0x100u ? 0x7fffffffu : 0u;
+              const int see = is & 1u ? 0 : limit - (j0 + 16 * i);
 #pragma unroll
-              for (int x = 0; x < 16; ++x) z[i / 2][16 * (i & 1) + x] = x < see ? z[i / 2][16 * (i & 1) + x] : 0xff800000u;
+              for (int x = 0; x < 16; ++x) z[i / 2][16 * (i & 1) + x] = x < see ? z[i / 2][16 * (i & 1) + x] | nan : 0xff800000u;
             }
           }
 #pragma unroll
@@ -398,10 +399,10 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
       for (uint32_t k = 0; k < (uint32_t)count_s; ++k) {
         if (!wait8(wt, ring.scales_full(k), Ring::scales_parity(k))) break;
         const float2 sc = scale_s[k % SR][min(lane, 127 >> a.page_shift)];
-        const int kb = __float_as_int(sc.x) & 0x7f800000, ve = (__float_as_int(sc.y) >> 23) & 255;
-        const uint32_t dead = __ballot_sync(0xffffffffu, kb == 0 || ve == 0);
-        if (lane < 8) page_s[k % SR][lane] = make_float4(kb == 0 ? 1.0f : __int_as_float(kb), (float)(ve - 127), __int_as_float((254 - ve) << 23), 0.0f);
-        if (lane == 0) dead_s[k % SR] = dead;
+        const int ke = (__float_as_int(sc.x) >> 23) & 255, ve = (__float_as_int(sc.y) >> 23) & 255;
+        const uint32_t dead = __ballot_sync(0xffffffffu, ke == 0 || ve == 0) & 0xffu, odd = __ballot_sync(0xffffffffu, ke == 255 || ve == 255) & 0xffu;
+        if (lane < 8) page_s[k % SR][lane] = make_float4(ke == 0 || ke == 255 ? 1.0f : __int_as_float(ke << 23), (float)(ve - 127), turned_over(ve), 0.0f);
+        if (lane == 0) dead_s[k % SR] = dead | odd << 8;
         __syncwarp();
         if (lane == 0) mbar_arrive(b_pg + 8 * (k % SR));
       }
