@@ -354,7 +354,7 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         for (int r = 0; r < RB; ++r) {
           if (r % 4 == 0 && r >= rows) break;
           const float2 col = info[r];
-          z[r] = fmaf(z[r], ks * col.x, e);
+          z[r] = fmaf(z[r] * ks, col.x, e);    // (in this order: what is 0 has the logit 0 also where the factors' product is infinite)
           z[r] = r >= from ? z[r] : -INFINITY;
           grow |= z[r] > col.y;
         }

@@ -182,7 +182,8 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
 #pragma unroll
           for (int i = 0; i < NP; ++i) {
             const float4 x = page_s[k % SR][(col0 + 16 * i) >> a.page_shift];
-            f[i] = x.x * qs;
+            // neither 0 nor infinite: a masked column stays minus infinity, and what is 0 has the logit 0
+            f[i] = fminf(fmaxf(x.x * qs, 0x1p-126f), 0x1.fffffep127f);
             e[i] = x.y;
             e_inv[i] = x.z;
           }

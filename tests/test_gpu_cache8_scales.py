@@ -62,3 +62,41 @@ def test_values_scales_at_the_ends_of_their_range(xkv, new, v_scale):
     # weights, sums and results differ by a power of two; the exponent of a weight is rounded with v_scale's in it, 2^-17 at most
     assert bool(((far.double() / v_scale - out.double()).abs() <= 2.0 ** -7 * out.double().abs() + 2.0 ** -16 * 448).all())
     assert bool(((far_lse - lse).abs() <= 2.0 ** -16).all())
+
+
+@pytest.mark.parametrize("new", NEWS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_query_of_zeros_over_faint_keys(xkv, new, d):
+    """Its logits are all 0, however small the keys' scales; a row behind a token's own stays out."""
+    for k_scale in (2.0 ** -60, 2.0 ** -90, 2.0 ** -100, 2.0 ** -126):
+        c = A.Case(xkv, [200, 30], [new, 1], H_kv=1, d=d, page=16, seed=5)
+        c.ks[:] = k_scale
+        c.q[0, 0] = 0.0
+        c.q[0, new - 1, 1] = 0.0
+        out, lse = c.run()
+        c.check(out, lse)
+        assert not bool(out.isnan().any())
+
+
+@pytest.mark.parametrize("new", NEWS)
+@pytest.mark.parametrize("scale", [1e-12, 1e-30, 1e-37, 1e-44])
+def test_a_tiny_softmax_scale(xkv, new, scale):
+    for k_scale in (2.0 ** -7, 2.0 ** -60):
+        c = A.Case(xkv, [200, 30], [new, 1], H_kv=1, page=16, seed=6, scale=scale)
+        c.ks[:] = k_scale
+        c.q[0, new - 1] = 0.0
+        out, lse = c.run()
+        c.check(out, lse)
+        assert not bool(out.isnan().any())
+
+
+@pytest.mark.parametrize("new", NEWS)
+def test_a_factor_beyond_fp32(xkv, new):
+    """Keys that are exactly 0 have logit 0 whatever scale and query say."""
+    c = A.Case(xkv, [120], [new], H_kv=1, page=16, seed=8)
+    c.ks[:] = 2.0 ** 100
+    c.q[:] = 2.0 ** 100
+    c.K[:] = 0
+    out, lse = c.run()
+    rows = torch.arange(120 - new + 1, 121, dtype=torch.float64, device="cuda")
+    assert bool(((lse[0].double() - rows.log()[:, None]).abs() <= 2.0 ** -18).all()) and not bool(out.isnan().any())
