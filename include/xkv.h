@@ -516,6 +516,8 @@ XKV_API int xkv_page_assign(const xkv_cache8_config* cfg, const int32_t* held, c
  *         if the run does not begin with the page's first row, the page holds the rows before it: then at least the old scale's exponent
  *   new codes = x 2^-e rounded to e4m3 (to nearest even), codes of the rows before the run = c 2^(e_old - e) rounded likewise
  *   scale = 2^e
+ * An old scale may be any power of two; one of 0 says that the page held nothing: the rows before the run become 0.  One that is not finite
+ * makes them NaN.
  * NaN becomes e4m3's NaN, infinities +-448 * 2^e.  Rows of a page behind the run are left as they were.
  * k, v   bf16 [G][n_tok][H_kv][d_h];  slot  int32 [n_tok], -1: the token is skipped (so are others out of range, flag).
  */

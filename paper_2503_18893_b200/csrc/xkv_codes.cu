@@ -18,7 +18,7 @@ namespace xkv {
 
 namespace {
 
-constexpr int kLowest = -60, kHighest = 120;   // exponents of scales (bf16's largest value is below 448 * 2^120)
+constexpr int kLowest = -60, kHighest = 120;   // exponents of scales of rows (bf16's largest value is below 448 * 2^120)
 constexpr int kAppendThreads = 256, kRunRows = 16;             // rows that a warp keeps
 
 struct CodesArgs {
@@ -35,11 +35,11 @@ struct CodesArgs {
   unsigned int* flags;
 };
 
-__device__ __forceinline__ float two_to(int e) { return __int_as_float((127 + e) << 23); }
-// The exponent of a scale, in the range that append gives (others come from memory that no call has written).
-__device__ __forceinline__ int exponent_of(float scale) {
-  return min(max(((__float_as_int(scale) >> 23) & 255) - 127, kLowest), kHighest);
-}
+// 2^e for -127 <= e <= 127.
+__device__ __forceinline__ float two_to(int e) { return e == -127 ? 0x1p-127f : __int_as_float((127 + e) << 23); }
+// The exponent of a scale; kNothing: it is 0 (or no normal number), kNotFinite: infinite or NaN.
+constexpr int kNothing = -127, kNotFinite = 128;
+__device__ __forceinline__ int exponent_of(float scale) { return ((__float_as_int(scale) >> 23) & 255) - 127; }
 // The smallest e with top <= 448 * 2^e = 1.75 * 2^(e + 8), for the bits of a bf16 magnitude.
 __device__ __forceinline__ int exponent_for(uint32_t top) {
   return min(max((int)(top >> 7) - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0), kLowest), kHighest);
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const CodesAr
     const size_t head = ((size_t)l * a.n_pages + (s >> a.page_shift)) * a.H_kv + h;
     uint8_t* codes = a.codes[kv] + (head << a.page_shift) * DH;
     float* scale = a.scale[kv] + head;
-    const int old = off > 0 ? exponent_of(*scale) : kLowest;
+    const int old = off > 0 ? exponent_of(*scale) : kNothing;
     const __nv_bfloat16* x = a.x[kv] + (((size_t)l * a.n_tok + t) * a.H_kv + h) * DH + lane * (2 * W);
     uint32_t v[kRunRows][W], top = 0;
 #pragma unroll
@@ -145,12 +145,12 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const CodesAr
       for (int i = 0; i < warps; ++i) top = max(top, top_s[group * warps + i]);
       ptx::named_bar_sync(1 + group, warps * 32);
     }
-    const int e = max(exponent_for(top), old);
-    if (e > old && off > 0) {
-      const float f = two_to(max(old - e, -126));
+    const int e = max(exponent_for(top), old == kNotFinite ? kLowest : old);
+    if (e != old && off > 0) {
+      const float f = old == kNotFinite ? __int_as_float(0x7fffffff) : two_to(max(old - e, -126));
       for (int i = part * 32 + lane; i < off * (DH / 4); i += warps * 32) {
         uint32_t* at = reinterpret_cast<uint32_t*>(codes) + i;
-        const uint32_t c = *at;
+        const uint32_t c = old == kNothing ? 0u : *at;
         const float2 lo = decode2(c), hi = decode2(c >> 16);
         *at = encode2(lo.x * f, lo.y * f) | (encode2(hi.x * f, hi.y * f) << 16);
       }
