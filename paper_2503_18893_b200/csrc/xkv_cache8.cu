@@ -58,6 +58,7 @@ int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const xkv_rope_
     return XKV_ERR_INVALID_ARG;
   if (direction < XKV_ROPE_FORWARD || direction > XKV_ROPE_INVERSE || type < XKV_BF16 || type > XKV_FP32) return XKV_ERR_INVALID_ARG;
   if (rows < 0 || n_pos < 1 || rows % n_pos != 0 || !pos || !aligned_to(4, {pos})) return XKV_ERR_INVALID_ARG;
+  int64_t heads = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const xkv_rope_tensor& t = tensors[i];
     if (t.heads < 0) return XKV_ERR_INVALID_ARG;
@@ -65,7 +66,9 @@ int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const xkv_rope_
     if (!t.x || !t.y || !aligned_to(type == XKV_FP32 ? 4 : 2, {t.x, t.y})) return XKV_ERR_INVALID_ARG;
     if (t.x == t.y && (t.x_row != t.y_row || t.x_head != t.y_head)) return XKV_ERR_INVALID_ARG;
     if ((double)rows * t.heads >= 2147483648.0) return XKV_ERR_UNSUPPORTED;
+    heads += t.heads;
   }
+  if (heads >= 2147483648LL - 1024) return XKV_ERR_UNSUPPORTED;               // (a thread steps past the last by its CTA's threads)
   int device = 0;
   const int st = current_sm100_device(&device);
   if (st != XKV_OK) return st;
