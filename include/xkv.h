@@ -472,7 +472,7 @@ XKV_API int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const x
  * No handle and no allocation.  flags as for the uncompressed cache: one device word or NULL.  A page number outside [0, n_pages), a
  * length or a slot out of range is not followed: what it names is skipped, XKV_FLAG_INDEX_RANGE is raised.
  * Limits: d_h 64 or 128, H_q a multiple of H_kv with H_q/H_kv <= 16, page 16, 32, 64 or 128, max_pages * page <= XKV_CACHE_MAX_ROWS
- * (else INVALID_ARG); G*batch*H_kv <= 65535, G*n_pages*H_kv*page < 2^31, G*n_tok*H_q < 2^31 (else UNSUPPORTED).  K8, V8, q, k, v, K, V, out
+ * (else INVALID_ARG); G*batch*H_kv <= 65535, G*n_pages*H_kv*page < 2^31; append, attend: G*n_tok*H_q < 2^31 (else UNSUPPORTED).  K8, V8, q, k, v, K, V, out
  * and workspaces are 16-byte aligned, int32 and fp32 arrays 4-byte.  Layers layer_begin <= l < layer_end are worked on; arrays span all
  * G.  Calls may run at the same time as long as none writes what another reads or writes.
  * Errors of all of them: INVALID_ARG, UNSUPPORTED, ARCH, CUDA.

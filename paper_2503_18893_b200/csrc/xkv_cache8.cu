@@ -93,6 +93,7 @@ int xkv_cache8_append(const xkv_cache8_config* cfg, int layer_begin, int layer_e
   if (st != XKV_OK) return st;
   if (!k || !v || !slot || !K8 || !V8 || !k_scale || !v_scale || n_tok < 0) return XKV_ERR_INVALID_ARG;
   if (!aligned_to(16, {k, v, K8, V8}) || !aligned_to(4, {slot, k_scale, v_scale, flags})) return XKV_ERR_INVALID_ARG;
+  if ((double)n_tok * cfg->H_q * cfg->G >= 2147483648.0) return XKV_ERR_UNSUPPORTED;
   int device = 0;
   if ((st = current_sm100_device(&device)) != XKV_OK) return st;
   if (n_tok == 0) return XKV_OK;

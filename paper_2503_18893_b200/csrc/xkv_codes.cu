@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const CodesAr
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int page = 1 << a.page_shift, warps = page / kRunRows, groups = kAppendThreads / 32 / warps;
   const int group = warp / warps, part = warp - group * warps;
-  const int t0 = ((int)blockIdx.x * groups + group) * a.per_group;
+  const int t0 = (int)min(((long long)blockIdx.x * groups + group) * a.per_group, (long long)a.n_tok);
   const int h = blockIdx.y, l = a.l0 + (int)(blockIdx.z >> 1), kv = blockIdx.z & 1;
   ptx::grid_dependency_wait();
   ptx::grid_dependency_launch();
@@ -230,7 +230,7 @@ cudaError_t launch_cache8_append(const xkv_cache8_config* c, int l0, int l1, con
   // looks for what is not finite only where there is something.)
   const int groups = kAppendThreads / 32 / (c->page / kRunRows);
   const long long per_token = (long long)c->H_kv * 2 * a.layers;
-  auto ctas = [&](int per_group) { return (n_tok + groups * per_group - 1) / (groups * per_group); };
+  auto ctas = [&](int per_group) { return (int)(((long long)n_tok + groups * per_group - 1) / (groups * per_group)); };
   a.per_group = 1;
   while (a.per_group < (c->page > 32 ? c->page : 32) && ctas(a.per_group) * per_token > kPlanSms * 16) a.per_group *= 2;
   const dim3 grid(ctas(a.per_group), c->H_kv, 2 * a.layers);

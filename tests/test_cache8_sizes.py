@@ -26,3 +26,10 @@ def test_heads_of_both_tensors_together(xkv, no_gpu):  # noqa: F811
     assert rope(xkv, ((1 << 31) - 1026, 1)) in fits
     assert rope(xkv, (1 << 30, (1 << 30) - 1025)) in fits
     assert rope(xkv, (1 << 10, 1 << 10), rows=(1 << 21) - 1) in fits
+
+
+def test_tokens_of_an_append(xkv, no_gpu):  # noqa: F811
+    cfg = config(xkv)                                    # G * H_q = 16
+    assert calls(xkv, cfg, n=1 << 27)["append"] == xkv.XKV_ERR_UNSUPPORTED
+    assert calls(xkv, cfg, n=(1 << 27) - 1)["append"] in (xkv.XKV_ERR_CUDA, xkv.XKV_ERR_ARCH)
+    assert calls(xkv, cfg, n=1 << 27)["assign"] in (xkv.XKV_ERR_CUDA, xkv.XKV_ERR_ARCH)
