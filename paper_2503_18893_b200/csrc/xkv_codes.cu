@@ -217,6 +217,20 @@ CodesArgs codes_args(const xkv_cache8_config* c, int l0, int l1, void* K8, void*
   return a;
 }
 
+// Keys and values of at most as many layers at a time as a grid's third dimension has room for.
+template <typename F>
+cudaError_t launch_layers(CodesArgs a, F launch) {
+  constexpr int kMost = 65535 / 2;
+  for (int l0 = a.l0, left = a.layers; left > 0; l0 += kMost, left -= kMost) {
+    a.l0 = l0;
+    a.layers = left < kMost ? left : kMost;
+    const cudaError_t e = launch(a, 2 * a.layers);
+    count_launch(kFamCodes);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 }  // namespace
 
 cudaError_t launch_cache8_append(const xkv_cache8_config* c, int l0, int l1, const __nv_bfloat16* k, const __nv_bfloat16* v,
@@ -233,11 +247,10 @@ cudaError_t launch_cache8_append(const xkv_cache8_config* c, int l0, int l1, con
   auto ctas = [&](int per_group) { return (int)(((long long)n_tok + groups * per_group - 1) / (groups * per_group)); };
   a.per_group = 1;
   while (a.per_group < (c->page > 32 ? c->page : 32) && ctas(a.per_group) * per_token > kPlanSms * 16) a.per_group *= 2;
-  const dim3 grid(ctas(a.per_group), c->H_kv, 2 * a.layers);
-  const cudaError_t e = c->d_h == 128 ? launch_pdl(append_kernel<2>, grid, dim3(kAppendThreads), 0, s, a)
-                                      : launch_pdl(append_kernel<1>, grid, dim3(kAppendThreads), 0, s, a);
-  count_launch(kFamCodes);
-  return e;
+  return launch_layers(a, [&](const CodesArgs& part, int z) {
+    const dim3 grid(ctas(part.per_group), c->H_kv, z), threads(kAppendThreads);
+    return c->d_h == 128 ? launch_pdl(append_kernel<2>, grid, threads, 0, s, part) : launch_pdl(append_kernel<1>, grid, threads, 0, s, part);
+  });
 }
 
 cudaError_t launch_cache8_read(const xkv_cache8_config* c, int l0, int l1, const int32_t* table, const int32_t* length, const void* K8,
@@ -246,11 +259,10 @@ cudaError_t launch_cache8_read(const xkv_cache8_config* c, int l0, int l1, const
   CodesArgs a = codes_args(c, l0, l1, const_cast<void*>(K8), const_cast<void*>(V8), const_cast<float*>(k_scale), const_cast<float*>(v_scale), flags);
   a.table = table; a.length = length; a.cap = cap; a.y[0] = K; a.y[1] = V;
   const int rows = kReadThreads / (c->d_h / 16), most = cap < c->max_pages * c->page ? cap : c->max_pages * c->page;
-  const dim3 grid((most + rows - 1) / rows, c->batch * c->H_kv, 2 * a.layers);
-  const cudaError_t e = c->d_h == 128 ? launch_pdl(read_kernel<128>, grid, dim3(kReadThreads), 0, s, a)
-                                      : launch_pdl(read_kernel<64>, grid, dim3(kReadThreads), 0, s, a);
-  count_launch(kFamCodes);
-  return e;
+  return launch_layers(a, [&](const CodesArgs& part, int z) {
+    const dim3 grid((most + rows - 1) / rows, c->batch * c->H_kv, z), threads(kReadThreads);
+    return c->d_h == 128 ? launch_pdl(read_kernel<128>, grid, threads, 0, s, part) : launch_pdl(read_kernel<64>, grid, threads, 0, s, part);
+  });
 }
 
 }  // namespace xkv
