@@ -5,6 +5,7 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include "xkv_blocks.h"
 #include "xkv_cache.cuh"
 
 namespace xkv {
@@ -75,29 +76,14 @@ __device__ __forceinline__ int rows_seen(const Attend8Args& a, const Seq& s, int
 }
 __device__ __forceinline__ int tiles_of(int rows) { return max(1, (rows + kTile - 1) / kTile); }
 
-// sum over i < n of floor((a i + b) / m), all of them below 2^31: Euclid's algorithm on (a, m).
-static __device__ long long floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
-  long long sum = 0;
-  while (n > 0) {
-    if (a >= m) { sum += (long long)n * (n - 1) / 2 * (a / m); a %= m; }
-    if (b >= m) { sum += (long long)n * (b / m); b %= m; }
-    const uint32_t y = a * n + b;
-    if (y < m) break;
-    n = y / m;
-    b = y % m;
-    const uint32_t t = m;
-    m = a;
-    a = t;
-  }
-  return sum;
-}
 // Tiles of one head in blocks 0 .. qp-1 of a sequence of n_qp blocks; those before the last are full: their rows grow by block_tok.
 static __device__ long long tiles_before(const Attend8Args& a, const Seq& s, int qp, int n_qp) {
   if (qp == 0) return 0;
   if (qp == n_qp) return tiles_before(a, s, qp - 1, n_qp) + tiles_of(rows_seen(a, s, qp - 1));
   const int most = kTile - s.base;             // blocks that see up to one tile count one
   const int ones = most > 0 ? min(qp, most / a.block_tok) : 0;
-  return ones + floor_sum(qp - ones, kTile, a.block_tok, (uint32_t)(s.base + (ones + 1) * a.block_tok + kTile - 1));
+  static_assert(kTile == 128, "tiles of sum_of_tiles");
+  return ones + sum_of_tiles(qp - ones, a.block_tok, s.base + (ones + 1) * a.block_tok + kTile - 1);
 }
 __device__ __forceinline__ long long tiles_of_head(const Attend8Args& a, const Seq& s) {
   if (s.n <= a.block_tok) return s.n > 0 ? tiles_of(rows_seen(a, s, 0)) : 0;
