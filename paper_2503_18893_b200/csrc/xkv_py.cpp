@@ -14,6 +14,7 @@
 #include <string>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -501,7 +502,7 @@ XKV_CACHE8_PY(cache8_attend, 18)
 XKV_CACHE_PY_END(xkv_cache8_attend(c, l0, l1, q, first, n, max_new, table, length, K8, V8, ks, vs, ws, need, out, lse, flags, s))
 
 // A tensor of heads: [..., heads, d_h] with the elements of a head side by side, and leading axes that join to one axis of rows.
-bool heads_of(Checked& a, const char* name, const at::Tensor& t, int d_h, void** p, int64_t* rows, int64_t* row, int64_t* head, int32_t* heads) {
+bool heads_of(Checked& a, const char* name, const at::Tensor& t, int d_h, int64_t* rows, int64_t* row, int64_t* head, int32_t* heads) {
   const char* what = nullptr;
   const int64_t n = t.dim();
   if (n < 3 || t.size(-1) != d_h) what = "is not [..., rows, heads, d_h]";
@@ -518,7 +519,6 @@ bool heads_of(Checked& a, const char* name, const at::Tensor& t, int d_h, void**
     PyErr_Format(PyExc_ValueError, "%s: the tensor %s", name, what);
     return false;
   }
-  *p = const_cast<void*>(t.const_data_ptr());
   *rows = r;
   *head = t.stride(-2);
   *heads = (int32_t)t.size(-2);
@@ -539,6 +539,8 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const int64_t n_pos = a.numel_of_next();
   const int32_t* pos = (const int32_t*)a.tensor("pos", at::kInt, {n_pos});
   xkv_rope_tensor t[2] = {};
+  const at::Tensor* xs[2];
+  const at::Tensor* ys[2];
   int n = 0, type = -1;
   int64_t rows = 0;
   for (int i = 0; i < 2 && !a.bad; ++i) {
@@ -554,25 +556,25 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const at::Tensor& ty = y == Py_None ? tx : THPVariable_Unpack(y);
     const at::ScalarType st = tx.scalar_type();
     const int ti = st == at::kBFloat16 ? XKV_BF16 : st == at::kHalf ? XKV_FP16 : st == at::kFloat ? XKV_FP32 : -1;
-    void *px, *py;
     int64_t rx, ry;
     int32_t hy;
     t[i].x_row = t[i].y_row = 0;
-    if (!heads_of(a, names[i][0], tx, plan->d_h, &px, &rx, &t[i].x_row, &t[i].x_head, &t[i].heads) ||
-        !heads_of(a, names[i][1], ty, plan->d_h, &py, &ry, &t[i].y_row, &t[i].y_head, &hy))
+    if (!heads_of(a, names[i][0], tx, plan->d_h, &rx, &t[i].x_row, &t[i].x_head, &t[i].heads) ||
+        !heads_of(a, names[i][1], ty, plan->d_h, &ry, &t[i].y_row, &t[i].y_head, &hy))
       return nullptr;
     const char* what = nullptr;
     if (ti < 0) what = "bfloat16, float16 or float32 expected";
     else if (i == 1 && ti != type) what = "both tensors have to have the same type";
     else if (ty.scalar_type() != st || ry != rx || hy != t[i].heads) what = "the output has another type or shape";
     else if (i == 1 && rx != rows) what = "both tensors have to have as many rows";
+    else if (at::GradMode::is_enabled() && ty.requires_grad()) what = "what is written requires a gradient, which would not learn of the rotation";
     else if (n_pos < 1 || rx % n_pos) what = "the number of positions does not divide the number of rows";
     if (what) {
       PyErr_Format(PyExc_ValueError, "%s: %s", names[i][0], what);
       return nullptr;
     }
-    t[i].x = px;
-    t[i].y = py;
+    xs[i] = &tx;
+    ys[i] = &ty;
     rows = rx;
     type = ti;
     n = i + 1;
@@ -580,11 +582,15 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (n == 1) a.at = 7;
   void* s = a.stream();
   if (a.bad) return nullptr;
+  for (int i = 0; i < n; ++i) t[i].y = ys[i]->mutable_data_ptr();              // (a lazy clone gets memory of its own: before addresses are taken)
+  for (int i = 0; i < n; ++i) t[i].x = xs[i]->const_data_ptr();
   int st;
   {
     const WithoutGil no_gil;
     st = xkv_rope(plan, direction, type, t, n, rows, pos, n_pos, s);
   }
+  // what was saved for a backward pass and is written into now is no longer what it was
+  for (int i = 0; i < n && st == XKV_OK; ++i) if (!ys[i]->is_inference()) ys[i]->unsafeGetTensorImpl()->bump_version();
   return PyLong_FromLong(st);
   END_HANDLE_TH_ERRORS
 }

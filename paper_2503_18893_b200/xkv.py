@@ -553,7 +553,8 @@ def make_rope(*, d_h, rot=None, layout="half", base=10000.0, scaling="none", fac
 def xkv_rope(plan: xkv_rope_plan, x, pos, out=None, x2=None, out2=None, *, direction="forward", stream=None) -> None:
     """Rotates x [..., rows, heads, d_h] (and x2, with as many rows) by the positions `pos` int32, into `out` or in place.  Rows and
     heads may lie at any distance, the elements of a head side by side; row r has position pos[r % len(pos)].
-    `direction`: "forward", "adjoint" (the gradient of forward) or "inverse" (undoes forward)."""
+    `direction`: "forward", "adjoint" (the gradient of forward) or "inverse" (undoes forward).  Nothing is recorded for autograd: a tensor
+    that requires a gradient is not written into (but under no_grad), and one that is counts as modified in place."""
     if direction not in XKV_ROPE_DIRECTIONS:
         raise ValueError(f"direction: {direction!r} is none of {', '.join(XKV_ROPE_DIRECTIONS)}")
     st = _xkv.rope(ctypes.addressof(plan), XKV_ROPE_DIRECTIONS[direction], pos, x, out, x2, out2, stream)
