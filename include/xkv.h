@@ -466,7 +466,10 @@ XKV_API int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const x
  * step, 2^-4 of the value, down to 2^-15 of the page's largest).
  *   xkv_page_assign    lengths of sequences that grow and shrink -> pages, places of new tokens
  *   xkv_cache8_append  new keys and values into their places
- *   xkv_cache8_read    rows back as an uncompressed cache (for xkv_dense_attend, xkv_tree_attend, xkv_clf_factorize)
+ *   xkv_cache8_read    rows back as an uncompressed cache (for xkv_dense_attend, xkv_tree_attend).  On the way to a compressed window one
+ *                      sequence is read at a time (batch 1, its row of the table): keys [G][1][H_kv][cap][d_h] are cap rows of G*H_kv heads, d_h
+ *                      and cap*d_h elements apart, which one call of xkv_rope turns back into X [T][G*d] of xkv_clf_factorize; values, and rotated
+ *                      keys for xkv_build_landmarks (rope_base 0), are the caller's to copy into the order of axes that is wanted there
  *   xkv_cache8_attend  attention of each sequence's last tokens over its rows
  * New tokens of a step lie behind one another, sequence by sequence: those of sequence b from first[b] to first[b+1] - 1 of n_tok.
  * No handle and no allocation.  flags as for the uncompressed cache: one device word or NULL.  A page number outside [0, n_pages), a
