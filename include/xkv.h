@@ -499,7 +499,8 @@ typedef struct {
  *            given back become -1, others are left as they are.
  * ring       int32 [n_pages], in and out, page numbers;  state  int32 [2], in and out: place of the first free page in the ring, free
  *            pages.  At the start ring = 0 .. n_pages-1, state = (0, n_pages).  A state out of range counts as no free page (flag).
- *            Pages given back that find no room in the ring (it would hold more than n_pages) are dropped (flag).
+ *            Pages given back that find no room in the ring (it would hold more than n_pages) are dropped (flag).  A page number out of
+ *            range that is taken or given back goes its way as it is (flag).
  * length     out int32 [batch]: want[b], or held[b] of a sequence that got no pages.  May be held or want.
  * first      out int32 [batch+1] or NULL: sums of max(want - held, 0): the places of new tokens, also of those that got no pages.
  *            (int32: a sum of 2^31 or more is cut to 2^31 - 1, flag).

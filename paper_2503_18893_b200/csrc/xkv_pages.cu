@@ -127,13 +127,18 @@ __global__ void __launch_bounds__(kSeqs) page_assign_kernel(const PageArgs a) {
     }
     for (int i = rank * kSeqs + tid; i < all.take; i += ranks * kSeqs) {       // pages taken
       const int x = sequence_of(take_s, i), h = held_s[x];
-      if (h >= 0) a.table[(size_t)(b0 + x) * a.max_pages + ((h + page - 1) >> a.page_shift) + i - take_s[x]] = a.ring[place(take0 + i)];
+      if (h >= 0) {
+        const int p = a.ring[place(take0 + i)];
+        a.table[(size_t)(b0 + x) * a.max_pages + ((h + page - 1) >> a.page_shift) + i - take_s[x]] = p;
+        bad |= p < 0 || p >= a.n_pages;
+      }
     }
     for (int i = rank * kSeqs + tid; i < all.give; i += ranks * kSeqs) {       // pages given back
       const int x = sequence_of(give_s, i);
       int32_t* entry = a.table + (size_t)(b0 + x) * a.max_pages + ((want_s[x] + page - 1) >> a.page_shift) + i - give_s[x];
-      if (give0 + i < room) a.ring[place(count + give0 + i)] = *entry;
-      else bad = true;
+      const int p = *entry;
+      if (give0 + i < room) a.ring[place(count + give0 + i)] = p;
+      bad |= give0 + i >= room || p < 0 || p >= a.n_pages;
       *entry = -1;
     }
     if (a.slot) {
