@@ -418,7 +418,7 @@ typedef struct {
   double original;             /* LLAMA3, YARN: positions of the context that the model was trained on, > 0 */
   double low, high;            /* LLAMA3: high > low > 0 */
   double beta_fast, beta_slow; /* YARN: > 0 */
-  double gain;                 /* 0: the scaling's own */
+  double gain;                 /* 0: the scaling's own; it and 1 / gain finite in fp32 */
 } xkv_rope_config;
 typedef struct {
   uint32_t struct_size;        /* sizeof(xkv_rope_plan) */

@@ -54,7 +54,8 @@ int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const xkv_rope_
              const int32_t* pos, int64_t n_pos, void* stream) {
   if (!plan || plan->struct_size != sizeof(xkv_rope_plan) || !tensors || n_tensors < 1 || n_tensors > 2) return XKV_ERR_INVALID_ARG;
   if (plan->d_h < 2 || plan->d_h > 1024 || plan->d_h % 2 || plan->rot < 2 || plan->rot % 2 || plan->rot > plan->d_h ||
-      plan->rot > XKV_ROPE_MAX_ROT || (plan->layout != XKV_ROPE_HALF && plan->layout != XKV_ROPE_INTERLEAVED) || !(plan->gain > 0.0f))
+      plan->rot > XKV_ROPE_MAX_ROT || (plan->layout != XKV_ROPE_HALF && plan->layout != XKV_ROPE_INTERLEAVED) || !(plan->gain > 0.0f) || isinf(plan->gain) ||
+      isinf(1.0f / plan->gain))
     return XKV_ERR_INVALID_ARG;
   if (direction < XKV_ROPE_FORWARD || direction > XKV_ROPE_INVERSE || type < XKV_BF16 || type > XKV_FP32) return XKV_ERR_INVALID_ARG;
   if (rows < 0 || n_pos < 1 || rows % n_pos != 0 || !pos || !aligned_to(4, {pos})) return XKV_ERR_INVALID_ARG;

@@ -212,7 +212,7 @@ int rope_plan_init(const xkv_rope_config* c, xkv_rope_plan* plan) {
   plan->layout = c->layout;
   plan->reserved = 0;
   plan->gain = (float)(c->gain > 0.0 ? c->gain : yarn ? 0.1L * logl(factor) + 1.0L : 1.0L);
-  if (!(plan->gain > 0.0f) || isinf(plan->gain)) return XKV_ERR_INVALID_ARG;
+  if (!(plan->gain > 0.0f) || isinf(plan->gain) || isinf(1.0f / plan->gain)) return XKV_ERR_INVALID_ARG;     // (the inverse divides by it)
   for (int i = 0; i < XKV_ROPE_MAX_ROT / 2; ++i) {
     plan->turns[i] = 0;
     if (i >= n / 2) continue;

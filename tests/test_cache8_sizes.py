@@ -1,4 +1,4 @@
-"""Sizes at the ends of what rotary positions and the operators over a paged cache of codes take (no GPU needed)."""
+"""Sizes and factors at the ends of what rotary positions and the operators over a paged cache of codes take (no GPU needed)."""
 import ctypes
 
 import pytest
@@ -33,3 +33,15 @@ def test_tokens_of_an_append(xkv, no_gpu):  # noqa: F811
     assert calls(xkv, cfg, n=1 << 27)["append"] == xkv.XKV_ERR_UNSUPPORTED
     assert calls(xkv, cfg, n=(1 << 27) - 1)["append"] in (xkv.XKV_ERR_CUDA, xkv.XKV_ERR_ARCH)
     assert calls(xkv, cfg, n=1 << 27)["assign"] in (xkv.XKV_ERR_CUDA, xkv.XKV_ERR_ARCH)
+
+
+def test_a_gain_that_the_inverse_cannot_divide_by(xkv):  # noqa: F811
+    for gain in (1e-39, 1e-45, 1e39):
+        with pytest.raises(xkv.XKVError):
+            xkv.make_rope(d_h=64, gain=gain)
+    for gain in (1e-37, 1e38):
+        assert xkv.make_rope(d_h=64, gain=gain).gain == ctypes.c_float(gain).value
+    plan = xkv.make_rope(d_h=64)
+    t = xkv.xkv_rope_tensor(x=P, y=P, x_row=64, x_head=64, y_row=64, y_head=64, heads=1)
+    for plan.gain in (1e-39, float("inf"), float("nan"), 0.0):
+        assert xkv._lib.xkv_rope(ctypes.byref(plan), 2, 0, ctypes.byref(t), 1, 1, P, 1, None) == xkv.XKV_ERR_INVALID_ARG
