@@ -438,7 +438,7 @@ XKV_API int xkv_rope_plan_init(const xkv_rope_config* cfg, xkv_rope_plan* plan);
  *            of rows and of heads in elements (parts of a fused projection's output, say).  y may be x (in place); they must not
  *            overlap in another way.  Pointers aligned to the type's size.  heads >= 0; a tensor without heads does nothing.
  * rows       >= 0; row r has position pos[r % n_pos]: layers of a window that are rotated together share positions.
- * pos        int32 [n_pos], device, any values; n_pos >= 1 divides rows.
+ * pos        int32 [n_pos], device, any values; n_pos >= 1 divides rows (without rows there need be no positions either).
  * Errors: INVALID_ARG, UNSUPPORTED (rows * heads of a tensor 2^31 or more, or heads of both together 2^31 - 1024 or more), ARCH, CUDA.
  */
 #define XKV_ROPE_FORWARD 0

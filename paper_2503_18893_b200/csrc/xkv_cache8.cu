@@ -58,7 +58,8 @@ int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const xkv_rope_
       isinf(1.0f / plan->gain))
     return XKV_ERR_INVALID_ARG;
   if (direction < XKV_ROPE_FORWARD || direction > XKV_ROPE_INVERSE || type < XKV_BF16 || type > XKV_FP32) return XKV_ERR_INVALID_ARG;
-  if (rows < 0 || n_pos < 1 || rows % n_pos != 0 || !pos || !aligned_to(4, {pos})) return XKV_ERR_INVALID_ARG;
+  if (rows < 0 || n_pos < 0 || !aligned_to(4, {pos})) return XKV_ERR_INVALID_ARG;
+  if (rows > 0 && (n_pos == 0 || rows % n_pos != 0 || !pos)) return XKV_ERR_INVALID_ARG;
   int64_t heads = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const xkv_rope_tensor& t = tensors[i];

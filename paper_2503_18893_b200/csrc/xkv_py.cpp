@@ -568,7 +568,7 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     else if (ty.scalar_type() != st || ry != rx || hy != t[i].heads) what = "the output has another type or shape";
     else if (i == 1 && rx != rows) what = "both tensors have to have as many rows";
     else if (at::GradMode::is_enabled() && ty.requires_grad()) what = "what is written requires a gradient, which would not learn of the rotation";
-    else if (n_pos < 1 || rx % n_pos) what = "the number of positions does not divide the number of rows";
+    else if (rx > 0 && (n_pos < 1 || rx % n_pos)) what = "the number of positions does not divide the number of rows";
     if (what) {
       PyErr_Format(PyExc_ValueError, "%s: %s", names[i][0], what);
       return nullptr;
@@ -582,6 +582,7 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (n == 1) a.at = 7;
   void* s = a.stream();
   if (a.bad) return nullptr;
+  if (rows == 0) return PyLong_FromLong(XKV_OK);               // (no positions either: tensors without elements have no address)
   for (int i = 0; i < n; ++i) t[i].y = ys[i]->mutable_data_ptr();              // (a lazy clone gets memory of its own: before addresses are taken)
   for (int i = 0; i < n; ++i) t[i].x = xs[i]->const_data_ptr();
   int st;
