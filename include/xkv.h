@@ -463,7 +463,7 @@ XKV_API int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const x
  *   k_scale, v_scale  fp32 [G][n_pages][H_kv]: powers of two; a code c of the page and head stands for the value c * scale
  *   table             int32 [batch][max_pages]
  * A scale that is a power of two costs e4m3 nothing but range: codes are the values' own roundings to 4 significant bits (half a
- * step, 2^-4 of the value, down to 2^-15 of the page's largest).
+ * step, 2^-4 of the value, down to 2^-13 of the page's largest).
  *   xkv_page_assign    lengths of sequences that grow and shrink -> pages, places of new tokens
  *   xkv_cache8_append  new keys and values into their places
  *   xkv_cache8_read    rows back as an uncompressed cache (for xkv_dense_attend, xkv_tree_attend).  On the way to a compressed window one

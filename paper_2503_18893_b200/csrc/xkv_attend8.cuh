@@ -194,21 +194,6 @@ __device__ __forceinline__ Place find_piece(const Attend8Args& a, int c, int gri
 }
 
 // ---- 8-bit codes
-__device__ __forceinline__ uint32_t encode_f32x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t encode_e5m2x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ __half2 decode_f16x2(uint32_t codes) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
-  return *reinterpret_cast<__half2*>(&h);
-}
 // 2^(127 - e), finite for every e of 0 .. 255: rows that are left out are multiplied by it, too.
 __device__ __forceinline__ float turned_over(int e) { return __int_as_float(max((254 - e) << 23, 0x400000)); }
 // Does one of four codes say NaN?
@@ -341,9 +326,10 @@ __device__ __forceinline__ void encode_query(const uint4& x, uint2* hi, uint2* l
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
-    h[e] = encode_f32x2(x0, x1);
-    const float2 b = __half22float2(decode_f16x2(h[e]));
-    l[e] = SCALED ? encode_f32x2((x0 - b.x) * 32.0f, (x1 - b.y) * 32.0f) : encode_e5m2x2(x0 - b.x, x1 - b.y);
+    h[e] = ptx::pack_e4m3(x0, x1);
+    const uint32_t back = ptx::unpack_e4m3(h[e]);
+    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&back));
+    l[e] = SCALED ? ptx::pack_e4m3((x0 - b.x) * 32.0f, (x1 - b.y) * 32.0f) : ptx::pack_e5m2(x0 - b.x, x1 - b.y);
   }
   *hi = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
   *lo = make_uint2(l[0] | (l[1] << 16), l[2] | (l[3] << 16));

@@ -373,9 +373,8 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
           uint32_t h[8];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const __half2 lo = decode_f16x2(w[e]), hi = decode_f16x2(w[e] >> 16);
-            h[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
-            h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
+            h[2 * e] = unpack_e4m3(w[e]);
+            h[2 * e + 1] = unpack_e4m3(w[e] >> 16);
           }
           uint8_t* row = dst + (c >> 2) * L::kSlab + r * 128;  // 64 columns: four units of codes, eight of values
           const int u = 2 * (c & 3);

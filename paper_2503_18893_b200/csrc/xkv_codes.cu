@@ -44,15 +44,9 @@ __device__ __forceinline__ int exponent_of(float scale) { return ((__float_as_in
 __device__ __forceinline__ int exponent_for(uint32_t top) {
   return min(max((int)(top >> 7) - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0), kLowest), kHighest);
 }
-__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 __device__ __forceinline__ float2 decode2(uint32_t codes) {    // the two codes of the low half
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
-  return __half22float2(*reinterpret_cast<__half2*>(&h));
+  const uint32_t h = ptx::unpack_e4m3(codes);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 __device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
@@ -152,7 +146,7 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const CodesAr
         uint32_t* at = reinterpret_cast<uint32_t*>(codes) + i;
         const uint32_t c = old == kNothing ? 0u : *at;
         const float2 lo = decode2(c), hi = decode2(c >> 16);
-        *at = encode2(lo.x * f, lo.y * f) | (encode2(hi.x * f, hi.y * f) << 16);
+        *at = ptx::pack_e4m3(lo.x * f, lo.y * f) | (ptx::pack_e4m3(hi.x * f, hi.y * f) << 16);
       }
     }
     const float f = two_to(-e);
@@ -161,8 +155,8 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const CodesAr
       const int r = part * kRunRows + i;
       if (r < rows) {
         uint8_t* dst = codes + (size_t)(off + r) * DH + lane * (2 * W);
-        const uint32_t c = encode2(bf16_lo(v[i][0]) * f, bf16_hi(v[i][0]) * f);
-        if constexpr (W == 2) *reinterpret_cast<uint32_t*>(dst) = c | (encode2(bf16_lo(v[i][1]) * f, bf16_hi(v[i][1]) * f) << 16);
+        const uint32_t c = ptx::pack_e4m3(bf16_lo(v[i][0]) * f, bf16_hi(v[i][0]) * f);
+        if constexpr (W == 2) *reinterpret_cast<uint32_t*>(dst) = c | (ptx::pack_e4m3(bf16_lo(v[i][1]) * f, bf16_hi(v[i][1]) * f) << 16);
         else *reinterpret_cast<uint16_t*>(dst) = (uint16_t)c;
       }
     }

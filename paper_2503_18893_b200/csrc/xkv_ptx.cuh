@@ -239,6 +239,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
+// Two 8-bit codes, `lo` in the low byte, of two fp32 values (to nearest even, beyond the range the largest), and what e4m3 codes stand for
+// (the two of the low half; fp16 holds them exactly, two in a word).
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_e5m2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t unpack_e4m3(uint32_t codes) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+  return h;
+}
+
 // Shared-memory matrix descriptor of a K-major tile with 128-byte rows and 128-byte swizzle
 // (8-row groups 1024 bytes apart).  The tile base must be 1024-byte aligned; `byte_off` selects the
 // 32-byte K step inside the 128-byte row.
