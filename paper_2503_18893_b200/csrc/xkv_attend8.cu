@@ -26,9 +26,10 @@
 // All tiles of all problems form one list that is cut into as many even pieces as there are CTAs; a piece that holds a whole problem
 // writes its output, the others leave (O, m, l) for the merge.  Lengths are read on the device only.
 //
-// Bound by HBM.  131072 rows of four layers of eight heads, four query heads each: 171-174 us for pages of 16 to 128 rows (6.2 TB/s, 0.96 of
-// the copy's rate); eight sequences of up to 8191 rows 76; 32 of 2047 rows 99 (floor 84); 300 rows 10, latencies of two kernels.  What a
-// step brought (128k rows; eight sequences; pages of 16): warps that wait asleep instead of polling 187 -> 174, 99 -> 77, 105 -> 76; one
+// Bound by HBM.  131072 rows of four layers of eight heads, four query heads each: 168-174 us for pages of 16 to 128 rows (6.2-6.4 TB/s, 0.96
+// of the copy's rate); eight sequences of up to 8191 rows 76-79; 32 of 2047 rows 102-117 (floor 84); 300 rows 10, latencies of two kernels.
+// The fourth code of a weight and what keeps scales' extremes apart cost nothing where HBM bounds, 3 % at 32 sequences.  What a step
+// brought (128k rows; eight sequences; pages of 16): warps that wait asleep instead of polling 187 -> 174, 99 -> 77, 105 -> 76; one
 // issuing warp, two products for the two codes of a query 199, 102; the merge finding places for itself 105.
 #include <cuda.h>
 #include <math.h>
@@ -568,8 +569,9 @@ cudaError_t launch_width(const CUtensorMap& k_map, const CUtensorMap& v_map, con
 }
 
 // Query rows of a block: as few as hold the tokens of the longest sequence.  From 17 on they are the wide side of the products (32 rows a
-// head over 131072 rows of four layers of eight heads: 321 us, as the narrow side 357; over 8191 rows of one layer 29 and 38; 21 rows over
-// 3000 of three sequences 32.5 and 34.5).
+// head over 131072 rows of four layers of eight heads: 321 us, as the narrow side, with three codes of a weight, 357; over 8191 rows of one
+// layer 29 and 38; 21 rows over 3000 of three sequences 32.5 and 34.5).  One choice for all sequences of a call: beside a chunk's tokens a
+// single one takes a block of 128 rows, too.
 int block_rows(int max_new, int n_rep) {
   const long long rows = (long long)max_new * n_rep;
   return rows <= 8 ? 8 : rows <= 16 ? 16 : 128;
