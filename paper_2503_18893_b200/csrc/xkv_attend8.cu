@@ -378,9 +378,10 @@ attend8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
             const float m = fmaxf(fmaxf(top_s[wg][0][row], top_s[wg][1][row]), fmaxf(top_s[wg][2][row], top_s[wg][3][row]));
             float f = 1.0f;
             if (row < rows && m > info[row].y) {
-              f = info[row].y == -INFINITY ? 0.0f : exp2f(sub[row] - (m - kSet));
-              sub_s[par][wg][row] = m - kSet;
-              info_s[par][wg][row].y = m - kSet + kTop;
+              const float off = taken_off(m);
+              f = info[row].y == -INFINITY ? 0.0f : exp2f(sub[row] - off);
+              sub_s[par][wg][row] = off;
+              info_s[par][wg][row].y = weight_bound(off);
             }
             fac_s[wg][row] = f;
           }

@@ -17,6 +17,10 @@ namespace xkv {
 // tokens over 12301 rows takes 221 us with 2^8, 226 with 2^9, 236 with 2^11; 16 query rows of 131072 220, 220, 228.  m moves for its own
 // row's sake only: what a token attends to does not depend on the tokens beside it.)
 constexpr float kTop = 15.75f, kSet = 9.0f;    // log2
+// What is taken off z where the largest is m, and the largest z that it holds for; rounded so that a weight is at most 2^kTop also where
+// logits are too large for fp32 to hold m - kSet.
+__device__ __forceinline__ float taken_off(float m) { return __fadd_ru(m, -kSet); }
+__device__ __forceinline__ float weight_bound(float off) { return __fadd_rd(off, kTop); }
 
 // A whole warp waits (as wait_warp does), asleep for most of the time: warps that poll take their SM's issue slots from those that work.
 static __device__ bool wait8_slow(const Wait& w, uint32_t bar, uint32_t parity) {

@@ -209,7 +209,7 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         }
         // Both have their logits in registers now: weights may go where the other's lay.  Does a maximum move (or has a wait run out)?
         tc_fence_before();
-        const bool vote = !ok || (warp_live && top > m_used + kTop);
+        const bool vote = !ok || (warp_live && top > weight_bound(m_used));
         if (named_bar_any(pair, 64, vote)) {
           // O holds the tiles before this one once the last product is done, which the commit of the next S tells, or its own
           const bool next = s + 1 < n;
@@ -218,9 +218,9 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
           if (named_bar_any(pair, 64, !ok)) { gone = true; break; }
           tc_fence_after();
           const float m = fmaxf(top, tell_s[side ^ 1][row]);
-          const bool grow = m > m_used + kTop;
-          const float g = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - (m - kSet))) : 1.0f;
-          if (grow) m_used = m - kSet;
+          const bool grow = m > weight_bound(m_used);
+          const float g = grow ? (m_used == -INFINITY ? 0.0f : ex2_approx(m_used - taken_off(m))) : 1.0f;
+          if (grow) m_used = taken_off(m);
           l *= g;
           if (s > 0 && __any_sync(0xffffffffu, grow)) {
 #pragma unroll 1
@@ -238,18 +238,20 @@ attend8_wide_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_cons
         }
         tc_fence_after();
         if (warp_live) {
-          const float shift = m_used == -INFINITY ? 0.0f : m_used;
+          const float shift = m_used == -INFINITY ? 0.0f : -m_used;
+          const u64 shift2 = pack2(shift, shift);
 #pragma unroll
           for (int i = 0; i < NC; ++i) {       // P, two to a column, in the upper half of S's columns
             uint32_t r[16];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int c = 2 * i + h;
-              const u64 f2 = pack2(f[c], f[c]), b2 = pack2(e[c] - shift, e[c] - shift);
+              const u64 f2 = pack2(f[c], f[c]), e2 = pack2(e[c], e[c]);
               u64 sum = 0ull;
 #pragma unroll
               for (int x = 0; x < 8; ++x) {
-                float2 w = unpack2(fma2(pack2u(z[i][16 * h + 2 * x], z[i][16 * h + 2 * x + 1]), f2, b2));
+                // (first what the maximum was formed of, so that no weight passes its bound, however large logits are)
+                float2 w = unpack2(add2(fma2(pack2u(z[i][16 * h + 2 * x], z[i][16 * h + 2 * x + 1]), f2, e2), shift2));
                 w.x = ex2_approx(w.x);
                 w.y = ex2_approx(w.y);
                 sum = add2(sum, pack2(w.x, w.y));
