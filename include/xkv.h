@@ -475,9 +475,9 @@ XKV_API int xkv_rope(const xkv_rope_plan* plan, int direction, int type, const x
  * No handle and no allocation.  flags as for the uncompressed cache: one device word or NULL.  A page number outside [0, n_pages), a
  * length or a slot out of range is not followed: what it names is skipped, XKV_FLAG_INDEX_RANGE is raised.
  * Limits: d_h 64 or 128, H_q a multiple of H_kv with H_q/H_kv <= 16, page 16, 32, 64 or 128, max_pages * page <= XKV_CACHE_MAX_ROWS
- * (else INVALID_ARG); G*batch*H_kv <= 65535, G*n_pages*H_kv*page < 2^31; append, attend: G*n_tok*H_q < 2^31 (else UNSUPPORTED).  K8, V8, q, k, v, K, V, out
- * and workspaces are 16-byte aligned, int32 and fp32 arrays 4-byte.  Layers layer_begin <= l < layer_end are worked on; arrays span all
- * G.  Calls may run at the same time as long as none writes what another reads or writes.
+ * (else INVALID_ARG); G*batch*H_kv <= 65535, G*n_pages*H_kv*page < 2^31; append, attend: G*n_tok*H_q < 2^31 (else UNSUPPORTED).  K8,
+ * V8, q, k, v, K, V, out and workspaces are 16-byte aligned, int32 and fp32 arrays 4-byte.  Layers layer_begin <= l < layer_end are
+ * worked on; arrays span all G.  Calls may run at the same time as long as none writes what another reads or writes.
  * Errors of all of them: INVALID_ARG, UNSUPPORTED, ARCH, CUDA.
  */
 typedef struct {
@@ -530,7 +530,8 @@ XKV_API int xkv_cache8_append(const xkv_cache8_config* cfg, int layer_begin, int
                               void* stream);
 
 /*
- * K, V bf16 [G][batch][H_kv][cap][d_h]: row j < length[b] becomes what its codes stand for (exactly); rows at and behind length[b], and rows of pages out of range, are left as they were.
+ * K, V bf16 [G][batch][H_kv][cap][d_h]: row j < length[b] becomes what its codes stand for (exactly); rows at and behind length[b],
+ * and rows of pages out of range, are left as they were.
  * length  int32 [batch], 0 <= length[b] <= min(cap, max_pages * page) (else clamped, flag).  1 <= cap <= XKV_CACHE_MAX_ROWS;
  *         G*batch*H_kv*cap < 2^31 (else UNSUPPORTED).  K or V may be NULL: that one is not read back.
  */
@@ -550,14 +551,15 @@ XKV_API int xkv_cache8_read(const xkv_cache8_config* cfg, int layer_begin, int l
  *            overlap (two streams, two captured graphs that are replayed at once) need one each.
  * out        bf16 [G][n_tok][H_q][d_h];  lse  optional fp32 [G][n_tok][H_q], natural logarithm of the sum of exp of scaled logits.
  * Tokens that belong to no sequence (before first[0], behind first[batch]) are left as they were.  A token that attends to nothing
- * (length[b] - n_b + i < 0, or all its rows' pages out of range), or whose logits are all minus infinity, gets 0 and lse -inf.
- * A row that a token does not attend to has no influence on it, also where its codes are NaN.  A query with an element that is not
- * finite gets NaN.  Scales are read as powers of two (their exponents), values' between 2^-90 and 2^120; one of 0 marks a page that holds nothing: it is left out,
- * whatever its other one is.  One that is not finite makes NaN of the tokens that attend to its page's rows.
+ * (length[b] - n_b + i < 0, or all its rows' pages out of range), or whose logits are all minus infinity, gets 0 and lse -inf. A row
+ * that a token does not attend to has no influence on it, also where its codes are NaN.  A query with an element that is not finite
+ * gets NaN.  Scales are read as powers of two (their exponents), values' between 2^-90 and 2^120; one of 0 marks a page that holds
+ * nothing: it is left out, whatever its other one is.  One that is not finite makes NaN of the tokens that attend to its page's rows.
  * Queries enter the product with the keys to 2^-21 of their largest element, weights the one with the values to 2^-11 of themselves or
- * 2^-34 of the largest weight (times its value's scale); sums, maxima and the products' accumulation are fp32.  A logit carries
- * the exponent of its value's scale: beyond 2^17 rows of equal logits in pages of different scales may differ in weight by 2^-24 of the logit.  What values of one head
- * stand for may differ by 2^60 between its pages; beyond that the denominator loses the fainter page's share.
+ * 2^-34 of the largest weight (times its value's scale); sums, maxima and the products' accumulation are fp32.  A logit carries the
+ * exponent of its value's scale: beyond 2^17 rows of equal logits in pages of different scales may differ in weight by 2^-24 of the
+ * logit.  What values of one head stand for may differ by 2^60 between its pages; beyond that the denominator loses the fainter page's
+ * share.
  */
 XKV_API int xkv_cache8_workspace_bytes(const xkv_cache8_config* cfg, int32_t max_new, uint64_t* bytes);
 XKV_API int xkv_cache8_attend(const xkv_cache8_config* cfg, int layer_begin, int layer_end, const void* q, const int32_t* first,

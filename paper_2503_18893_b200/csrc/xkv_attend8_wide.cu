@@ -14,8 +14,8 @@
 //              when a weight would pass 2^15.75 (kTop): one vote of the two warps per tile
 // Bound by the softmax: what a warp does for a row of a tile (logits from tensor memory, maximum, exponentials, weights back) is longer than
 // its instructions, and two warps of an SM's quarter do not fill it; warps that poll beside them make it worse.  131072 rows of four layers of
-// eight heads with four query heads: 8 tokens 327 us, 16 340, 32 366; a chunk of 512 tokens over 12301 rows of two sequences, seven query
-// heads, 225 (0.64 PFLOP/s).  What did not help, with a merge that took 12 us more: one thread a row and blocks of 256 rows (steps of half a
+// eight heads with four query heads: 8 tokens 327 us, 16 341, 32 368; a chunk of 512 tokens over 12301 rows of two sequences, seven query
+// heads, 227 (0.63 PFLOP/s).  What did not help, with a merge that took 12 us more: one thread a row and blocks of 256 rows (steps of half a
 // tile) 231 for the chunk and 412 for 32 tokens; softmax warps that poll 275 and 431; two threads a row and 256 rows 323 (registers); 256
 // rows with whole tiles, S once, 251.
 #include <math.h>
