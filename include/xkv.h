@@ -557,8 +557,8 @@ XKV_API int xkv_cache8_read(const xkv_cache8_config* cfg, int layer_begin, int l
  * nothing: it is left out, whatever its other one is.  One that is not finite makes NaN of the tokens that attend to its page's rows.
  * Queries enter the product with the keys to 2^-21 of their largest element, weights the one with the values to 2^-11 of themselves or
  * 2^-34 of the largest weight (times its value's scale); sums, maxima and the products' accumulation are fp32.  A logit carries the
- * exponent of its value's scale: beyond 2^17 rows of equal logits in pages of different scales may differ in weight by 2^-24 of the
- * logit.  What values of one head stand for may differ by 2^60 between its pages; beyond that the denominator loses the fainter page's
+ * exponent of its value's scale: where logits pass 2^17, those of rows in pages of different scales are rounded apart, by 2^-24 of
+ * them.  What values of one head stand for may differ by 2^60 between its pages; beyond that the denominator loses the fainter page's
  * share.
  */
 XKV_API int xkv_cache8_workspace_bytes(const xkv_cache8_config* cfg, int32_t max_new, uint64_t* bytes);
